@@ -15,6 +15,8 @@
  *                        (paper section 4.2.1)
  *   blink_make_schedule_servers / blink_hybrid_split
  *                        several servers, two classes of links (sections 3.5, 3.4)
+ *   blink_embedding* / blink_route* / blink_orthogonal*
+ *                        what a training step does around its collectives
  *
  * Conventions
  *   - Every function that can fail returns blink_status_t; results come back
@@ -61,7 +63,8 @@ typedef enum {
     BLINK_ELIMIT = 7         /* the schedule does not fit the fixed device block of blink_allreduce_noalloc */
 } blink_status_t;
 
-typedef enum { BLINK_INT32 = 0, BLINK_FP32 = 1 } blink_dtype_t;
+/* The collectives take INT32 and FP32; what each of the operators takes is said there. */
+typedef enum { BLINK_INT32 = 0, BLINK_FP32 = 1, BLINK_BF16 = 2, BLINK_FP16 = 3, BLINK_INT64 = 4 } blink_dtype_t;
 /* Collectives (paper section 4.1).  REDUCE is the reduce phase of AllReduce on
  * its own: afterwards only the root of each tree holds the result (on that
  * tree's share); what the other ranks' buffers hold is unspecified. */
@@ -483,6 +486,85 @@ size_t blink_miad_chunk(const blink_miad_t* m);   /* chunk for the next iteratio
 int blink_miad_steady(const blink_miad_t* m);     /* 1 once the search has ended */
 blink_status_t blink_miad_report(blink_miad_t* m, double throughput);
 void blink_miad_free(blink_miad_t* m);
+
+/* ---- operators around the collectives ---------------------------------------------------
+ *
+ * What a data-parallel training step does next to its collectives: the rows of an embedding
+ * table and the gradient that ranks then sum, a router's choice of experts with the counts
+ * and sums that ranks then add up, and the orthogonalised update of a matrix once its
+ * gradient is summed.  Each call enqueues gfx950 kernels on the stream and returns; none
+ * allocates, copies or synchronises, so each can be recorded into a HIP graph, and calls
+ * on different streams are independent if their buffers are.
+ *   - All buffers are device memory unless "host" is said; strides count elements.
+ *   - workspace: device memory of at least the bytes that the *_workspace function returns
+ *     for the call's sizes (0: none is needed, or the sizes are refused), 256-byte aligned,
+ *     with any contents; the call's own until it has run.
+ *   - Results are the same from call to call: no number is added by an atomic.
+ *   - Outputs may not overlap inputs, except where "in place" is said.
+ *   - Floating types are FP32, BF16, FP16; sums are formed in 32 bits or more and rounded once.
+ */
+
+/* out[i] = scale * table[tokens[i]], rows of dim elements, for i < n_tokens; a token outside
+ * [0, vocab) is padding, its row is zero.  Tokens are INT32 or INT64. */
+blink_status_t blink_embedding(const void* table, blink_dtype_t table_type, size_t vocab, size_t dim, size_t table_stride,
+                               const void* tokens, blink_dtype_t token_type, size_t n_tokens, float scale,
+                               void* out, blink_dtype_t out_type, size_t out_stride, void* stream);
+
+/* grad_table[v] = scale * (sum of grad_out[i] over the i with tokens[i] = v), added to what is
+ * there if accumulate is 1.  Else every row is written, zeros where no token names it.
+ * grad_stride may be 0 (one row for all tokens).  Padding tokens add nothing. */
+size_t blink_embedding_gradient_workspace(size_t n_tokens, size_t vocab, size_t dim);
+blink_status_t blink_embedding_gradient(const void* tokens, blink_dtype_t token_type, size_t n_tokens,
+                                        const void* grad_out, blink_dtype_t grad_type, size_t grad_stride,
+                                        float scale, int accumulate, void* grad_table, blink_dtype_t table_type,
+                                        size_t vocab, size_t dim, size_t table_stride,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* A router: for every token the k (<= n_experts <= 1024) largest of its logits, the lowest
+ * index first among equals, with p = softmax(logits).
+ *   keep      null, or a byte per token: where it is 0 the token is left out of everything
+ *   chosen    [n_tokens][k]; -1 where no logit above -inf is left, and for tokens left out
+ *   weights   [n_tokens][k]: p of the chosen, divided by its sum over them if normalize; 0 next to a -1
+ *   counts    [n_experts + 1]: tokens that chose each expert; last the tokens counted (kept, and not all -inf)
+ *   sums      [n_experts + 1]: sum of p over the tokens counted; last that of log(sum exp(logits))^2
+ * counts and sums add up over ranks: blink_allreduce on INT32 and on FP32.  A NaN or +inf among
+ * the logits of a token that is kept makes its p NaN; a NaN is not chosen. */
+size_t blink_route_workspace(size_t n_tokens, int n_experts);
+blink_status_t blink_route(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride,
+                           const uint8_t* keep, int k, int normalize, int32_t* chosen, float* weights,
+                           int32_t* counts, float* sums, void* workspace, size_t workspace_bytes, void* stream);
+/* loss[1] = balance * n_experts / (k n^2) * sum_e counts[e] sums[e], which is least where all
+ * experts are used alike; loss[2] = z / n * sums[n_experts], which keeps logits small; loss[0] their
+ * sum.  n = counts[n_experts]; zeros if that is 0. */
+blink_status_t blink_route_loss(const int32_t* counts, const float* sums, int n_experts, int k,
+                                float balance, float z, float* loss, void* stream);
+/* Gradient of grad_loss[0] * loss[0] (grad_loss null: 1) plus what the gradient of the weights,
+ * grad_weights [n_tokens][k] (null: none), adds; zeros for tokens that are not counted.  counts as
+ * they went into the loss (over all ranks), themselves without a gradient; the other arguments as in blink_route. */
+blink_status_t blink_route_gradient(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride,
+                                    const uint8_t* keep, int k, int normalize, const int32_t* chosen,
+                                    const float* grad_weights, const int32_t* counts, const float* grad_loss,
+                                    float balance, float z, void* grad_logits, size_t grad_stride, void* stream);
+
+/* Each of `batch` matrices (rows x cols) moved towards the nearest matrix with orthonormal rows
+ * (columns, if there are fewer): X = M / (|M| + eps), |.| the Frobenius norm, then for each of the `steps` (1 to 64)
+ * coefficients a, b, c (host, 3 * steps): X <- a X + (b A + c A A) X with A = X X' (of the
+ * transpose where rows > cols).  EINVAL where the coefficients let singular values that
+ * start in [0, 1] pass 1.95 or the polynomial a + b s^2 + c s^4 pass 7.75.  dtype: of the matrix and the
+ * result.  FP32 is computed to 32 bits' accuracy, BF16 and FP16 to 16 bits'.  In place: out may be the matrix. */
+size_t blink_orthogonalize_workspace(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype);
+blink_status_t blink_orthogonalize(const void* matrix, blink_dtype_t dtype, size_t batch, size_t rows, size_t cols,
+                                   size_t row_stride, size_t batch_stride, const float* coefficients, int steps, float eps,
+                                   void* out, size_t out_row_stride, size_t out_batch_stride,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+/* An optimiser's step with it: momentum_out = beta * momentum + grad; the update is that, or
+ * grad + beta * momentum_out if nesterov; weights_out = (1 - decay) * weights - rate *
+ * orthogonalised update.  All are contiguous [batch][rows][cols], FP32 but for the gradient.  In place: weights_out may
+ * be weights, momentum_out may be momentum.  Workspace: blink_orthogonalize_workspace of FP32. */
+blink_status_t blink_orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out,
+                                     const void* grad, blink_dtype_t grad_type, size_t batch, size_t rows, size_t cols,
+                                     float beta, int nesterov, const float* coefficients, int steps, float eps,
+                                     float rate, float decay, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* blink_strerror(blink_status_t st);
 

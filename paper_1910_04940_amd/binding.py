@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libblink.so")
 BLINK_MAX_RANKS = 16
 BLINK_ROOT_ANY = -1
 BLINK_OK, BLINK_EINVAL, BLINK_EDISCONNECTED, BLINK_ENOMEM, BLINK_EMISMATCH, BLINK_EHIP, BLINK_ESTUCK, BLINK_ELIMIT = range(8)
-BLINK_INT32, BLINK_FP32 = 0, 1
+BLINK_INT32, BLINK_FP32, BLINK_BF16, BLINK_FP16, BLINK_INT64 = 0, 1, 2, 3, 4
 BLINK_OP_BROADCAST, BLINK_OP_ALLREDUCE, BLINK_OP_REDUCE, BLINK_OP_ALLGATHER, BLINK_OP_GATHER = 0, 1, 2, 3, 4
 BLINK_SUM, BLINK_PROD, BLINK_MIN, BLINK_MAX = 0, 1, 2, 3
 BLINK_STEP_REDUCE, BLINK_STEP_COPY = 0, 1
@@ -55,6 +55,9 @@ EXPORTS = [
     "blink_schedule_set_wait_limit", "blink_schedule_test_skip_call", "blink_allreduce_noalloc",
     "blink_schedule_set_kernel", "blink_schedule_last_kernel", "blink_schedule_set_sweep", "blink_schedule_get_tickets", "blink_schedule_batch",
     "blink_schedule_kernel_bytes", "blink_schedule_set_hand_over", "blink_schedule_handed_over",
+    "blink_embedding", "blink_embedding_gradient_workspace", "blink_embedding_gradient", "blink_route_workspace",
+    "blink_route", "blink_route_loss", "blink_route_gradient", "blink_orthogonalize_workspace", "blink_orthogonalize",
+    "blink_orthogonal_step",
 ]
 
 
@@ -160,6 +163,17 @@ def lib() -> C.CDLL:
     L.blink_miad_report.argtypes = [vp, C.c_double]
     L.blink_miad_free.argtypes = [vp]
     L.blink_miad_free.restype = None
+    z, f, i = C.c_size_t, C.c_float, C.c_int   # the operators around the collectives
+    L.blink_embedding.argtypes = [vp, i, z, z, z, vp, i, z, f, vp, i, z, vp]
+    L.blink_embedding_gradient.argtypes = [vp, i, z, vp, i, z, f, i, vp, i, z, z, z, vp, z, vp]
+    L.blink_route.argtypes = [vp, i, z, i, z, vp, i, i, vp, vp, vp, vp, vp, z, vp]
+    L.blink_route_loss.argtypes = [vp, vp, i, i, f, f, vp, vp]
+    L.blink_route_gradient.argtypes = [vp, i, z, i, z, vp, i, i, vp, vp, vp, vp, f, f, vp, z, vp]
+    L.blink_orthogonalize.argtypes = [vp, i, z, z, z, z, z, C.POINTER(f), i, f, vp, z, z, vp, z, vp]
+    L.blink_orthogonal_step.argtypes = [vp, vp, vp, vp, vp, i, z, z, z, f, i, C.POINTER(f), i, f, f, f, vp, z, vp]
+    for name, sizes in (("embedding_gradient", [z, z, z]), ("route", [z, i]), ("orthogonalize", [z, z, z, i])):
+        getattr(L, f"blink_{name}_workspace").argtypes = sizes
+        getattr(L, f"blink_{name}_workspace").restype = z
     L.blink_strerror.argtypes = [C.c_int]
     L.blink_strerror.restype = C.c_char_p
     try:

@@ -1,0 +1,559 @@
+// Rows of an embedding table for tokens, and the gradient of the table.
+//
+//   rows      out[i] = scale * table[token[i]]
+//   gradient  table'[v] = scale * sum of grad[i] over the i with token[i] = v, in the order of i
+//
+// A token outside [0, vocab) is padding: its row is zero and its gradient goes nowhere.
+//
+// Both are bound by memory.  The gradient is formed without atomics on numbers, so that it is the same every time: the
+// tokens are sorted with their positions (a stable radix sort), and the sorted list is merged with the table's rows:
+// "row ends" and "positions" form one sequence in which position j of the sorted list has the place j + token[j] and the
+// end of row v the place v + (tokens up to v).  Every wave takes an equal stretch of that sequence and walks it, so a
+// row named by thousands of tokens and a thousand rows named by none cost what they move, every row is written once,
+// and a stretch's start is found by a search over the sorted list.  What a stretch has of a row that it does not begin
+// or does not end goes to the workspace in 32 bits; a second kernel joins those in order.
+#include "operators_api.hpp"
+
+#include <algorithm>
+
+namespace blink {
+namespace {
+
+// ---- rows ---------------------------------------------------------------------------------------------------------------
+constexpr int kRowThreads = 256;
+constexpr int kRowUnits = 4;   // packs of one thread, their loads under way together
+
+// A pack is V elements; a row has `packs` of them.  Places go out pack by pack through all rows, so short and long rows
+// fill the waves alike.
+template <typename In, typename Out, typename Token, int V>
+__global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, uint64_t vocab, uint64_t table_stride, const Token* tokens,
+                                                              uint64_t units, uint32_t packs, float scale, Out* out, uint64_t out_stride) {
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kRowThreads * kRowUnits) + threadIdx.x;
+    int64_t token[kRowUnits];
+    uint64_t row[kRowUnits];
+    uint32_t at[kRowUnits];
+#pragma unroll
+    for (int u = 0; u < kRowUnits; ++u) {
+        const uint64_t unit = first + u * kRowThreads;
+        row[u] = unit >> 32 ? unit / packs : static_cast<uint32_t>(unit) / packs;
+        at[u] = static_cast<uint32_t>(unit - row[u] * packs) * V;
+        token[u] = unit < units ? static_cast<int64_t>(tokens[row[u]]) : -1;
+    }
+    Pack<In, V> x[kRowUnits];
+#pragma unroll
+    for (int u = 0; u < kRowUnits; ++u) {
+        x[u] = Pack<In, V>{};
+        if (static_cast<uint64_t>(token[u]) < vocab)
+            x[u] = *reinterpret_cast<const Pack<In, V>*>(table + static_cast<uint64_t>(token[u]) * table_stride + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowUnits; ++u) {
+        Pack<Out, V> y;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {   // (a padding token's row is +0 whatever the scale)
+            float z = scale * static_cast<float>(x[u].v[i]);
+            if constexpr (sizeof(Out) < 4) asm("" : "+v"(z));   // a 32-bit product: the mixed 16-bit one rounds it otherwise
+            y.v[i] = static_cast<uint64_t>(token[u]) < vocab ? static_cast<Out>(z) : static_cast<Out>(0.0f);
+        }
+        if (first + u * kRowThreads < units) *reinterpret_cast<Pack<Out, V>*>(out + row[u] * out_stride + at[u]) = y;
+    }
+}
+
+// ---- sorting tokens with their positions ------------------------------------------------------------------------------------
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+
+// Ranks the items of a wave by digit, 64 at a time in order: counts[digit] goes up by the wave's items with that digit,
+// the result is an item's place among them.  Items of lanes that are not `in` count nowhere.
+__device__ inline uint32_t rank_in_wave(uint32_t digit, bool in, int bits, volatile uint32_t* counts) {
+    const uint32_t lane = threadIdx.x & 63;
+    unsigned long long same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = digit >> b & 1;
+        const unsigned long long ones = __ballot(one);
+        same &= one ? ones : ~ones;
+    }
+    const uint32_t below = __popcll(same & ((1ull << lane) - 1));
+    uint32_t before = 0;
+    if (in) {
+        before = counts[digit];
+        if (below == 0) counts[digit] = before + __popcll(same);
+    }
+    return before + below;
+}
+
+// From counts[wave][digit]: the wave's items with that digit come at counts[wave][digit] (afterwards) past the digit's
+// begin, which is returned for digit = thread (sum of all smaller digits' items).
+template <int THREADS>
+__device__ inline uint32_t scan_counts(uint32_t (*counts)[kDigits], int digits, uint32_t* wave_sum) {
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint32_t total = 0;
+    if (t < digits)
+        for (int w = 0; w < THREADS / 64; ++w) {
+            const uint32_t c = counts[w][t];
+            counts[w][t] = total;
+            total += c;
+        }
+    uint32_t sum = total;
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+    }
+    if (lane == 63) wave_sum[wave] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += wave_sum[w];
+    __syncthreads();
+    return before + sum - total;
+}
+
+template <typename Token>
+__device__ inline uint32_t key_of(Token token, uint32_t vocab) {
+    return static_cast<uint64_t>(static_cast<int64_t>(token)) < vocab ? static_cast<uint32_t>(token) : vocab;
+}
+
+// Up to kOneThreads * kOneItems tokens: one workgroup, the list in LDS from pass to pass.
+constexpr int kOneThreads = 1024, kOneItems = 8, kOneMost = kOneThreads * kOneItems;
+template <typename Token>
+__global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* tokens, uint32_t n, uint32_t vocab, int bits, int passes,
+                                                                  uint32_t* key_out, uint32_t* pos_out) {
+    __shared__ uint32_t counts[kOneThreads / 64][kDigits];
+    __shared__ uint32_t begin[kDigits], wave_sum[kOneThreads / 64];
+    __shared__ uint32_t keys[kOneMost], places[kOneMost];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    // every wave has a run of whole 64s, as few as hold them all
+    const uint32_t rounds = (n + kOneThreads - 1) / kOneThreads;
+    const uint32_t first = wave * rounds * 64 + lane;
+    uint32_t key[kOneItems], pos[kOneItems], rank[kOneItems];
+    for (int pass = 0, shift = 0; pass < passes; ++pass, shift += bits) {
+        for (int i = t; i < kOneThreads / 64 * kDigits; i += kOneThreads) counts[i / kDigits][i % kDigits] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kOneItems; ++j)
+            if (j < static_cast<int>(rounds)) {
+                const uint32_t i = first + j * 64;
+                const bool in = i < n;
+                key[j] = !in ? 0 : pass == 0 ? key_of(tokens[i], vocab) : keys[i];
+                pos[j] = !in ? 0 : pass == 0 ? i : places[i];
+                rank[j] = rank_in_wave(key[j] >> shift & ((1u << bits) - 1), in, bits, counts[wave]);
+            }
+        __syncthreads();
+        const uint32_t b = scan_counts<kOneThreads>(counts, 1 << bits, wave_sum);
+        if (t < 1 << bits) begin[t] = b;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kOneItems; ++j)
+            if (j < static_cast<int>(rounds) && first + j * 64 < n) {
+                const uint32_t digit = key[j] >> shift & ((1u << bits) - 1);
+                const uint32_t to = begin[digit] + counts[wave][digit] + rank[j];
+                (pass == passes - 1 ? key_out : keys)[to] = key[j];
+                (pass == passes - 1 ? pos_out : places)[to] = pos[j];
+            }
+        __syncthreads();
+    }
+}
+
+// More tokens: tiles of kTile.  Each pass counts the digits of every tile, sums the counts along the tiles, and moves.
+constexpr int kTileThreads = 512, kTileItems = 4, kTile = kTileThreads * kTileItems;
+static_assert(kDigits <= kTileThreads, "a thread per digit");
+
+template <typename Token>
+__global__ __launch_bounds__(kTileThreads) void embedding_sort_count(const Token* tokens, const uint32_t* keys, uint32_t n, uint32_t vocab, int shift,
+                                                                     int bits, uint32_t tiles, uint32_t* counts) {
+    __shared__ uint32_t count[kDigits];
+    const int t = threadIdx.x;
+    count[t] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kTileItems; ++j) {
+        const uint32_t i = blockIdx.x * kTile + j * kTileThreads + t;
+        if (i < n) atomicAdd(&count[(tokens ? key_of(tokens[i], vocab) : keys[i]) >> shift & ((1u << bits) - 1)], 1u);
+    }
+    __syncthreads();
+    if (t < 1 << bits) counts[static_cast<uint64_t>(t) * tiles + blockIdx.x] = count[t];
+}
+
+// One workgroup per digit: counts along the tiles become the items before each tile's, and their sum.
+constexpr int kScanThreads = 256;
+__global__ __launch_bounds__(kScanThreads) void embedding_sort_scan(uint32_t* counts, uint32_t tiles, uint32_t* totals) {
+    __shared__ uint32_t wave_sum[kScanThreads / 64];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint32_t* const row = counts + static_cast<uint64_t>(blockIdx.x) * tiles;
+    uint32_t before = 0;
+    for (uint32_t lo = 0; lo < tiles; lo += kScanThreads) {
+        const uint32_t c = lo + t < tiles ? row[lo + t] : 0;
+        uint32_t sum = c;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        if (lane == 63) wave_sum[wave] = sum;
+        __syncthreads();
+        uint32_t all = 0, mine = 0;
+        for (int w = 0; w < kScanThreads / 64; ++w) {
+            if (w == wave) mine = all;
+            all += wave_sum[w];
+        }
+        if (lo + t < tiles) row[lo + t] = before + mine + sum - c;
+        before += all;
+        __syncthreads();
+    }
+    if (t == 0) totals[blockIdx.x] = before;
+}
+
+template <typename Token>
+__global__ __launch_bounds__(kTileThreads) void embedding_sort_move(const Token* tokens, const uint32_t* keys, const uint32_t* places, uint32_t n,
+                                                                    uint32_t vocab, int shift, int bits, uint32_t tiles, const uint32_t* before,
+                                                                    const uint32_t* totals, uint32_t* key_out, uint32_t* pos_out) {
+    __shared__ uint32_t counts[kTileThreads / 64][kDigits];
+    __shared__ uint32_t begin[kDigits], wave_sum[kTileThreads / 64];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, digits = 1 << bits;
+    for (int w = 0; w < kTileThreads / 64; ++w) counts[w][t] = 0;
+    // where each digit begins: the sum of the smaller digits' totals, and this tile's place among the digit's items
+    uint32_t sum = t < digits ? totals[t] : 0;
+    const uint32_t own = sum, ahead = t < digits ? before[static_cast<uint64_t>(t) * tiles + blockIdx.x] : 0;
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+    }
+    if (lane == 63) wave_sum[wave] = sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) sum += wave_sum[w];
+    begin[t] = sum - own + ahead;
+    const uint32_t first = blockIdx.x * kTile + wave * (64 * kTileItems) + lane;
+    uint32_t key[kTileItems], pos[kTileItems], rank[kTileItems];
+#pragma unroll
+    for (int j = 0; j < kTileItems; ++j) {
+        const uint32_t i = first + j * 64;
+        const bool in = i < n;
+        key[j] = !in ? 0 : tokens ? key_of(tokens[i], vocab) : keys[i];
+        pos[j] = !in ? 0 : tokens ? i : places[i];
+    }
+#pragma unroll
+    for (int j = 0; j < kTileItems; ++j) rank[j] = rank_in_wave(key[j] >> shift & (digits - 1), first + j * 64 < n, bits, counts[wave]);
+    __syncthreads();
+    if (t < digits) {
+        uint32_t total = 0;
+        for (int w = 0; w < kTileThreads / 64; ++w) {
+            const uint32_t c = counts[w][t];
+            counts[w][t] = total;
+            total += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kTileItems; ++j)
+        if (first + j * 64 < n) {
+            const uint32_t digit = key[j] >> shift & (digits - 1), to = begin[digit] + counts[wave][digit] + rank[j];
+            key_out[to] = key[j];
+            pos_out[to] = pos[j];
+        }
+}
+
+// ---- the sums ---------------------------------------------------------------------------------------------------------------
+// How many of the sorted positions come before place `d`: those j with j + key[j] < d (ALL), or d itself where rows that no
+// token names are left alone and only positions have places.  A wave's 64 lanes probe 64 positions at a time.
+template <bool ALL>
+__device__ inline uint32_t positions_before(const uint32_t* keys, uint32_t n, uint64_t d) {
+    if (!ALL) return static_cast<uint32_t>(d < n ? d : n);
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t lo = 0, hi = n;   // the answer is in [lo, hi]
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + 63) / 64;
+        const uint64_t j = lo + static_cast<uint64_t>(step) * lane;
+        const bool before = j < hi && j + keys[j] < d;
+        const int many = __popcll(__ballot(before));
+        if (many == 0) return lo;
+        const uint64_t top = static_cast<uint64_t>(lo) + static_cast<uint64_t>(step) * many;
+        lo += step * (many - 1) + 1;
+        hi = static_cast<uint32_t>(top < hi ? top : hi);
+    }
+    return lo;
+}
+
+struct Sums {
+    const void* grad;
+    uint64_t grad_stride;
+    const uint32_t *keys, *places;
+    uint32_t n, vocab, dim;
+    float scale;
+    void* table;
+    uint64_t table_stride;
+    uint32_t stretch;         // places of a wave
+    uint32_t stretches;
+    float *head, *tail;       // [stretch][dim]: what a stretch has of a row that began before it, of one that does not end in it
+    uint32_t dim_up;          // elements of a row of head and tail
+};
+
+template <typename T, int V>
+__device__ inline void load_up(float (&x)[V], const T* p) {
+    const Pack<T, V> y = *reinterpret_cast<const Pack<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = static_cast<float>(y.v[i]);
+}
+// The row's final sum: scaled, added to what is there where ADD, rounded once.
+template <typename T, int V, bool ADD>
+__device__ inline void store_row(T* p, const float (&sum)[V], float scale) {
+    Pack<T, V> y;
+    if (ADD) y = *reinterpret_cast<const Pack<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) y.v[i] = static_cast<T>(ADD ? __builtin_fmaf(scale, sum[i], static_cast<float>(y.v[i])) : scale * sum[i]);
+    *reinterpret_cast<Pack<T, V>*>(p) = y;
+}
+
+constexpr int kSumThreads = 256;
+constexpr int kSumAhead = 8;   // rows of a sum whose loads are under way together
+
+// A wave: V elements per lane of the columns [64 V y, ...) of the rows of its stretch.  ALL: rows that no token names are
+// written as zeros, else (ADD too) left alone.
+template <typename Grad, typename T, int V, bool ADD>
+__global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
+    constexpr bool ALL = !ADD;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    if (w >= s.stretches) return;
+    const uint32_t lane = threadIdx.x & 63, col = (blockIdx.y * 64 + lane) * V;
+    const bool in = col < s.dim;
+    const Grad* const grad = static_cast<const Grad*>(s.grad) + (in ? col : 0);
+    T* const table = static_cast<T*>(s.table) + (in ? col : 0);
+    const uint64_t places = static_cast<uint64_t>(s.n) + (ALL ? s.vocab : 0), d0 = static_cast<uint64_t>(w) * s.stretch;
+    const uint64_t d1 = d0 + s.stretch < places ? d0 + s.stretch : places;
+    uint32_t p = __builtin_amdgcn_readfirstlane(positions_before<ALL>(s.keys, s.n, d0));
+    const uint32_t end = __builtin_amdgcn_readfirstlane(positions_before<ALL>(s.keys, s.n, d1));
+    const uint32_t r_end = static_cast<uint32_t>(ALL ? d1 - end : s.vocab);   // rows below it end here (ALL)
+    uint32_t r = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ALL ? d0 - p : p < end ? s.keys[p] : s.vocab));
+    bool begun = p > 0 && r < s.vocab && __builtin_amdgcn_readfirstlane(s.keys[p - 1]) == r;   // the row has positions in an earlier stretch
+    bool any = false;                                                                          // and in this one
+    float sum[V] = {};
+    const auto finish = [&] {   // row r ends
+        if (in) {
+            if (begun) *reinterpret_cast<Pack<float, V>*>(s.head + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
+            else if (ALL || any) store_row<T, V, ADD>(table + static_cast<uint64_t>(r) * s.table_stride, sum, s.scale);
+        }
+        begun = any = false;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    };
+    const auto finish_up_to = [&](uint32_t next) {
+        if (!ALL) {
+            if (r != next) finish();
+            r = next;
+        } else
+            for (; r < next; ++r) finish();
+    };
+    while (p < end) {
+        const uint32_t many = end - p < 64 ? end - p : 64;
+        const uint32_t key = lane < many ? s.keys[p + lane] : s.vocab, place = lane < many ? s.places[p + lane] : 0;
+        const uint32_t real = __popcll(__ballot(key < s.vocab));   // padding comes last
+        for (uint32_t j = 0; j < real; j += kSumAhead) {
+            float x[kSumAhead][V];
+#pragma unroll
+            for (int a = 0; a < kSumAhead; ++a)
+                if (j + a < real) {
+                    const uint32_t row = __builtin_amdgcn_readlane(place, j + a);
+                    if (in) load_up<Grad, V>(x[a], grad + static_cast<uint64_t>(row) * s.grad_stride);
+                }
+#pragma unroll
+            for (int a = 0; a < kSumAhead; ++a)
+                if (j + a < real) {
+                    finish_up_to(__builtin_amdgcn_readlane(key, j + a));
+                    any = true;
+                    if (in)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) sum[i] += x[a][i];
+                }
+        }
+        p += many;
+        if (real < many) break;
+    }
+    if (ALL) finish_up_to(r_end);
+    if (!any) return;
+    if (!ALL && (p >= s.n || __builtin_amdgcn_readfirstlane(s.keys[p]) != r)) finish();
+    else if (in) *reinterpret_cast<Pack<float, V>*>(s.tail + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
+}
+
+// Rows that several stretches share: their sums, joined in the order of the stretches.  A workgroup looks at the stretch in
+// which such a row ends; its waves take equal parts of the stretches before.
+constexpr int kJoinThreads = 512;
+template <typename T, int V, bool ADD>
+__global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
+    constexpr bool ALL = !ADD;
+    __shared__ Pack<float, V> part[kJoinThreads / 64][64];
+    const uint32_t w = blockIdx.x + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t places = static_cast<uint64_t>(s.n) + (ALL ? s.vocab : 0), d0 = static_cast<uint64_t>(w) * s.stretch;
+    const uint64_t d1 = d0 + s.stretch < places ? d0 + s.stretch : places;
+    const uint32_t p = positions_before<ALL>(s.keys, s.n, d0);
+    if (p == 0) return;
+    const uint32_t r = s.keys[p - 1];
+    if (r >= s.vocab) return;
+    if (ALL ? d0 - p != r : p >= s.n || s.keys[p] != r) return;   // no row reaches into this stretch
+    // the row ends here?
+    const uint32_t end = positions_before<ALL>(s.keys, s.n, d1);
+    if (ALL ? d1 - end <= r : end < s.n && s.keys[end] == r) return;
+    // the first position of the row: [lo, hi] holds it
+    uint32_t lo = 0, hi = p - 1;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (s.keys[mid] < r) lo = mid + 1;
+        else hi = mid;
+    }
+    const uint32_t from = static_cast<uint32_t>((static_cast<uint64_t>(lo) + (ALL ? r : 0)) / s.stretch), many = w - from;
+    const uint32_t col = (blockIdx.y * 64 + lane) * V;
+    const bool in = col < s.dim;
+    const uint32_t each = (many + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
+    const uint32_t a = from + min(many, wave * each), b = from + min(many, (wave + 1) * each);
+    float sum[V] = {};
+    if (in) {
+#pragma unroll 8
+        for (uint32_t i = a; i < b; ++i) {
+            float x[V];
+            load_up<float, V>(x, s.tail + static_cast<uint64_t>(i) * s.dim_up + col);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += x[v];
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) part[wave][lane].v[v] = sum[v];
+    __syncthreads();
+    if (wave != 0 || !in) return;
+    for (int o = 1; o < kJoinThreads / 64; ++o)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += part[o][lane].v[v];
+    float x[V];
+    load_up<float, V>(x, s.head + static_cast<uint64_t>(w) * s.dim_up + col);
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] += x[v];
+    store_row<T, V, ADD>(static_cast<T*>(s.table) + static_cast<uint64_t>(r) * s.table_stride + col, sum, s.scale);
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------------------
+// What the sort and the sums need of a call, by its sizes alone.
+struct GradientPlan {
+    int bits = 0, passes = 0;
+    uint32_t tiles = 0, stretch = 0, stretches_all = 0, stretches_add = 0, dim_up = 0;
+    size_t bytes = 0;
+    uint32_t *key[2], *place[2], *counts, *totals;
+    float *head, *tail;
+};
+
+GradientPlan plan_gradient(size_t n, size_t vocab, size_t dim, void* workspace) {
+    GradientPlan g;
+    int all = 1;   // keys are 0 ... vocab, the last for padding
+    while (vocab >> all) ++all;
+    g.passes = (all + kDigitBits - 1) / kDigitBits;
+    g.bits = (all + g.passes - 1) / g.passes;
+    g.tiles = n <= kOneMost ? 1 : static_cast<uint32_t>(ceil_div(n, kTile));
+    g.dim_up = static_cast<uint32_t>((dim + 7) / 8 * 8);
+    // 64 places to a stretch; fewer where that leaves the GPU without waves, at least 8 (below that the joining costs more)
+    const uint64_t columns = ceil_div(dim, 256);
+    g.stretch = static_cast<uint32_t>(std::min<uint64_t>(64, std::max<uint64_t>(8, (n + vocab) * columns / 8192)));
+    g.stretches_all = static_cast<uint32_t>(ceil_div(n + vocab, g.stretch));
+    g.stretches_add = static_cast<uint32_t>(ceil_div(n, g.stretch));
+    Carve c(workspace);
+    for (int i = 0; i < 2; ++i) {
+        g.key[i] = c.take<uint32_t>(n);
+        g.place[i] = c.take<uint32_t>(n);
+    }
+    g.counts = c.take<uint32_t>(g.tiles > 1 ? static_cast<size_t>(g.tiles) << g.bits : 0);
+    g.totals = c.take<uint32_t>(g.tiles > 1 ? kDigits : 0);
+    // only stretches that a token's position lies in have such rows, but any may
+    const size_t rows = n > 0 ? static_cast<size_t>(g.stretches_all) * g.dim_up : 0;
+    g.head = c.take<float>(rows);
+    g.tail = c.take<float>(rows);
+    g.bytes = c.at;
+    return g;
+}
+
+template <typename Token>
+blink_status_t sort_tokens(const Token* tokens, uint32_t n, uint32_t vocab, const GradientPlan& g, hipStream_t stream, int* where) {
+    if (g.tiles == 1) {
+        *where = 0;
+        return launch(embedding_sort_one<Token>, dim3(1), dim3(kOneThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
+    }
+    for (int pass = 0; pass < g.passes; ++pass) {
+        const Token* const from = pass == 0 ? tokens : nullptr;
+        const int shift = pass * g.bits, in = (pass + 1) & 1, out = pass & 1;
+        BLINK_TRY(launch(embedding_sort_count<Token>, dim3(g.tiles), dim3(kTileThreads), stream, from, g.key[in], n, vocab, shift, g.bits, g.tiles, g.counts));
+        BLINK_TRY(launch(embedding_sort_scan, dim3(1u << g.bits), dim3(kScanThreads), stream, g.counts, g.tiles, g.totals));
+        BLINK_TRY(launch(embedding_sort_move<Token>, dim3(g.tiles), dim3(kTileThreads), stream, from, g.key[in], g.place[in], n, vocab, shift, g.bits,
+                         g.tiles, g.counts, g.totals, g.key[out], g.place[out]));
+        *where = out;
+    }
+    return BLINK_OK;
+}
+
+template <typename Grad, typename T, int V>
+blink_status_t run_sums(const Sums& s, bool add, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kSumThreads / 64)), static_cast<uint32_t>(ceil_div(s.dim, 64 * V)));
+    BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, grid, dim3(kSumThreads), stream, s));
+    if (s.n < 2 || s.stretches < 2) return BLINK_OK;   // no row lies in two stretches
+    return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, dim3(s.stretches - 1, grid.y), dim3(kJoinThreads), stream, s);
+}
+
+}  // namespace
+
+size_t embedding_gradient_workspace(size_t n, size_t vocab, size_t dim) { return plan_gradient(n, vocab, dim, nullptr).bytes; }
+
+blink_status_t embedding(const void* table, blink_dtype_t table_type, size_t vocab, size_t dim, size_t table_stride, const void* tokens,
+                         blink_dtype_t token_type, size_t n, float scale, void* out, blink_dtype_t out_type, size_t out_stride, hipStream_t stream) {
+    if (n == 0 || dim == 0) return BLINK_OK;
+    return with_float(table_type, [&](auto in) {
+        return with_float(out_type, [&](auto to) -> blink_status_t {
+            using In = decltype(in);
+            using Out = decltype(to);
+            constexpr int kMost = 16 / static_cast<int>(sizeof(In) > sizeof(Out) ? sizeof(In) : sizeof(Out));
+            const auto fits = [&](size_t v) {
+                return dim % v == 0 && table_stride % v == 0 && out_stride % v == 0 && aligned(table, v * sizeof(In)) && aligned(out, v * sizeof(Out));
+            };
+            const int v = fits(kMost) ? kMost : 1;
+            const uint64_t packs = dim / v, units = n * packs, blocks = ceil_div(units, kRowThreads * kRowUnits);
+            if (blocks > 0x7fffffff) return BLINK_EINVAL;
+            const auto with_token = [&](auto token) {
+                using Token = decltype(token);
+                const auto kernel = v == kMost ? embedding_rows<In, Out, Token, kMost> : embedding_rows<In, Out, Token, 1>;
+                return launch(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kRowThreads), stream, static_cast<const In*>(table), vocab, table_stride,
+                              static_cast<const Token*>(tokens), units, static_cast<uint32_t>(packs), scale, static_cast<Out*>(out), out_stride);
+            };
+            return token_type == BLINK_INT64 ? with_token(int64_t()) : with_token(int32_t());
+        });
+    });
+}
+
+blink_status_t embedding_gradient(const void* tokens, blink_dtype_t token_type, size_t n, const void* grad, blink_dtype_t grad_type,
+                                  size_t grad_stride, float scale, bool accumulate, void* table, blink_dtype_t table_type, size_t vocab, size_t dim,
+                                  size_t table_stride, void* workspace, hipStream_t stream) {
+    if (vocab == 0 || dim == 0 || (n == 0 && accumulate)) return BLINK_OK;
+    const GradientPlan g = plan_gradient(n, vocab, dim, workspace);
+    int where = 0;
+    const uint32_t n32 = static_cast<uint32_t>(n), v32 = static_cast<uint32_t>(vocab);
+    if (n > 0) {
+        BLINK_TRY(token_type == BLINK_INT64 ? sort_tokens(static_cast<const int64_t*>(tokens), n32, v32, g, stream, &where)
+                                            : sort_tokens(static_cast<const int32_t*>(tokens), n32, v32, g, stream, &where));
+    }
+    Sums s;
+    s.grad = grad;
+    s.grad_stride = grad_stride;
+    s.keys = g.key[where];
+    s.places = g.place[where];
+    s.n = n32;
+    s.vocab = v32;
+    s.dim = static_cast<uint32_t>(dim);
+    s.scale = scale;
+    s.table = table;
+    s.table_stride = table_stride;
+    s.stretch = g.stretch;
+    s.stretches = accumulate ? g.stretches_add : g.stretches_all;
+    s.head = g.head;
+    s.tail = g.tail;
+    s.dim_up = g.dim_up;
+    return with_float(grad_type, [&](auto from) {
+        return with_float(table_type, [&](auto to) -> blink_status_t {
+            using Grad = decltype(from);
+            using T = decltype(to);
+            constexpr int kMost = 16 / static_cast<int>(sizeof(Grad) > sizeof(T) ? sizeof(Grad) : sizeof(T));
+            const bool wide = dim % kMost == 0 && grad_stride % kMost == 0 && table_stride % kMost == 0 && aligned(grad, kMost * sizeof(Grad)) &&
+                              aligned(table, kMost * sizeof(T));
+            return wide ? run_sums<Grad, T, kMost>(s, accumulate, stream) : run_sums<Grad, T, 1>(s, accumulate, stream);
+        });
+    });
+}
+
+}  // namespace blink

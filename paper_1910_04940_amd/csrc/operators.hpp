@@ -1,0 +1,76 @@
+// What the operators around the collectives share (embedding.hip, route.hip, orthogonal.hip): element types, wide
+// loads, the launch.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <cstdio>
+#include <tuple>
+#include <utility>
+
+#include "../../include/blink.h"
+
+namespace blink {
+
+// N elements that are loaded and stored at once; rows of them start on their alignment wherever this is used.
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack {
+    T v[N];
+};
+
+inline size_t size_of(blink_dtype_t t) { return t == BLINK_INT64 ? 8 : t == BLINK_BF16 || t == BLINK_FP16 ? 2 : 4; }
+inline bool is_float(blink_dtype_t t) { return t == BLINK_FP32 || t == BLINK_BF16 || t == BLINK_FP16; }
+inline bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// Calls f with a value of the C++ type of `t` (a floating one).
+template <typename F>
+auto with_float(blink_dtype_t t, F f) {
+    if (t == BLINK_BF16) return f(__bf16());
+    if (t == BLINK_FP16) return f(_Float16());
+    return f(float());
+}
+
+// hipLaunchKernel returns its own error, not one that somebody else's call left behind.
+template <typename... P, size_t... I>
+blink_status_t launch_with(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, std::tuple<P...>& args, std::index_sequence<I...>) {
+    void* at[] = {static_cast<void*>(&std::get<I>(args))...};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, 0, stream);
+    if (err == hipSuccess) return BLINK_OK;
+    std::fprintf(stderr, "blink: kernel launch failed: %s\n", hipGetErrorString(err));
+    return err == hipErrorOutOfMemory ? BLINK_ENOMEM : BLINK_EHIP;
+}
+template <typename... P, typename... A>
+blink_status_t launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, A... a) {
+    std::tuple<P...> args(static_cast<P>(a)...);
+    return launch_with(kernel, grid, block, stream, args, std::index_sequence_for<P...>());
+}
+
+// Orders a wave's accesses to LDS for the compiler; the wave itself makes them in order.
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+#define BLINK_TRY(call)                                   \
+    do {                                                  \
+        const blink_status_t st__ = (call);               \
+        if (st__ != BLINK_OK) return st__;                \
+    } while (0)
+
+inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// Parts of a workspace, each on a 256-byte line.
+struct Carve {
+    char* base;
+    size_t at = 0;
+    explicit Carve(void* p) : base(static_cast<char*>(p)) {}
+    template <typename T>
+    T* take(size_t n) {
+        T* const p = reinterpret_cast<T*>(base + at);
+        at += (n * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+}  // namespace blink

@@ -1,0 +1,515 @@
+// Orthogonalised updates: the iteration of Newton and Schulz, which moves a matrix's singular values towards 1.
+//
+//   X = U / (|U| + eps)     (Frobenius norm; the transpose where U is tall, so that X is m x n with m <= n)
+//   then for every step (a, b, c):  A = X X',  B = a I + b A + c A A,  X <- B X
+//
+// Bound by matrix products: m^2 n + m^3 + 2 m^2 n multiplications and additions a step, A and B being symmetric: of
+// those only the tiles on and below the diagonal are computed.
+//
+// Numerics.  The products run on the 16-bit matrix instructions with sums in 32 bits.  An error in A or B is relative to X and
+// stays so; one in X lies across the small singular values, which a step makes up to a times larger, so X needs more
+// bits than the result has.  X is kept as a pair of 16-bit floats, hi = round(x) and lo = round(x - hi), 22 bits together.  For a
+// 32-bit matrix so are A and B, and a product is the sum of three: hi hi + hi lo + lo hi.  Against 64 bits (1024 x
+// 1024, five steps): relative error 2e-7 like that, 1e-5 with 32-bit floats throughout.  For a 16-bit matrix, whose result is rounded to
+// 8 or 11 bits, A and B are single 16-bit floats, A from X's hi alone: 9e-4 before the rounding, where bfloat16 throughout
+// has 9e-3.  Everything is scaled by powers of two, so that what is stored lies in the middle of the 16-bit range.
+//
+// Layout.  All three products are sums over the contiguous index of both operands: A = X X', A A = A A', X B' with B'
+// = B, so X is kept both ways round (X for the first, its transpose for the third).  A row of pairs is a sequence of groups of 128
+// bytes, 32 hi and then their 32 lo, so one stage of a tile's row is one line of memory.  Sizes are rounded up to whole tiles with
+// zeros, which the iteration keeps, and only the first and the last pass see the caller's sizes and strides.
+#include "operators_api.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace blink {
+namespace {
+
+using Half = _Float16;
+typedef Half Half8 __attribute__((ext_vector_type(8)));
+typedef float Float16v __attribute__((ext_vector_type(16)));
+
+// Powers of two: |X| <= 2 (singular values of what the caller's coefficients allow, see coefficients_fit), |A| <= 4, |B| < 8.
+constexpr float kScaleX = 16384.0f, kScaleA = 16384.0f, kScaleB = 8192.0f;
+
+enum Last { kNone = 0, kMatrix, kWeights };   // what the last product writes: the matrix, or weights updated by it
+
+// The caller's side: what is read at the start and written at the end.
+struct Outer {
+    const void* in;          // U, or the gradient
+    uint64_t in_row, in_batch;
+    const float* momentum;   // null: U is `in`
+    float* momentum_out;
+    float beta;
+    bool nesterov;
+    uint32_t rows, cols;
+    const float* weights;
+    float* weights_out;
+    void* out;
+    uint64_t out_row, out_batch;
+    float rate, keep;        // weights' = keep * weights - rate * result
+};
+
+// U's element, given the new momentum where there is one.
+template <typename In>
+__device__ inline float update_of(const Outer& o, uint64_t batch, uint32_t r, uint32_t c) {
+    const float g = static_cast<float>(static_cast<const In*>(o.in)[batch * o.in_batch + r * o.in_row + c]);
+    if (!o.momentum) return g;
+    const float m = o.momentum_out[(batch * o.rows + r) * o.cols + c];
+    return o.nesterov ? __builtin_fmaf(o.beta, m, g) : m;
+}
+
+// ---- the norm, and the momentum ------------------------------------------------------------------------------------------
+// A workgroup per part of a matrix; squares are added in 64 bits, where no 32-bit float's overflows or vanishes.
+constexpr int kNormThreads = 256, kNormMost = 256;
+template <typename In>
+__global__ __launch_bounds__(kNormThreads) void ortho_norm(const Outer o, double* parts) {
+    __shared__ double wave_sum[kNormThreads / 64];
+    const uint64_t batch = blockIdx.y, all = static_cast<uint64_t>(o.rows) * o.cols;
+    double s = 0.0;
+    for (uint64_t e = blockIdx.x * static_cast<uint64_t>(kNormThreads) + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kNormThreads) {
+        const uint32_t r = static_cast<uint32_t>(all >> 32 ? e / o.cols : static_cast<uint32_t>(e) / o.cols), c = static_cast<uint32_t>(e - static_cast<uint64_t>(r) * o.cols);
+        if (o.momentum) {
+            const float g = static_cast<float>(static_cast<const In*>(o.in)[batch * o.in_batch + r * o.in_row + c]);
+            o.momentum_out[batch * all + e] = __builtin_fmaf(o.beta, o.momentum[batch * all + e], g);
+        }
+        const double u = update_of<In>(o, batch, r, c);
+        s += u * u;
+    }
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormThreads / 64; ++w) s += wave_sum[w];
+        parts[batch * gridDim.x + blockIdx.x] = s;
+    }
+}
+
+// ---- 16-bit storage ----------------------------------------------------------------------------------------------------------
+// Sixteen values of a row from column j (a multiple of 16) on.
+template <bool PAIR>
+__device__ inline void store16(Half* row, uint32_t j, const float (&v)[16]) {
+    Half8 h[2], l[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const Half hi = static_cast<Half>(v[i]);
+        h[i / 8][i % 8] = hi;
+        if (PAIR) l[i / 8][i % 8] = static_cast<Half>(v[i] - static_cast<float>(hi));
+    }
+    Half* const at = PAIR ? row + (j >> 5) * 64 + (j & 31) : row + j;
+    *reinterpret_cast<Half8*>(at) = h[0];
+    *reinterpret_cast<Half8*>(at + 8) = h[1];
+    if (PAIR) {
+        *reinterpret_cast<Half8*>(at + 32) = l[0];
+        *reinterpret_cast<Half8*>(at + 40) = l[1];
+    }
+}
+template <bool PAIR>
+__device__ inline void load16(float (&v)[16], const Half* row, uint32_t j) {
+    const Half* const at = PAIR ? row + (j >> 5) * 64 + (j & 31) : row + j;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const Half8 h = *reinterpret_cast<const Half8*>(at + 8 * q);
+        Half8 l = {};
+        if (PAIR) l = *reinterpret_cast<const Half8*>(at + 32 + 8 * q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * q + i] = static_cast<float>(h[i]) + (PAIR ? static_cast<float>(l[i]) : 0.0f);
+    }
+}
+
+// ---- X and its transpose from U ------------------------------------------------------------------------------------------------
+// 64 x 64 of X to a workgroup.  X's own rows are pairs where PAIR, its transpose's always are.
+constexpr int kFirstThreads = 256;
+template <typename In, bool PAIR>
+__global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool tall, const double* parts, uint32_t n_parts, float eps, uint32_t mp, uint32_t np,
+                                                             Half* x, Half* xt) {
+    __shared__ float tile[64][65];
+    __shared__ double factor;   // its product with an element is a 32-bit float, itself it may be past their range
+    const int t = threadIdx.x;
+    const uint64_t batch = blockIdx.z;
+    const uint32_t i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+    if (t < 64) {
+        double s = 0.0;
+        for (uint32_t p = t; p < n_parts; p += 64) s += parts[batch * n_parts + p];
+        for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+        if (t == 0) {   // a matrix of zeros, its norm and eps both 0, stays one
+            const double norm = sqrt(s) + eps;
+            factor = norm == 0.0 ? 0.0 : kScaleX / norm;
+        }
+    }
+    // along the caller's contiguous index: X's columns, or its rows where U is tall
+    const uint32_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {
+        const uint32_t r = q * 4 + t / 64, c = t % 64;
+        const float u = r0 + r < o.rows && c0 + c < o.cols ? update_of<In>(o, batch, r0 + r, c0 + c) : 0.0f;
+        if (tall) tile[c][r] = u;
+        else tile[r][c] = u;
+    }
+    __syncthreads();
+    const double f = factor;
+    const uint32_t row = t / 4, col = t % 4 * 16;
+    constexpr uint32_t kX = PAIR ? 2 : 1;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(tile[row][col + i] * f);
+    store16<PAIR>(x + (batch * mp + i0 + row) * np * kX, j0 + col, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(tile[col + i][row] * f);
+    store16<true>(xt + (batch * np + j0 + row) * mp * 2, i0 + col, v);
+}
+
+// ---- the products --------------------------------------------------------------------------------------------------------------
+enum Product { kGram, kSquare, kApply, kApplyLast };   // A = X X', B of A, X <- B X, the result
+
+struct Factors {
+    const Half *p, *q;     // out[i][j] = sum over k of p[i][k] q[j][k]
+    uint32_t mp, np;       // rows of p and q
+    uint32_t k;            // a multiple of the stage
+    uint32_t tiles, tiles_n;
+    const Half* a;         // kSquare: A itself
+    Half *out, *out_t;     // what is written, and its transpose (kApply); A and B are their own transposes
+    float c0, c1, c2;      // factors of I, of A, of the product
+    float eps;
+};
+
+// A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, or 64 where both operands are
+// single, so a row of a stage is 128 bytes (64 where it is single and the other is not).  Stages are copied to LDS by
+// the loads themselves, one ahead of the stage that is multiplied.  The eight 16-byte parts of a line lie in the order part ^
+// line % 8, so that a block's 32 rows, read part by part, fall on all banks.
+template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+struct Tile {
+    static constexpr int kThreads = WAVES_M * WAVES_N * 64;
+    static constexpr int kStage = PP || QP ? 32 : 64;                 // of k
+    static constexpr int kLineP = PP == QP || PP ? 128 : 64, kLineQ = PP == QP || QP ? 128 : 64;   // bytes of a row's stage
+    static constexpr int kBytesP = TM * kLineP, kBytesQ = TN * kLineQ, kBytes = kBytesP + kBytesQ;
+    static constexpr int kWM = TM / WAVES_M, kWN = TN / WAVES_N, kBM = kWM / 32, kBN = kWN / 32;
+    static constexpr int kBlock = 32 * 33 * 4;                        // bytes of a wave's block at the end
+    static_assert(WAVES_M * WAVES_N * kBlock <= 2 * kBytes, "the blocks fit the stages");
+};
+
+template <int LINE>
+__device__ inline uint32_t slot_of(uint32_t row, uint32_t part) {   // byte offset of a part of a row
+    if constexpr (LINE == 128) return row * 128 + ((part ^ (row & 7)) * 16);
+    else {   // two rows to a line
+        const uint32_t line = row >> 1, at = (row & 1) * 4 + part;
+        return line * 128 + ((at ^ (line & 7)) * 16);
+    }
+}
+
+// Copies rows [row0, row0 + ROWS) of a stage: every thread 16 bytes at a time, in the order of LDS, each from where its part is.
+template <int ROWS, int LINE, int THREADS>
+__device__ inline void copy_stage(const Half* from, uint64_t pitch, uint32_t k_bytes, char* to) {
+    constexpr int kTimes = ROWS * LINE / 16 / THREADS;
+    static_assert(kTimes * THREADS * 16 == ROWS * LINE, "whole rounds");
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kTimes; ++u) {
+        const uint32_t at = u * THREADS + t, line = at >> 3, slot = (at & 7) ^ (line & 7);
+        const uint32_t row = LINE == 128 ? line : line * 2 + (slot >> 2), part = LINE == 128 ? slot : slot & 3;
+        const char* const g = reinterpret_cast<const char*>(from) + row * pitch + k_bytes + part * 16;
+        char* const l = to + (u * THREADS + (t & ~63)) * 16;   // of the wave; lanes follow one another
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+    }
+}
+
+template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+__device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES_M / 32][TN / WAVES_N / 32], int wm, int wn) {
+    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    const char* const p = at;
+    const char* const q = at + S::kBytesP;
+#pragma unroll
+    for (int ks = 0; ks < S::kStage / 16; ++ks) {   // 16 of k: two parts of 8
+        const uint32_t part = ks * 2 + half;
+        Half8 ph[S::kBM], pl[S::kBM], qh[S::kBN], ql[S::kBN];
+#pragma unroll
+        for (int i = 0; i < S::kBM; ++i) {
+            const uint32_t r = wm * S::kWM + i * 32 + row;
+            ph[i] = *reinterpret_cast<const Half8*>(p + slot_of<S::kLineP>(r, part));
+            if (PP) pl[i] = *reinterpret_cast<const Half8*>(p + slot_of<S::kLineP>(r, part + 4));
+        }
+#pragma unroll
+        for (int j = 0; j < S::kBN; ++j) {
+            const uint32_t r = wn * S::kWN + j * 32 + row;
+            qh[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part));
+            if (QP) ql[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part + 4));
+        }
+#pragma unroll
+        for (int i = 0; i < S::kBM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kBN; ++j) {
+                if (QP) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
+                if (PP) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
+            }
+    }
+}
+
+// XP: X's own rows are pairs (and A's and B's).
+template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
+    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
+    __shared__ __align__(1024) char even[S::kBytes];
+    __shared__ __align__(1024) char odd[S::kBytes];
+    constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
+    static_assert(!kSymmetric || TM == TN, "square tiles");
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / WAVES_N, wn = wave % WAVES_N;
+    // workgroups go round the eight dies in turn: each die gets a run of neighbouring tiles
+    const uint32_t all = gridDim.x, per = all >> 3, bid = blockIdx.x;
+    const uint32_t place = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
+    const uint64_t batch = place / f.tiles;
+    const uint32_t tile = place - static_cast<uint32_t>(batch) * f.tiles;
+    uint32_t ti, tj;
+    if (kSymmetric) {   // rows of the triangle: row i has i + 1 tiles
+        ti = static_cast<uint32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+        while (ti * (ti + 1) / 2 > tile) --ti;
+        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+        tj = tile - ti * (ti + 1) / 2;
+    } else {
+        ti = tile / f.tiles_n;
+        tj = tile - ti * f.tiles_n;
+    }
+    const uint64_t pitch_p = static_cast<uint64_t>(f.k) * (PP ? 4 : 2), pitch_q = static_cast<uint64_t>(f.k) * (QP ? 4 : 2);   // bytes
+    const Half* const p = f.p + (batch * f.mp + ti * TM) * (pitch_p / 2);
+    const Half* const q = f.q + (batch * f.np + tj * TN) * (pitch_q / 2);
+    Float16v acc[S::kBM][S::kBN] = {};
+    const auto copy = [&](uint32_t stage, char* to) {
+        copy_stage<TM, S::kLineP, S::kThreads>(p, pitch_p, stage * S::kLineP, to);
+        copy_stage<TN, S::kLineQ, S::kThreads>(q, pitch_q, stage * S::kLineQ, to + S::kBytesP);
+    };
+    const auto arrived = [] {   // this wave's copies; then everybody's
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+    };
+    const uint32_t stages = f.k / S::kStage;
+    copy(0, even);
+    for (uint32_t s = 0; s < stages; s += 2) {
+        arrived();
+        if (s + 1 < stages) copy(s + 1, odd);
+        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(even, acc, wm, wn);
+        if (s + 1 == stages) break;
+        arrived();
+        if (s + 2 < stages) copy(s + 2, even);
+        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(odd, acc, wm, wn);
+    }
+    __syncthreads();
+    // 32 x 32 at a time through LDS, so that rows are written whole in both directions
+    constexpr int kFits = S::kBytes / S::kBlock;
+    float* const block = reinterpret_cast<float*>((wave < kFits ? even : odd) + (wave < kFits ? wave : wave - kFits) * S::kBlock);
+    const uint32_t i0 = ti * TM + wm * S::kWM, j0 = tj * TN + wn * S::kWN;
+#pragma unroll
+    for (int bi = 0; bi < S::kBM; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < S::kBN; ++bj) {
+            const uint32_t i = i0 + bi * 32, j = j0 + bj * 32;
+            wave_sync();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) block[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * 33 + (lane & 31)] = acc[bi][bj][r] * f.c2;
+            wave_sync();
+            if constexpr (WHAT == kApplyLast) {
+#pragma unroll 4
+                for (int u = 0; u < 16; ++u) {
+                    const uint32_t r = u * 2 + (lane >> 5), c = lane & 31;   // of the caller's matrix
+                    const float v = tall ? block[c * 33 + r] : block[r * 33 + c];
+                    const uint32_t row = (tall ? j : i) + r, col = (tall ? i : j) + c;
+                    if (row < o.rows && col < o.cols) {
+                        if constexpr (LAST == kWeights) {
+                            const uint64_t at = (batch * o.rows + row) * o.cols + col;
+                            o.weights_out[at] = __builtin_fmaf(-o.rate, v, o.keep * o.weights[at]);
+                        } else {
+                            static_cast<Out*>(o.out)[batch * o.out_batch + row * o.out_row + col] = static_cast<Out>(v);
+                        }
+                    }
+                }
+            } else {
+                const uint32_t r = lane >> 1, c = (lane & 1) * 16;
+                float v[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) v[u] = block[r * 33 + c + u];
+                if constexpr (WHAT == kSquare) {
+                    float a[16];
+                    load16<XP>(a, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) {
+                        v[u] = __builtin_fmaf(f.c1, a[u], v[u]) + (i + r == j + c + u ? f.c0 : 0.0f);
+                        block[r * 33 + c + u] = v[u];
+                    }
+                    wave_sync();
+                }
+                store16<XP>(f.out + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c, v);
+                // the transpose: of A and B the tile on the other side of the diagonal
+                if (!kSymmetric || ti != tj) {
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) v[u] = block[(c + u) * 33 + r];
+                    if constexpr (kSymmetric) store16<XP>(f.out + (batch * f.mp + j + r) * f.np * (XP ? 2 : 1), i + c, v);
+                    else store16<true>(f.out_t + (batch * f.np + j + r) * f.mp * 2, i + c, v);
+                }
+            }
+        }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------------------------
+struct Sizes {
+    uint32_t m, n, mp, np, tile;
+    uint32_t norm_parts;
+    bool pair;
+};
+
+// Tiles of 256 keep the matrix instructions busiest, if there are about as many as compute units; smaller ones fill the GPU.
+Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
+    Sizes z;
+    z.m = static_cast<uint32_t>(std::min(rows, cols));
+    z.n = static_cast<uint32_t>(std::max(rows, cols));
+    const auto tiles = [&](uint64_t t) { return batch * ceil_div(z.m, t) * ceil_div(z.n, t); };
+    z.tile = tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+    z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
+    z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
+    z.pair = dtype == BLINK_FP32;
+    // parts of 4096 elements, so that a part's sum costs no more than its loads
+    z.norm_parts = static_cast<uint32_t>(std::max<uint64_t>(1, std::min<uint64_t>(kNormMost, ceil_div(static_cast<uint64_t>(rows) * cols, 4096))));
+    return z;
+}
+
+struct Space {
+    double* parts;
+    Half *x, *xt[2], *a, *b;
+    size_t bytes;
+};
+Space space_of(const Sizes& z, size_t batch, void* workspace) {
+    Space s;
+    Carve c(workspace);
+    const size_t mn = batch * z.mp * z.np, mm = batch * z.mp * z.mp, one = z.pair ? 2 : 1;
+    s.parts = c.take<double>(batch * z.norm_parts);
+    s.x = c.take<Half>(mn * one);
+    for (Half*& t : s.xt) t = c.take<Half>(mn * 2);
+    s.a = c.take<Half>(mm * one);
+    s.b = c.take<Half>(mm * one);
+    s.bytes = c.at;
+    return s;
+}
+
+// T: the tile's edge.  XP: the three factors' rows are pairs (a 32-bit matrix), else only those of X's transpose are.
+template <int T, bool XP, Product WHAT, Last LAST, typename Out>
+blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t batch, hipStream_t stream) {
+    constexpr bool kQ = XP || WHAT == kApply || WHAT == kApplyLast;
+    constexpr int kM = 2, kN = T == 256 ? 4 : 2;
+    Factors g = f;
+    const uint32_t tm = f.mp / T, tn = f.np / T;
+    g.tiles_n = tn;
+    g.tiles = WHAT == kGram || WHAT == kSquare ? tm * (tm + 1) / 2 : tm * tn;
+    const uint64_t groups = static_cast<uint64_t>(g.tiles) * batch;
+    if (groups > 0x7fffffff) return BLINK_EINVAL;
+    return launch(ortho_product<T, T, kM, kN, XP, kQ, XP, WHAT, LAST, Out>, dim3(static_cast<uint32_t>(groups)), dim3(kM * kN * 64), stream, g, o, tall);
+}
+
+template <int T, bool XP, Last LAST, typename Out>
+blink_status_t iterate(const Sizes& z, const Space& s, const Outer& o, bool tall, size_t batch, const float* co, int steps, hipStream_t stream) {
+    for (int step = 0; step < steps; ++step, co += 3) {
+        Factors f{};
+        f.p = f.q = s.x;
+        f.mp = f.np = z.mp;
+        f.k = z.np;
+        f.out = s.a;
+        f.c2 = kScaleA / (kScaleX * kScaleX);
+        BLINK_TRY((run_product<T, XP, kGram, kNone, float>(f, o, tall, batch, stream)));
+        f.p = f.q = f.a = s.a;
+        f.k = z.mp;
+        f.out = s.b;
+        f.c0 = co[0] * kScaleB;
+        f.c1 = co[1] * (kScaleB / kScaleA);
+        f.c2 = co[2] * (kScaleB / (kScaleA * kScaleA));
+        BLINK_TRY((run_product<T, XP, kSquare, kNone, float>(f, o, tall, batch, stream)));
+        f.p = s.b;
+        f.q = s.xt[step & 1];
+        f.np = z.np;
+        f.out = s.x;
+        f.out_t = s.xt[~step & 1];
+        if (step < steps - 1) {
+            f.c2 = 1.0f / kScaleB;
+            BLINK_TRY((run_product<T, XP, kApply, kNone, float>(f, o, tall, batch, stream)));
+        } else {
+            f.c2 = 1.0f / (kScaleB * kScaleX);
+            BLINK_TRY((run_product<T, XP, kApplyLast, LAST, Out>(f, o, tall, batch, stream)));
+        }
+    }
+    return BLINK_OK;
+}
+
+template <typename In, bool XP, Last LAST, typename Out>
+blink_status_t run_all(const Sizes& z, size_t batch, const Outer& o, const float* co, int steps, float eps, void* workspace, hipStream_t stream) {
+    const Space s = space_of(z, batch, workspace);
+    const bool tall = o.rows > o.cols;
+    BLINK_TRY(launch(ortho_norm<In>, dim3(z.norm_parts, static_cast<uint32_t>(batch)), dim3(kNormThreads), stream, o, s.parts));
+    BLINK_TRY(launch(ortho_first<In, XP>, dim3(z.np / 64, z.mp / 64, static_cast<uint32_t>(batch)), dim3(kFirstThreads), stream, o, tall, s.parts, z.norm_parts, eps,
+                     z.mp, z.np, s.x, s.xt[0]));
+    if (z.tile == 256) return iterate<256, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+    if (z.tile == 128) return iterate<128, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+    return iterate<64, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+}
+
+}  // namespace
+
+// Whether the iteration keeps singular values below 2 and the polynomial's below 8 for all that start in [0, 1].
+bool coefficients_fit(const float* co, int steps) {
+    double most = 1.0;
+    for (int i = 0; i < steps; ++i, co += 3) {
+        if (!std::isfinite(co[0]) || !std::isfinite(co[1]) || !std::isfinite(co[2])) return false;
+        double next = 0.0;
+        for (int u = 0; u <= 1024; ++u) {
+            const double x = most * u / 1024, p = co[0] + x * x * (co[1] + x * x * co[2]);
+            if (std::fabs(p) > 7.75) return false;
+            next = std::max(next, std::fabs(x * p));
+        }
+        most = next * 1.001;
+        if (most > 1.95) return false;
+    }
+    return true;
+}
+
+size_t orthogonalize_workspace(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
+    return space_of(sizes_of(batch, rows, cols, dtype), batch, nullptr).bytes;
+}
+
+blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, size_t rows, size_t cols, size_t in_row, size_t in_batch, const float* co,
+                             int steps, float eps, void* out, size_t out_row, size_t out_batch, void* workspace, hipStream_t stream) {
+    Outer o{};
+    o.in = in;
+    o.in_row = in_row;
+    o.in_batch = in_batch;
+    o.rows = static_cast<uint32_t>(rows);
+    o.cols = static_cast<uint32_t>(cols);
+    o.out = out;
+    o.out_row = out_row;
+    o.out_batch = out_batch;
+    const Sizes z = sizes_of(batch, rows, cols, dtype);
+    if (dtype == BLINK_FP32) return run_all<float, true, kMatrix, float>(z, batch, o, co, steps, eps, workspace, stream);
+    if (dtype == BLINK_BF16) return run_all<__bf16, false, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream);
+    return run_all<Half, false, kMatrix, Half>(z, batch, o, co, steps, eps, workspace, stream);
+}
+
+blink_status_t orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out, const void* grad,
+                               blink_dtype_t grad_type, size_t batch, size_t rows, size_t cols, float beta, bool nesterov, const float* co, int steps,
+                               float eps, float rate, float decay, void* workspace, hipStream_t stream) {
+    Outer o{};
+    o.in = grad;
+    o.in_row = cols;
+    o.in_batch = rows * cols;
+    o.momentum = momentum;
+    o.momentum_out = momentum_out;
+    o.beta = beta;
+    o.nesterov = nesterov;
+    o.rows = static_cast<uint32_t>(rows);
+    o.cols = static_cast<uint32_t>(cols);
+    o.weights = weights;
+    o.weights_out = weights_out;
+    o.rate = rate;
+    o.keep = 1.0f - decay;
+    const Sizes z = sizes_of(batch, rows, cols, BLINK_FP32);
+    return with_float(grad_type, [&](auto type) {
+        return run_all<decltype(type), true, kWeights, float>(z, batch, o, co, steps, eps, workspace, stream);
+    });
+}
+
+}  // namespace blink

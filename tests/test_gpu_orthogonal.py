@@ -1,0 +1,187 @@
+"""Orthogonalised updates against the iteration in 64 bits."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_1910_04940_amd as bl  # noqa: E402
+
+CODES = {torch.float32: bl.BLINK_FP32, torch.bfloat16: bl.BLINK_BF16, torch.float16: bl.BLINK_FP16}
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _want(m, steps=bl.BLINK_STEPS, eps=1e-7):
+    x = m.double().reshape(-1, *m.shape[-2:])
+    tall = x.shape[1] > x.shape[2]
+    x = x.mT.contiguous() if tall else x
+    norm = torch.linalg.matrix_norm(x, keepdim=True) + eps
+    x = torch.where(norm > 0, x / norm, 0.0)
+    for a, b, c in steps:
+        gram = x @ x.mT.contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return (x.mT if tall else x).reshape(m.shape)
+
+
+def _allowed(want, dtype, shape):
+    """Of the norm of the difference.  What is stored of X is off by `unit` of its size each step and grows by at most 3.45 in a step, so by 5 * 3.45^5
+    units of a norm of 1 in all; sums of K numbers are off by a few sqrt(K) units more.  For 16-bit matrices A and B are off by 2^-12 of their size,
+    which counts about 12 times (|b| + 2 |c| s^2 + a) in each of five steps against the result's norm.  Then the result's rounding."""
+    k = max(shape[-2:])
+    norm = float(torch.linalg.matrix_norm(want.reshape(-1, *want.shape[-2:])).max())
+    unit = 2.0 ** -22 + 4 * math.sqrt(k) * 2.0 ** -24
+    off = 5 * 3.45 ** 5 * unit
+    if dtype != torch.float32:
+        off += 5 * 12 * 2.0 ** -12 * norm
+    return off + UNIT[dtype] * norm
+
+
+def _run(m, out=None, steps=bl.BLINK_STEPS, eps=1e-7):
+    batch = m.shape[0] if m.dim() == 3 else 1
+    size = bl.blink_orthogonalize_workspace(batch, m.shape[-2], m.shape[-1], CODES[m.dtype])
+    work = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(m, 7.0) if out is None else out
+    bl.blink_orthogonalize(m, out, work, steps, eps, _stream())
+    return out
+
+
+def _check(got, m, **kw):
+    want = _want(m, **kw)
+    off = torch.linalg.matrix_norm((got.double() - want).reshape(-1, *m.shape[-2:])).max()
+    assert float(off) <= _allowed(want, m.dtype, m.shape), (float(off), _allowed(want, m.dtype, m.shape))
+
+
+def _matrix(shape, dtype, seed, scale=1e-3):
+    return (scale * torch.randn(*shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda")).to(dtype)
+
+
+SHAPES = [(1, 1), (1, 7), (5, 1), (2, 2), (16, 16), (31, 33), (64, 64), (65, 130), (130, 65), (3, 700), (700, 3), (128, 512), (200, 300), (1003, 389), (257, 1100),
+          (4, 40, 24), (3, 64, 64), (2, 129, 257), (17, 20, 90), (1, 512, 512), (20, 250, 500), (12, 520, 520)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes(shape, dtype):
+    m = _matrix(shape, dtype, sum(shape))
+    got = _run(m)
+    _check(got, m)
+    assert torch.equal(got.view(torch.uint8), _run(m).view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_large_tiles(dtype):
+    """Enough tiles of 256 to be served by them, sizes that end inside one, both ways round."""
+    for shape in ((20, 600, 900), (20, 900, 600)):
+        m = _matrix(shape, dtype, 3)
+        _check(_run(m), m)
+
+
+@pytest.mark.parametrize("scale", [1e-37, 1e-18, 1.0, 1e18, 1e36])
+def test_sizes_of_elements(scale):
+    """Squares of the elements pass the range of 32-bit floats at both ends; eps is 0."""
+    m = _matrix((60, 80), torch.float32, 5, scale)
+    _check(_run(m, eps=0.0), m, eps=0.0)
+
+
+def test_singular_values_move_to_one():
+    m = _matrix((96, 160), torch.float32, 7)
+    s = torch.linalg.svdvals(_run(m).double())
+    assert 0.6 < float(s.min()) and float(s.max()) < 1.25
+
+
+def test_zeros_and_one_nonzero():
+    z = torch.zeros(40, 50, device="cuda")
+    assert (_run(z, eps=0.0) == 0).all() and (_run(z) == 0).all()
+    z[3, 4] = -2.0
+    got = _run(z)
+    _check(got, z)
+    assert int((got != 0).sum()) == 1
+
+
+def test_low_rank():
+    u, v = _matrix((300, 4), torch.float32, 8, 1.0), _matrix((4, 500), torch.float32, 9, 1.0)
+    m = u @ v
+    _check(_run(m), m)
+
+
+def test_nan_shows():
+    m = _matrix((3, 40, 50), torch.float32, 8)
+    m[1, 2, 3] = math.nan
+    got = _run(m)
+    assert torch.isnan(got[1]).all() and torch.isfinite(got[0]).all() and torch.isfinite(got[2]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tall", [False, True])
+def test_views_and_in_place(dtype, tall):
+    shape = (2, 150, 90) if tall else (2, 90, 150)
+    whole = _matrix((2, shape[1] + 3, shape[2] + 5), dtype, 10)
+    view = whole[:, 1:1 + shape[1], 2:2 + shape[2]]
+    want = _run(view.contiguous())
+    out = torch.full_like(whole, 3.0)
+    _run(view, out[:, 1:1 + shape[1], 2:2 + shape[2]])
+    assert torch.equal(out[:, 1:1 + shape[1], 2:2 + shape[2]], want)
+    out[:, 1:1 + shape[1], 2:2 + shape[2]] = 3.0
+    assert (out == 3.0).all()
+    same = view.contiguous()
+    _run(same, same)
+    assert torch.equal(same, want)
+    again = whole[:1].expand(3, -1, -1)     # one matrix read three times
+    got = _run(again, torch.empty(again.shape, dtype=dtype, device="cuda"))
+    assert torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("steps", [((1.5, -0.5, 0.0),), ((1.875, -1.25, 0.375),) * 3, ((3.4445, -4.7750, 2.0315),) * 2 + ((1.5, -0.5, 0.0),) * 4])
+def test_other_coefficients(steps):
+    m = _matrix((100, 140), torch.float32, 12)
+    _check(_run(m, steps=steps), m, steps=steps)
+
+
+@pytest.mark.parametrize("grad_type", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape,nesterov", [((70, 30), True), ((30, 70), False), ((3, 129, 65), True), ((1, 1), True), ((2, 300, 256), False)])
+def test_step(shape, nesterov, grad_type):
+    w, m, g = _matrix(shape, torch.float32, 1, 0.02), _matrix(shape, torch.float32, 2), _matrix(shape, grad_type, 3)
+    batch = shape[0] if len(shape) == 3 else 1
+    work = torch.full((bl.blink_orthogonalize_workspace(batch, *shape[-2:], bl.BLINK_FP32),), 255, dtype=torch.uint8, device="cuda")
+    w1, m1 = torch.empty_like(w), torch.empty_like(m)
+    kw = dict(rate=0.02, beta=0.9, nesterov=nesterov, decay=0.01, stream=_stream())
+    bl.blink_orthogonal_step(w, m, g, w1, m1, work, **kw)
+    m_want = 0.9 * m.double() + g.double()
+    u = g.double() + 0.9 * m_want if nesterov else m_want
+    assert ((m1.double() - m_want).abs() <= 2.0 ** -23 * (m.double().abs() + m_want.abs())).all()
+    o = _want(u)
+    want = 0.99 * w.double() - 0.02 * o
+    off = float(torch.linalg.matrix_norm((w1.double() - want).reshape(-1, *shape[-2:])).max())
+    assert off <= 0.02 * _allowed(o, torch.float32, shape) + 2.0 ** -23 * float((w.norm() + want.norm()))
+    w2, m2 = w.clone(), m.clone()
+    bl.blink_orthogonal_step(w2, m2, g, w2, m2, work, **kw)     # in place
+    assert torch.equal(w1, w2) and torch.equal(m1, m2)
+
+
+def test_in_a_graph_and_on_another_stream():
+    m = _matrix((2, 100, 200), torch.float32, 15)
+    want = _run(m)
+    out = torch.empty_like(m)
+    work = torch.empty(bl.blink_orthogonalize_workspace(2, 100, 200, bl.BLINK_FP32), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bl.blink_orthogonalize(m, out, work, stream=_stream())
+    for _ in range(3):
+        out.fill_(5.0)
+        work.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    side = torch.cuda.Stream()
+    out.fill_(5.0)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        bl.blink_orthogonalize(m, out, work, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(out, want)
