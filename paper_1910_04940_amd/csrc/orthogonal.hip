@@ -198,20 +198,23 @@ __device__ inline uint32_t slot_of(uint32_t row, uint32_t part) {   // byte offs
     }
 }
 
-// Copies rows [row0, row0 + ROWS) of a stage: every thread 16 bytes at a time, in the order of LDS, each from where its part is.
+// Copies a stage of ROWS rows: every thread 16 bytes at a time, in the order of LDS, each from where its part is.  A thread's places
+// in the rounds are a whole number of eights of lines apart, so one offset serves them all.
+template <int LINE>
+__device__ inline uint32_t first_offset(uint32_t pitch) {
+    const uint32_t t = threadIdx.x, line = t >> 3, slot = (t & 7) ^ (line & 7);
+    const uint32_t row = LINE == 128 ? line : line * 2 + (slot >> 2), part = LINE == 128 ? slot : slot & 3;
+    return row * pitch + part * 16;
+}
 template <int ROWS, int LINE, int THREADS>
-__device__ inline void copy_stage(const Half* from, uint64_t pitch, uint32_t k_bytes, char* to) {
-    constexpr int kTimes = ROWS * LINE / 16 / THREADS;
-    static_assert(kTimes * THREADS * 16 == ROWS * LINE, "whole rounds");
-    const int t = threadIdx.x;
+__device__ inline void copy_stage(__amdgpu_buffer_rsrc_t from, uint32_t offset, uint32_t pitch, uint32_t k_bytes, char* to) {
+    constexpr int kTimes = ROWS * LINE / 16 / THREADS, kRows = ROWS / kTimes;   // rounds, rows of one
+    static_assert(kTimes * THREADS * 16 == ROWS * LINE && THREADS % 64 == 0, "whole rounds");
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int u = 0; u < kTimes; ++u) {
-        const uint32_t at = u * THREADS + t, line = at >> 3, slot = (at & 7) ^ (line & 7);
-        const uint32_t row = LINE == 128 ? line : line * 2 + (slot >> 2), part = LINE == 128 ? slot : slot & 3;
-        const char* const g = reinterpret_cast<const char*>(from) + row * pitch + k_bytes + part * 16;
-        char* const l = to + (u * THREADS + (t & ~63)) * 16;   // of the wave; lanes follow one another
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g, (__attribute__((address_space(3))) void*)l, 16, 0, 0);
-    }
+    for (int u = 0; u < kTimes; ++u)   // (a wave's lanes follow one another in LDS)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (u * THREADS + wave * 64) * 16), 16, offset,
+                                                 k_bytes + u * kRows * pitch, 0, 0);
 }
 
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
@@ -236,14 +239,17 @@ __device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES
             qh[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part));
             if (QP) ql[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part + 4));
         }
+        // the same sums again only after all the others
 #pragma unroll
-        for (int i = 0; i < S::kBM; ++i)
+        for (int term = 0; term < 3; ++term)
 #pragma unroll
-            for (int j = 0; j < S::kBN; ++j) {
-                if (QP) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
-                if (PP) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
-            }
+            for (int i = 0; i < S::kBM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kBN; ++j) {
+                    if (QP && term == 0) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
+                    if (PP && term == 1) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
+                    if (term == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
+                }
     }
 }
 
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
     static_assert(!kSymmetric || TM == TN, "square tiles");
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / WAVES_N, wn = wave % WAVES_N;
     // workgroups go round the eight dies in turn: each die gets a run of neighbouring tiles
-    const uint32_t all = gridDim.x, per = all >> 3, bid = blockIdx.x;
+    const uint32_t per = gridDim.x >> 3, bid = blockIdx.x;
     const uint32_t place = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
     const uint64_t batch = place / f.tiles;
     const uint32_t tile = place - static_cast<uint32_t>(batch) * f.tiles;
@@ -271,13 +277,16 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
         ti = tile / f.tiles_n;
         tj = tile - ti * f.tiles_n;
     }
-    const uint64_t pitch_p = static_cast<uint64_t>(f.k) * (PP ? 4 : 2), pitch_q = static_cast<uint64_t>(f.k) * (QP ? 4 : 2);   // bytes
-    const Half* const p = f.p + (batch * f.mp + ti * TM) * (pitch_p / 2);
-    const Half* const q = f.q + (batch * f.np + tj * TN) * (pitch_q / 2);
+    const uint32_t pitch_p = f.k * (PP ? 4 : 2), pitch_q = f.k * (QP ? 4 : 2);   // bytes
+    const auto rows_of = [](const Half* from, uint64_t row, uint32_t pitch, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(from)) + row * pitch, 0, rows * pitch, 0x00020000);
+    };
+    const auto p = rows_of(f.p, batch * f.mp + ti * TM, pitch_p, TM), q = rows_of(f.q, batch * f.np + tj * TN, pitch_q, TN);
+    const uint32_t from_p = first_offset<S::kLineP>(pitch_p), from_q = first_offset<S::kLineQ>(pitch_q);
     Float16v acc[S::kBM][S::kBN] = {};
     const auto copy = [&](uint32_t stage, char* to) {
-        copy_stage<TM, S::kLineP, S::kThreads>(p, pitch_p, stage * S::kLineP, to);
-        copy_stage<TN, S::kLineQ, S::kThreads>(q, pitch_q, stage * S::kLineQ, to + S::kBytesP);
+        copy_stage<TM, S::kLineP, S::kThreads>(p, from_p, pitch_p, stage * S::kLineP, to);
+        copy_stage<TN, S::kLineQ, S::kThreads>(q, from_q, pitch_q, stage * S::kLineQ, to + S::kBytesP);
     };
     const auto arrived = [] {   // this wave's copies; then everybody's
         __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -285,14 +294,18 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
     };
     const uint32_t stages = f.k / S::kStage;
     copy(0, even);
-    for (uint32_t s = 0; s < stages; s += 2) {
+    uint32_t s = 0;
+    for (; s + 1 < stages; s += 2) {
         arrived();
-        if (s + 1 < stages) copy(s + 1, odd);
+        copy(s + 1, odd);
         multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(even, acc, wm, wn);
-        if (s + 1 == stages) break;
         arrived();
         if (s + 2 < stages) copy(s + 2, even);
         multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(odd, acc, wm, wn);
+    }
+    if (s < stages) {
+        arrived();
+        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(even, acc, wm, wn);
     }
     __syncthreads();
     // 32 x 32 at a time through LDS, so that rows are written whole in both directions
