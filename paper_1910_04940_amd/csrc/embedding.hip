@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, u
             if constexpr (sizeof(Out) < 4) asm("" : "+v"(z));   // a 32-bit product: the mixed 16-bit one rounds it otherwise
             y.v[i] = static_cast<uint64_t>(token[u]) < vocab ? static_cast<Out>(z) : static_cast<Out>(0.0f);
         }
-        if (first + u * kRowThreads < units) *reinterpret_cast<Pack<Out, V>*>(out + row[u] * out_stride + at[u]) = y;
+        if (first + u * kRowThreads < units) store_past(reinterpret_cast<Pack<Out, V>*>(out + row[u] * out_stride + at[u]), y);
     }
 }
 
@@ -81,18 +81,24 @@ __device__ inline uint32_t rank_in_wave(uint32_t digit, bool in, int bits, volat
     return before + below;
 }
 
-// From counts[wave][digit]: the wave's items with that digit come at counts[wave][digit] (afterwards) past the digit's
-// begin, which is returned for digit = thread (sum of all smaller digits' items).
+// From counts[wave][digit]: begin[digit] becomes the sum of all smaller digits' items, counts[wave][digit] those of the digit in the waves before.
 template <int THREADS>
-__device__ inline uint32_t scan_counts(uint32_t (*counts)[kDigits], int digits, uint32_t* wave_sum) {
+__device__ inline void scan_counts(uint32_t (*counts)[kDigits], int digits, uint32_t* begin, uint32_t* wave_sum) {
+    constexpr int kEach = kDigits > THREADS ? kDigits / THREADS : 1;   // neighbouring digits of a thread
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    uint32_t total = 0;
-    if (t < digits)
-        for (int w = 0; w < THREADS / 64; ++w) {
-            const uint32_t c = counts[w][t];
-            counts[w][t] = total;
-            total += c;
-        }
+    uint32_t own[kEach], total = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int digit = t * kEach + e;
+        own[e] = 0;
+        if (digit < digits)
+            for (int w = 0; w < THREADS / 64; ++w) {
+                const uint32_t c = counts[w][digit];
+                counts[w][digit] = own[e];
+                own[e] += c;
+            }
+        total += own[e];
+    }
     uint32_t sum = total;
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t other = __shfl_up(sum, d);
@@ -100,10 +106,14 @@ __device__ inline uint32_t scan_counts(uint32_t (*counts)[kDigits], int digits, 
     }
     if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < wave; ++w) before += wave_sum[w];
+    sum -= total;
+    for (int w = 0; w < wave; ++w) sum += wave_sum[w];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        if (t * kEach + e < digits) begin[t * kEach + e] = sum;
+        sum += own[e];
+    }
     __syncthreads();
-    return before + sum - total;
 }
 
 template <typename Token>
@@ -111,39 +121,45 @@ __device__ inline uint32_t key_of(Token token, uint32_t vocab) {
     return static_cast<uint64_t>(static_cast<int64_t>(token)) < vocab ? static_cast<uint32_t>(token) : vocab;
 }
 
-// Up to kOneThreads * kOneItems tokens: one workgroup, the list in LDS from pass to pass.
-constexpr int kOneThreads = 1024, kOneItems = 8, kOneMost = kOneThreads * kOneItems;
-template <typename Token>
-__global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* tokens, uint32_t n, uint32_t vocab, int bits, int passes,
-                                                                  uint32_t* key_out, uint32_t* pos_out) {
-    __shared__ uint32_t counts[kOneThreads / 64][kDigits];
-    __shared__ uint32_t begin[kDigits], wave_sum[kOneThreads / 64];
-    __shared__ uint32_t keys[kOneMost], places[kOneMost];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+// Few tokens: one workgroup, the list in LDS from pass to pass; four waves do for up to 2048 (509 tokens, two passes: 1024 threads 8.5 us).
+constexpr int kOneItems = 8, kFewThreads = 256, kFewMost = kFewThreads * kOneItems, kOneThreads = 1024, kOneMost = kOneThreads * kOneItems;
+template <typename Token, int THREADS>
+__global__ __launch_bounds__(THREADS) void embedding_sort_one(const Token* tokens, uint32_t n, uint32_t vocab, int bits, int passes, uint32_t* key_out,
+                                                              uint32_t* pos_out) {
+    __shared__ uint32_t counts[THREADS / 64][kDigits];
+    __shared__ uint32_t begin[kDigits], wave_sum[THREADS / 64];
+    __shared__ uint32_t keys[THREADS * kOneItems], places[THREADS * kOneItems];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, digits = 1 << bits;
     // every wave has a run of whole 64s, as few as hold them all
-    const uint32_t rounds = (n + kOneThreads - 1) / kOneThreads;
+    const uint32_t rounds = (n + THREADS - 1) / THREADS;
     const uint32_t first = wave * rounds * 64 + lane;
     uint32_t key[kOneItems], pos[kOneItems], rank[kOneItems];
+#pragma unroll
+    for (int j = 0; j < kOneItems; ++j)
+        if (j < static_cast<int>(rounds)) {
+            const uint32_t i = first + j * 64;
+            key[j] = i < n ? key_of(tokens[i], vocab) : 0;
+            pos[j] = i;
+        }
     for (int pass = 0, shift = 0; pass < passes; ++pass, shift += bits) {
-        for (int i = t; i < kOneThreads / 64 * kDigits; i += kOneThreads) counts[i / kDigits][i % kDigits] = 0;
-        __syncthreads();
+        for (int d = lane; d < digits; d += 64) counts[wave][d] = 0;   // (a wave's counts are its own until the scan)
+        wave_sync();
 #pragma unroll
         for (int j = 0; j < kOneItems; ++j)
             if (j < static_cast<int>(rounds)) {
                 const uint32_t i = first + j * 64;
-                const bool in = i < n;
-                key[j] = !in ? 0 : pass == 0 ? key_of(tokens[i], vocab) : keys[i];
-                pos[j] = !in ? 0 : pass == 0 ? i : places[i];
-                rank[j] = rank_in_wave(key[j] >> shift & ((1u << bits) - 1), in, bits, counts[wave]);
+                if (pass > 0 && i < n) {
+                    key[j] = keys[i];
+                    pos[j] = places[i];
+                }
+                rank[j] = rank_in_wave(key[j] >> shift & (digits - 1), i < n, bits, counts[wave]);
             }
         __syncthreads();
-        const uint32_t b = scan_counts<kOneThreads>(counts, 1 << bits, wave_sum);
-        if (t < 1 << bits) begin[t] = b;
-        __syncthreads();
+        scan_counts<THREADS>(counts, digits, begin, wave_sum);
 #pragma unroll
         for (int j = 0; j < kOneItems; ++j)
             if (j < static_cast<int>(rounds) && first + j * 64 < n) {
-                const uint32_t digit = key[j] >> shift & ((1u << bits) - 1);
+                const uint32_t digit = key[j] >> shift & (digits - 1);
                 const uint32_t to = begin[digit] + counts[wave][digit] + rank[j];
                 (pass == passes - 1 ? key_out : keys)[to] = key[j];
                 (pass == passes - 1 ? pos_out : places)[to] = pos[j];
@@ -152,65 +168,56 @@ __global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* t
     }
 }
 
-// More tokens: tiles of kTile.  Each pass counts the digits of every tile, sums the counts along the tiles, and moves.
-constexpr int kTileThreads = 512, kTileItems = 4, kTile = kTileThreads * kTileItems;
+// More tokens: at most kMostChunks chunks of whole tiles, a workgroup to each.  A pass counts the digits of every chunk, then
+// every workgroup adds up what it needs of the counts (two launches a pass; a third that scans them cost 4.5 us), and moves its items.
+constexpr int kTileThreads = 512, kTileItems = 2, kTile = kTileThreads * kTileItems, kMostChunks = 256;
 static_assert(kDigits <= kTileThreads, "a thread per digit");
 
 template <typename Token>
-__global__ __launch_bounds__(kTileThreads) void embedding_sort_count(const Token* tokens, const uint32_t* keys, uint32_t n, uint32_t vocab, int shift,
-                                                                     int bits, uint32_t tiles, uint32_t* counts) {
+__global__ __launch_bounds__(kTileThreads) void embedding_sort_count(const Token* tokens, const uint32_t* keys, uint32_t n, uint32_t vocab, uint32_t chunk,
+                                                                     int shift, int bits, uint32_t* counts) {
     __shared__ uint32_t count[kDigits];
-    const int t = threadIdx.x;
+    const uint32_t t = threadIdx.x;
     count[t] = 0;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kTileItems; ++j) {
-        const uint32_t i = blockIdx.x * kTile + j * kTileThreads + t;
-        if (i < n) atomicAdd(&count[(tokens ? key_of(tokens[i], vocab) : keys[i]) >> shift & ((1u << bits) - 1)], 1u);
-    }
+    const uint64_t from = static_cast<uint64_t>(blockIdx.x) * chunk, to = from + chunk < n ? from + chunk : n;
+#pragma unroll 2
+    for (uint64_t i = from + t; i < to; i += kTileThreads)
+        atomicAdd(&count[(tokens ? key_of(tokens[i], vocab) : keys[i]) >> shift & ((1u << bits) - 1)], 1u);
     __syncthreads();
-    if (t < 1 << bits) counts[static_cast<uint64_t>(t) * tiles + blockIdx.x] = count[t];
-}
-
-// One workgroup per digit: counts along the tiles become the items before each tile's, and their sum.
-constexpr int kScanThreads = 256;
-__global__ __launch_bounds__(kScanThreads) void embedding_sort_scan(uint32_t* counts, uint32_t tiles, uint32_t* totals) {
-    __shared__ uint32_t wave_sum[kScanThreads / 64];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    uint32_t* const row = counts + static_cast<uint64_t>(blockIdx.x) * tiles;
-    uint32_t before = 0;
-    for (uint32_t lo = 0; lo < tiles; lo += kScanThreads) {
-        const uint32_t c = lo + t < tiles ? row[lo + t] : 0;
-        uint32_t sum = c;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
-        if (lane == 63) wave_sum[wave] = sum;
-        __syncthreads();
-        uint32_t all = 0, mine = 0;
-        for (int w = 0; w < kScanThreads / 64; ++w) {
-            if (w == wave) mine = all;
-            all += wave_sum[w];
-        }
-        if (lo + t < tiles) row[lo + t] = before + mine + sum - c;
-        before += all;
-        __syncthreads();
-    }
-    if (t == 0) totals[blockIdx.x] = before;
+    if (t < 1u << bits) counts[(blockIdx.x << bits) + t] = count[t];
 }
 
 template <typename Token>
 __global__ __launch_bounds__(kTileThreads) void embedding_sort_move(const Token* tokens, const uint32_t* keys, const uint32_t* places, uint32_t n,
-                                                                    uint32_t vocab, int shift, int bits, uint32_t tiles, const uint32_t* before,
-                                                                    const uint32_t* totals, uint32_t* key_out, uint32_t* pos_out) {
+                                                                    uint32_t vocab, uint32_t chunk, int shift, int bits, const uint32_t* all_counts,
+                                                                    uint32_t* key_out, uint32_t* pos_out) {
     __shared__ uint32_t counts[kTileThreads / 64][kDigits];
     __shared__ uint32_t begin[kDigits], wave_sum[kTileThreads / 64];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, digits = 1 << bits;
-    for (int w = 0; w < kTileThreads / 64; ++w) counts[w][t] = 0;
-    // where each digit begins: the sum of the smaller digits' totals, and this tile's place among the digit's items
-    uint32_t sum = t < digits ? totals[t] : 0;
-    const uint32_t own = sum, ahead = t < digits ? before[static_cast<uint64_t>(t) * tiles + blockIdx.x] : 0;
+    const uint64_t from = static_cast<uint64_t>(blockIdx.x) * chunk, end = from + chunk < n ? from + chunk : n;
+    uint64_t first = from + wave * (64 * kTileItems) + lane;
+    uint32_t key[kTileItems], pos[kTileItems], rank[kTileItems];
+    const auto load = [&] {
+#pragma unroll
+        for (int j = 0; j < kTileItems; ++j) {
+            const uint64_t i = first + j * 64;
+            const bool in = i < end;
+            key[j] = !in ? 0 : tokens ? key_of(tokens[i], vocab) : keys[i];
+            pos[j] = !in ? 0 : tokens ? static_cast<uint32_t>(i) : places[i];
+        }
+    };
+    load();
+    // where each digit begins: after the smaller digits of all chunks and its own of the chunks before
+    uint32_t own = 0, ahead = 0;
+    if (t < digits)
+#pragma unroll 16
+        for (uint32_t c = 0; c < gridDim.x; ++c) {
+            const uint32_t many = all_counts[(c << bits) + t];
+            own += many;
+            ahead += c < blockIdx.x ? many : 0;
+        }
+    uint32_t sum = own;
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t other = __shfl_up(sum, d);
         if (lane >= d) sum += other;
@@ -219,55 +226,56 @@ __global__ __launch_bounds__(kTileThreads) void embedding_sort_move(const Token*
     __syncthreads();
     for (int w = 0; w < wave; ++w) sum += wave_sum[w];
     begin[t] = sum - own + ahead;
-    const uint32_t first = blockIdx.x * kTile + wave * (64 * kTileItems) + lane;
-    uint32_t key[kTileItems], pos[kTileItems], rank[kTileItems];
+    for (uint64_t tile = from; tile < end; tile += kTile, first += kTile) {
+        if (tile != from) load();
+        for (int d = lane; d < digits; d += 64) counts[wave][d] = 0;
+        wave_sync();
 #pragma unroll
-    for (int j = 0; j < kTileItems; ++j) {
-        const uint32_t i = first + j * 64;
-        const bool in = i < n;
-        key[j] = !in ? 0 : tokens ? key_of(tokens[i], vocab) : keys[i];
-        pos[j] = !in ? 0 : tokens ? i : places[i];
-    }
-#pragma unroll
-    for (int j = 0; j < kTileItems; ++j) rank[j] = rank_in_wave(key[j] >> shift & (digits - 1), first + j * 64 < n, bits, counts[wave]);
-    __syncthreads();
-    if (t < digits) {
+        for (int j = 0; j < kTileItems; ++j) rank[j] = rank_in_wave(key[j] >> shift & (digits - 1), first + j * 64 < end, bits, counts[wave]);
+        __syncthreads();
         uint32_t total = 0;
-        for (int w = 0; w < kTileThreads / 64; ++w) {
-            const uint32_t c = counts[w][t];
-            counts[w][t] = total;
-            total += c;
-        }
-    }
-    __syncthreads();
+        if (t < digits)
+            for (int w = 0; w < kTileThreads / 64; ++w) {
+                const uint32_t c = counts[w][t];
+                counts[w][t] = total;
+                total += c;
+            }
+        __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kTileItems; ++j)
-        if (first + j * 64 < n) {
-            const uint32_t digit = key[j] >> shift & (digits - 1), to = begin[digit] + counts[wave][digit] + rank[j];
-            key_out[to] = key[j];
-            pos_out[to] = pos[j];
-        }
+        for (int j = 0; j < kTileItems; ++j)
+            if (first + j * 64 < end) {
+                const uint32_t digit = key[j] >> shift & (digits - 1), to = begin[digit] + counts[wave][digit] + rank[j];
+                key_out[to] = key[j];
+                pos_out[to] = pos[j];
+            }
+        __syncthreads();
+        if (t < digits) begin[t] += total;
+    }
 }
 
 // ---- the sums ---------------------------------------------------------------------------------------------------------------
-// How many of the sorted positions come before place `d`: those j with j + key[j] < d (ALL), or d itself where rows that no
-// token names are left alone and only positions have places.  A wave's 64 lanes probe 64 positions at a time.
-template <bool ALL>
-__device__ inline uint32_t positions_before(const uint32_t* keys, uint32_t n, uint64_t d) {
-    if (!ALL) return static_cast<uint32_t>(d < n ? d : n);
+// How many of the sorted positions, from the first on, are `before`.  A wave's 64 lanes probe 64 of them at a time.
+template <typename F>
+__device__ inline uint32_t search(uint32_t n, F before) {
     const uint32_t lane = threadIdx.x & 63;
     uint32_t lo = 0, hi = n;   // the answer is in [lo, hi]
     while (lo < hi) {
         const uint32_t step = (hi - lo + 63) / 64;
         const uint64_t j = lo + static_cast<uint64_t>(step) * lane;
-        const bool before = j < hi && j + keys[j] < d;
-        const int many = __popcll(__ballot(before));
+        const int many = __popcll(__ballot(j < hi && before(j)));
         if (many == 0) return lo;
         const uint64_t top = static_cast<uint64_t>(lo) + static_cast<uint64_t>(step) * many;
         lo += step * (many - 1) + 1;
         hi = static_cast<uint32_t>(top < hi ? top : hi);
     }
     return lo;
+}
+// Those that come before place `d`: all j with j + key[j] < d (ALL), or d itself where rows that no token names are left alone and
+// only positions have places.
+template <bool ALL>
+__device__ inline uint32_t positions_before(const uint32_t* keys, uint32_t n, uint64_t d) {
+    if (!ALL) return static_cast<uint32_t>(d < n ? d : n);
+    return search(n, [=](uint64_t j) { return j + keys[j] < d; });
 }
 
 struct Sums {
@@ -279,10 +287,12 @@ struct Sums {
     void* table;
     uint64_t table_stride;
     uint32_t stretch;         // places of a wave
-    uint32_t stretches;
+    uint32_t stretches, columns;   // waves beside one another on a row
     float *head, *tail;       // [stretch][dim]: what a stretch has of a row that began before it, of one that does not end in it
+    uint32_t* joined;         // [stretch]: the row that began before the stretch and ends in it, or kNoRow
     uint32_t dim_up;          // elements of a row of head and tail
 };
+constexpr uint32_t kNoRow = ~0u;
 
 template <typename T, int V>
 __device__ inline void load_up(float (&x)[V], const T* p) {
@@ -290,27 +300,27 @@ __device__ inline void load_up(float (&x)[V], const T* p) {
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = static_cast<float>(y.v[i]);
 }
-// The row's final sum: scaled, added to what is there where ADD, rounded once.
+// The row's final sum: scaled, added to `y`, what is there, where ADD, rounded once.
 template <typename T, int V, bool ADD>
-__device__ inline void store_row(T* p, const float (&sum)[V], float scale) {
-    Pack<T, V> y;
-    if (ADD) y = *reinterpret_cast<const Pack<T, V>*>(p);
+__device__ inline void store_row(T* p, Pack<T, V> y, const float (&sum)[V], float scale) {
 #pragma unroll
     for (int i = 0; i < V; ++i) y.v[i] = static_cast<T>(ADD ? __builtin_fmaf(scale, sum[i], static_cast<float>(y.v[i])) : scale * sum[i]);
-    *reinterpret_cast<Pack<T, V>*>(p) = y;
+    if (ADD) *reinterpret_cast<Pack<T, V>*>(p) = y;
+    else store_past(reinterpret_cast<Pack<T, V>*>(p), y);
 }
 
 constexpr int kSumThreads = 256;
 constexpr int kSumAhead = 8;   // rows of a sum whose loads are under way together
 
-// A wave: V elements per lane of the columns [64 V y, ...) of the rows of its stretch.  ALL: rows that no token names are
-// written as zeros, else (ADD too) left alone.
+// A wave: 64 V columns of the rows of its stretch, V to a lane; the next wave has the columns after them, so that a workgroup
+// writes rows in one piece.  ALL: rows that no token names are written as zeros, else (ADD too) left alone.
 template <typename Grad, typename T, int V, bool ADD>
 __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     constexpr bool ALL = !ADD;
-    const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    const uint32_t place_of = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    const uint32_t w = place_of / s.columns, column = place_of - w * s.columns;
     if (w >= s.stretches) return;
-    const uint32_t lane = threadIdx.x & 63, col = (blockIdx.y * 64 + lane) * V;
+    const uint32_t lane = threadIdx.x & 63, col = (column * 64 + lane) * V;
     const bool in = col < s.dim;
     const Grad* const grad = static_cast<const Grad*>(s.grad) + (in ? col : 0);
     T* const table = static_cast<T*>(s.table) + (in ? col : 0);
@@ -323,10 +333,13 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     bool begun = p > 0 && r < s.vocab && __builtin_amdgcn_readfirstlane(s.keys[p - 1]) == r;   // the row has positions in an earlier stretch
     bool any = false;                                                                          // and in this one
     float sum[V] = {};
+    Pack<T, V> there;   // what the row holds (ADD)
+    uint32_t joins = kNoRow;
     const auto finish = [&] {   // row r ends
+        if (begun) joins = r;
         if (in) {
             if (begun) *reinterpret_cast<Pack<float, V>*>(s.head + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
-            else if (ALL || any) store_row<T, V, ADD>(table + static_cast<uint64_t>(r) * s.table_stride, sum, s.scale);
+            else if (ALL || any) store_row<T, V, ADD>(table + static_cast<uint64_t>(r) * s.table_stride, there, sum, s.scale);
         }
         begun = any = false;
 #pragma unroll
@@ -345,17 +358,20 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
         const uint32_t real = __popcll(__ballot(key < s.vocab));   // padding comes last
         for (uint32_t j = 0; j < real; j += kSumAhead) {
             float x[kSumAhead][V];
+            Pack<T, V> held[kSumAhead];   // (a row's every time, so that none is waited for at its end)
 #pragma unroll
             for (int a = 0; a < kSumAhead; ++a)
                 if (j + a < real) {
-                    const uint32_t row = __builtin_amdgcn_readlane(place, j + a);
+                    const uint32_t row = __builtin_amdgcn_readlane(place, j + a), to = __builtin_amdgcn_readlane(key, j + a);
                     if (in) load_up<Grad, V>(x[a], grad + static_cast<uint64_t>(row) * s.grad_stride);
+                    if (ADD && in) held[a] = *reinterpret_cast<const Pack<T, V>*>(table + static_cast<uint64_t>(to) * s.table_stride);
                 }
 #pragma unroll
             for (int a = 0; a < kSumAhead; ++a)
                 if (j + a < real) {
                     finish_up_to(__builtin_amdgcn_readlane(key, j + a));
                     any = true;
+                    if (ADD && in) there = held[a];
                     if (in)
 #pragma unroll
                         for (int i = 0; i < V; ++i) sum[i] += x[a][i];
@@ -365,73 +381,68 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
         if (real < many) break;
     }
     if (ALL) finish_up_to(r_end);
-    if (!any) return;
-    if (!ALL && (p >= s.n || __builtin_amdgcn_readfirstlane(s.keys[p]) != r)) finish();
-    else if (in) *reinterpret_cast<Pack<float, V>*>(s.tail + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
+    if (any) {
+        if (!ALL && (p >= s.n || __builtin_amdgcn_readfirstlane(s.keys[p]) != r)) finish();
+        else if (in) *reinterpret_cast<Pack<float, V>*>(s.tail + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
+    }
+    if (column == 0 && lane == 0) s.joined[w] = joins;
 }
 
-// Rows that several stretches share: their sums, joined in the order of the stretches.  A workgroup looks at the stretch in
-// which such a row ends; its waves take equal parts of the stretches before.
-constexpr int kJoinThreads = 512;
+// Rows that several stretches share: their sums, joined in the order of the stretches.  A workgroup looks at four stretches; where
+// such a row ends in one, its waves take equal parts of the stretches before.
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64, kJoinStretches = 4;
 template <typename T, int V, bool ADD>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
     constexpr bool ALL = !ADD;
-    __shared__ Pack<float, V> part[kJoinThreads / 64][64];
-    const uint32_t w = blockIdx.x + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t places = static_cast<uint64_t>(s.n) + (ALL ? s.vocab : 0), d0 = static_cast<uint64_t>(w) * s.stretch;
-    const uint64_t d1 = d0 + s.stretch < places ? d0 + s.stretch : places;
-    const uint32_t p = positions_before<ALL>(s.keys, s.n, d0);
-    if (p == 0) return;
-    const uint32_t r = s.keys[p - 1];
-    if (r >= s.vocab) return;
-    if (ALL ? d0 - p != r : p >= s.n || s.keys[p] != r) return;   // no row reaches into this stretch
-    // the row ends here?
-    const uint32_t end = positions_before<ALL>(s.keys, s.n, d1);
-    if (ALL ? d1 - end <= r : end < s.n && s.keys[end] == r) return;
-    // the first position of the row: [lo, hi] holds it
-    uint32_t lo = 0, hi = p - 1;
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (s.keys[mid] < r) lo = mid + 1;
-        else hi = mid;
-    }
-    const uint32_t from = static_cast<uint32_t>((static_cast<uint64_t>(lo) + (ALL ? r : 0)) / s.stretch), many = w - from;
+    __shared__ Pack<float, V> part[kJoinWaves][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t col = (blockIdx.y * 64 + lane) * V;
     const bool in = col < s.dim;
-    const uint32_t each = (many + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
-    const uint32_t a = from + min(many, wave * each), b = from + min(many, (wave + 1) * each);
-    float sum[V] = {};
-    if (in) {
+    for (uint32_t w = blockIdx.x * kJoinStretches; w < (blockIdx.x + 1) * kJoinStretches && w < s.stretches; ++w) {
+        const uint32_t r = s.joined[w];
+        if (r == kNoRow) continue;
+        const uint32_t first = search(s.n, [&](uint64_t j) { return s.keys[j] < r; });
+        const uint32_t from = static_cast<uint32_t>((static_cast<uint64_t>(first) + (ALL ? r : 0)) / s.stretch), many = w - from;
+        const uint32_t each = (many + kJoinWaves - 1) / kJoinWaves;
+        const uint32_t a = from + min(many, wave * each), b = from + min(many, (wave + 1) * each);
+        float sum[V] = {};
+        if (in) {
 #pragma unroll 8
-        for (uint32_t i = a; i < b; ++i) {
-            float x[V];
-            load_up<float, V>(x, s.tail + static_cast<uint64_t>(i) * s.dim_up + col);
+            for (uint32_t i = a; i < b; ++i) {
+                float x[V];
+                load_up<float, V>(x, s.tail + static_cast<uint64_t>(i) * s.dim_up + col);
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += x[v];
+                for (int v = 0; v < V; ++v) sum[v] += x[v];
+            }
         }
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) part[wave][lane].v[v] = sum[v];
+        __syncthreads();
+        if (wave != 0 || !in) continue;
+        for (int o = 1; o < kJoinWaves; ++o)
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += part[o][lane].v[v];
+        float x[V];
+        load_up<float, V>(x, s.head + static_cast<uint64_t>(w) * s.dim_up + col);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += x[v];
+        T* const to = static_cast<T*>(s.table) + static_cast<uint64_t>(r) * s.table_stride + col;
+        Pack<T, V> there;
+        if (ADD) there = *reinterpret_cast<const Pack<T, V>*>(to);
+        store_row<T, V, ADD>(to, there, sum, s.scale);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) part[wave][lane].v[v] = sum[v];
-    __syncthreads();
-    if (wave != 0 || !in) return;
-    for (int o = 1; o < kJoinThreads / 64; ++o)
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += part[o][lane].v[v];
-    float x[V];
-    load_up<float, V>(x, s.head + static_cast<uint64_t>(w) * s.dim_up + col);
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] += x[v];
-    store_row<T, V, ADD>(static_cast<T*>(s.table) + static_cast<uint64_t>(r) * s.table_stride + col, sum, s.scale);
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
 // What the sort and the sums need of a call, by its sizes alone.
 struct GradientPlan {
     int bits = 0, passes = 0;
-    uint32_t tiles = 0, stretch = 0, stretches_all = 0, stretches_add = 0, dim_up = 0;
+    uint32_t chunk = 0, chunks = 0, stretch = 0, stretches_all = 0, stretches_add = 0, dim_up = 0;
     size_t bytes = 0;
-    uint32_t *key[2], *place[2], *counts, *totals;
+    uint32_t *key[2], *place[2], *counts;
     float *head, *tail;
+    uint32_t* joined;
 };
 
 GradientPlan plan_gradient(size_t n, size_t vocab, size_t dim, void* workspace) {
@@ -440,7 +451,8 @@ GradientPlan plan_gradient(size_t n, size_t vocab, size_t dim, void* workspace) 
     while (vocab >> all) ++all;
     g.passes = (all + kDigitBits - 1) / kDigitBits;
     g.bits = (all + g.passes - 1) / g.passes;
-    g.tiles = n <= kOneMost ? 1 : static_cast<uint32_t>(ceil_div(n, kTile));
+    g.chunk = static_cast<uint32_t>(ceil_div(ceil_div(n, kMostChunks), kTile) * kTile);
+    g.chunks = n <= kOneMost ? 1 : static_cast<uint32_t>(ceil_div(n, g.chunk));
     g.dim_up = static_cast<uint32_t>((dim + 7) / 8 * 8);
     // 64 places to a stretch; fewer where that leaves the GPU without waves, at least 8 (below that the joining costs more)
     const uint64_t columns = ceil_div(dim, 256);
@@ -452,40 +464,44 @@ GradientPlan plan_gradient(size_t n, size_t vocab, size_t dim, void* workspace) 
         g.key[i] = c.take<uint32_t>(n);
         g.place[i] = c.take<uint32_t>(n);
     }
-    g.counts = c.take<uint32_t>(g.tiles > 1 ? static_cast<size_t>(g.tiles) << g.bits : 0);
-    g.totals = c.take<uint32_t>(g.tiles > 1 ? kDigits : 0);
+    g.counts = c.take<uint32_t>(g.chunks > 1 ? static_cast<size_t>(g.chunks) << g.bits : 0);
     // only stretches that a token's position lies in have such rows, but any may
     const size_t rows = n > 0 ? static_cast<size_t>(g.stretches_all) * g.dim_up : 0;
     g.head = c.take<float>(rows);
     g.tail = c.take<float>(rows);
+    g.joined = c.take<uint32_t>(g.stretches_all);
     g.bytes = c.at;
     return g;
 }
 
 template <typename Token>
 blink_status_t sort_tokens(const Token* tokens, uint32_t n, uint32_t vocab, const GradientPlan& g, hipStream_t stream, int* where) {
-    if (g.tiles == 1) {
+    if (n <= kOneMost) {
         *where = 0;
-        return launch(embedding_sort_one<Token>, dim3(1), dim3(kOneThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
+        if (n <= kFewMost)
+            return launch(embedding_sort_one<Token, kFewThreads>, dim3(1), dim3(kFewThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
+        return launch(embedding_sort_one<Token, kOneThreads>, dim3(1), dim3(kOneThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
     }
     for (int pass = 0; pass < g.passes; ++pass) {
         const Token* const from = pass == 0 ? tokens : nullptr;
         const int shift = pass * g.bits, in = (pass + 1) & 1, out = pass & 1;
-        BLINK_TRY(launch(embedding_sort_count<Token>, dim3(g.tiles), dim3(kTileThreads), stream, from, g.key[in], n, vocab, shift, g.bits, g.tiles, g.counts));
-        BLINK_TRY(launch(embedding_sort_scan, dim3(1u << g.bits), dim3(kScanThreads), stream, g.counts, g.tiles, g.totals));
-        BLINK_TRY(launch(embedding_sort_move<Token>, dim3(g.tiles), dim3(kTileThreads), stream, from, g.key[in], g.place[in], n, vocab, shift, g.bits,
-                         g.tiles, g.counts, g.totals, g.key[out], g.place[out]));
+        BLINK_TRY(launch(embedding_sort_count<Token>, dim3(g.chunks), dim3(kTileThreads), stream, from, g.key[in], n, vocab, g.chunk, shift, g.bits, g.counts));
+        BLINK_TRY(launch(embedding_sort_move<Token>, dim3(g.chunks), dim3(kTileThreads), stream, from, g.key[in], g.place[in], n, vocab, g.chunk, shift, g.bits,
+                         g.counts, g.key[out], g.place[out]));
         *where = out;
     }
     return BLINK_OK;
 }
 
 template <typename Grad, typename T, int V>
-blink_status_t run_sums(const Sums& s, bool add, hipStream_t stream) {
-    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kSumThreads / 64)), static_cast<uint32_t>(ceil_div(s.dim, 64 * V)));
-    BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, grid, dim3(kSumThreads), stream, s));
+blink_status_t run_sums(Sums s, bool add, hipStream_t stream) {
+    s.columns = static_cast<uint32_t>(ceil_div(s.dim, 64 * V));
+    const uint64_t groups = ceil_div(static_cast<uint64_t>(s.stretches) * s.columns, kSumThreads / 64);
+    if (groups > 0x3fffffff) return BLINK_EINVAL;
+    BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, dim3(static_cast<uint32_t>(groups)), dim3(kSumThreads), stream, s));
     if (s.n < 2 || s.stretches < 2) return BLINK_OK;   // no row lies in two stretches
-    return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, dim3(s.stretches - 1, grid.y), dim3(kJoinThreads), stream, s);
+    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kJoinStretches)), s.columns);
+    return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, grid, dim3(kJoinThreads), stream, s);
 }
 
 }  // namespace
@@ -543,6 +559,7 @@ blink_status_t embedding_gradient(const void* tokens, blink_dtype_t token_type, 
     s.stretches = accumulate ? g.stretches_add : g.stretches_all;
     s.head = g.head;
     s.tail = g.tail;
+    s.joined = g.joined;
     s.dim_up = g.dim_up;
     return with_float(grad_type, [&](auto from) {
         return with_float(table_type, [&](auto to) -> blink_status_t {

@@ -19,6 +19,16 @@ struct alignas(sizeof(T) * N) Pack {
     T v[N];
 };
 
+// Stores a pack past the caches' usual order of replacement: results larger than the caches, not read again soon.
+template <typename P>
+__device__ inline void store_past(P* to, const P& y) {
+    typedef unsigned U4 __attribute__((ext_vector_type(4)));
+    typedef unsigned U2 __attribute__((ext_vector_type(2)));
+    if constexpr (sizeof(P) == 16) __builtin_nontemporal_store(__builtin_bit_cast(U4, y), reinterpret_cast<U4*>(to));
+    else if constexpr (sizeof(P) == 8) __builtin_nontemporal_store(__builtin_bit_cast(U2, y), reinterpret_cast<U2*>(to));
+    else *to = y;
+}
+
 inline size_t size_of(blink_dtype_t t) { return t == BLINK_INT64 ? 8 : t == BLINK_BF16 || t == BLINK_FP16 ? 2 : 4; }
 inline bool is_float(blink_dtype_t t) { return t == BLINK_FP32 || t == BLINK_BF16 || t == BLINK_FP16; }
 inline bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
