@@ -81,24 +81,17 @@ __device__ inline uint32_t rank_in_wave(uint32_t digit, bool in, int bits, volat
     return before + below;
 }
 
-// From counts[wave][digit]: begin[digit] becomes the sum of all smaller digits' items, counts[wave][digit] those of the digit in the waves before.
-template <int THREADS>
+// From counts[wave][digit]: begin[digit] becomes the sum of all smaller digits' items, counts[wave][digit] those of the digit in the waves
+// before.  Of a workgroup with a thread to a digit at least.
 __device__ inline void scan_counts(uint32_t (*counts)[kDigits], int digits, uint32_t* begin, uint32_t* wave_sum) {
-    constexpr int kEach = kDigits > THREADS ? kDigits / THREADS : 1;   // neighbouring digits of a thread
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    uint32_t own[kEach], total = 0;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const int digit = t * kEach + e;
-        own[e] = 0;
-        if (digit < digits)
-            for (int w = 0; w < THREADS / 64; ++w) {
-                const uint32_t c = counts[w][digit];
-                counts[w][digit] = own[e];
-                own[e] += c;
-            }
-        total += own[e];
-    }
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, waves = blockDim.x >> 6;
+    uint32_t total = 0;
+    if (t < digits)
+        for (int w = 0; w < waves; ++w) {
+            const uint32_t c = counts[w][t];
+            counts[w][t] = total;
+            total += c;
+        }
     uint32_t sum = total;
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t other = __shfl_up(sum, d);
@@ -106,13 +99,8 @@ __device__ inline void scan_counts(uint32_t (*counts)[kDigits], int digits, uint
     }
     if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
-    sum -= total;
     for (int w = 0; w < wave; ++w) sum += wave_sum[w];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        if (t * kEach + e < digits) begin[t * kEach + e] = sum;
-        sum += own[e];
-    }
+    if (t < digits) begin[t] = sum - total;
     __syncthreads();
 }
 
@@ -121,17 +109,49 @@ __device__ inline uint32_t key_of(Token token, uint32_t vocab) {
     return static_cast<uint64_t>(static_cast<int64_t>(token)) < vocab ? static_cast<uint32_t>(token) : vocab;
 }
 
-// Few tokens: one workgroup, the list in LDS from pass to pass; four waves do for up to 2048 (509 tokens, two passes: 1024 threads 8.5 us).
-constexpr int kOneItems = 8, kFewThreads = 256, kFewMost = kFewThreads * kOneItems, kOneThreads = 1024, kOneMost = kOneThreads * kOneItems;
-template <typename Token, int THREADS>
-__global__ __launch_bounds__(THREADS) void embedding_sort_one(const Token* tokens, uint32_t n, uint32_t vocab, int bits, int passes, uint32_t* key_out,
+// A token's place is the number of tokens that come before it.  Up to 2048 tokens are counted against one another, 64 tokens to a
+// workgroup, a part of the list to each of its waves: no passes that wait for one another (509 tokens: two passes of the next kernel 8.1 us).
+constexpr int kFewThreads = 256, kFewMost = 2048;
+template <typename Token>
+__global__ __launch_bounds__(kFewThreads) void embedding_sort_few(const Token* tokens, uint32_t n, uint32_t vocab, uint32_t* key_out, uint32_t* pos_out) {
+    constexpr int kWaves = kFewThreads / 64;
+    __shared__ __align__(16) uint32_t keys[kFewMost];
+    __shared__ uint32_t before[kWaves][64];
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), i = blockIdx.x * 64 + lane;
+    const uint32_t up = (n + 63) / 64 * 64;
+    for (uint32_t j = t; j < up; j += kFewThreads) keys[j] = j < n ? key_of(tokens[j], vocab) : ~0u;
+    __syncthreads();
+    const uint32_t key = keys[i];
+    uint32_t many = 0;
+    for (uint32_t block = wave; block < up / 64; block += kWaves) {
+        if (block == blockIdx.x) {
+#pragma unroll 16
+            for (uint32_t j = 0; j < 64; ++j) many += keys[block * 64 + j] < key + (j < lane);
+        } else {   // an equal one counts if it is in a block before
+            const uint32_t least = key + (block < blockIdx.x);
+#pragma unroll 16
+            for (uint32_t j = 0; j < 64; ++j) many += keys[block * 64 + j] < least;
+        }
+    }
+    before[wave][lane] = many;
+    __syncthreads();
+    if (wave != 0 || i >= n) return;
+    for (int w = 1; w < kWaves; ++w) many += before[w][lane];
+    key_out[many] = key;
+    pos_out[many] = i;
+}
+
+// More: one workgroup, the list in LDS from pass to pass.
+constexpr int kOneThreads = 1024, kOneItems = 8, kOneMost = kOneThreads * kOneItems;
+template <typename Token>
+__global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* tokens, uint32_t n, uint32_t vocab, int bits, int passes, uint32_t* key_out,
                                                               uint32_t* pos_out) {
-    __shared__ uint32_t counts[THREADS / 64][kDigits];
-    __shared__ uint32_t begin[kDigits], wave_sum[THREADS / 64];
-    __shared__ uint32_t keys[THREADS * kOneItems], places[THREADS * kOneItems];
+    __shared__ uint32_t counts[kOneThreads / 64][kDigits];
+    __shared__ uint32_t begin[kDigits], wave_sum[kOneThreads / 64];
+    __shared__ uint32_t keys[kOneMost], places[kOneMost];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, digits = 1 << bits;
     // every wave has a run of whole 64s, as few as hold them all
-    const uint32_t rounds = (n + THREADS - 1) / THREADS;
+    const uint32_t rounds = (n + kOneThreads - 1) / kOneThreads;
     const uint32_t first = wave * rounds * 64 + lane;
     uint32_t key[kOneItems], pos[kOneItems], rank[kOneItems];
 #pragma unroll
@@ -155,7 +175,7 @@ __global__ __launch_bounds__(THREADS) void embedding_sort_one(const Token* token
                 rank[j] = rank_in_wave(key[j] >> shift & (digits - 1), i < n, bits, counts[wave]);
             }
         __syncthreads();
-        scan_counts<THREADS>(counts, digits, begin, wave_sum);
+        scan_counts(counts, digits, begin, wave_sum);
 #pragma unroll
         for (int j = 0; j < kOneItems; ++j)
             if (j < static_cast<int>(rounds) && first + j * 64 < n) {
@@ -286,7 +306,7 @@ struct Sums {
     float scale;
     void* table;
     uint64_t table_stride;
-    uint32_t stretch;         // places of a wave
+    uint32_t stretch;         // places of a wave, at most 64
     uint32_t stretches, columns;   // waves beside one another on a row
     float *head, *tail;       // [stretch][dim]: what a stretch has of a row that began before it, of one that does not end in it
     uint32_t* joined;         // [stretch]: the row that began before the stretch and ends in it, or kNoRow
@@ -326,11 +346,16 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     T* const table = static_cast<T*>(s.table) + (in ? col : 0);
     const uint64_t places = static_cast<uint64_t>(s.n) + (ALL ? s.vocab : 0), d0 = static_cast<uint64_t>(w) * s.stretch;
     const uint64_t d1 = d0 + s.stretch < places ? d0 + s.stretch : places;
-    uint32_t p = __builtin_amdgcn_readfirstlane(positions_before<ALL>(s.keys, s.n, d0));
-    const uint32_t end = __builtin_amdgcn_readfirstlane(positions_before<ALL>(s.keys, s.n, d1));
+    const uint32_t p = __builtin_amdgcn_readfirstlane(positions_before<ALL>(s.keys, s.n, d0));
+    // the stretch's positions lie in the 64 from p on
+    const bool there_is = p + lane < s.n;
+    const uint32_t key = there_is ? s.keys[p + lane] : s.vocab, place = there_is ? s.places[p + lane] : 0;
+    const uint32_t last = p > 0 ? s.keys[p - 1] : kNoRow;
+    const uint32_t many = __popcll(__ballot(there_is && (ALL ? p + lane + static_cast<uint64_t>(key) < d1 : p + lane < d1))), end = p + many;
+    const uint32_t real = __popcll(__ballot(lane < many && key < s.vocab));   // padding comes last
     const uint32_t r_end = static_cast<uint32_t>(ALL ? d1 - end : s.vocab);   // rows below it end here (ALL)
-    uint32_t r = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ALL ? d0 - p : p < end ? s.keys[p] : s.vocab));
-    bool begun = p > 0 && r < s.vocab && __builtin_amdgcn_readfirstlane(s.keys[p - 1]) == r;   // the row has positions in an earlier stretch
+    uint32_t r = static_cast<uint32_t>(ALL ? d0 - p : __builtin_amdgcn_readfirstlane(key));
+    bool begun = p > 0 && r < s.vocab && __builtin_amdgcn_readfirstlane(last) == r;   // the row has positions in an earlier stretch
     bool any = false;                                                                          // and in this one
     float sum[V] = {};
     Pack<T, V> there;   // what the row holds (ADD)
@@ -352,61 +377,51 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
         } else
             for (; r < next; ++r) finish();
     };
-    while (p < end) {
-        const uint32_t many = end - p < 64 ? end - p : 64;
-        const uint32_t key = lane < many ? s.keys[p + lane] : s.vocab, place = lane < many ? s.places[p + lane] : 0;
-        const uint32_t real = __popcll(__ballot(key < s.vocab));   // padding comes last
-        for (uint32_t j = 0; j < real; j += kSumAhead) {
-            float x[kSumAhead][V];
-            Pack<T, V> held[kSumAhead];   // (a row's every time, so that none is waited for at its end)
+    for (uint32_t j = 0; j < real; j += kSumAhead) {
+        float x[kSumAhead][V];
+        Pack<T, V> held[kSumAhead];   // (a row's every time, so that none is waited for at its end)
 #pragma unroll
-            for (int a = 0; a < kSumAhead; ++a)
-                if (j + a < real) {
-                    const uint32_t row = __builtin_amdgcn_readlane(place, j + a), to = __builtin_amdgcn_readlane(key, j + a);
-                    if (in) load_up<Grad, V>(x[a], grad + static_cast<uint64_t>(row) * s.grad_stride);
-                    if (ADD && in) held[a] = *reinterpret_cast<const Pack<T, V>*>(table + static_cast<uint64_t>(to) * s.table_stride);
-                }
+        for (int a = 0; a < kSumAhead; ++a)
+            if (j + a < real) {
+                const uint32_t row = __builtin_amdgcn_readlane(place, j + a), to = __builtin_amdgcn_readlane(key, j + a);
+                if (in) load_up<Grad, V>(x[a], grad + static_cast<uint64_t>(row) * s.grad_stride);
+                if (ADD && in) held[a] = *reinterpret_cast<const Pack<T, V>*>(table + static_cast<uint64_t>(to) * s.table_stride);
+            }
 #pragma unroll
-            for (int a = 0; a < kSumAhead; ++a)
-                if (j + a < real) {
-                    finish_up_to(__builtin_amdgcn_readlane(key, j + a));
-                    any = true;
-                    if (ADD && in) there = held[a];
-                    if (in)
+        for (int a = 0; a < kSumAhead; ++a)
+            if (j + a < real) {
+                finish_up_to(__builtin_amdgcn_readlane(key, j + a));
+                any = true;
+                if (ADD && in) there = held[a];
+                if (in)
 #pragma unroll
-                        for (int i = 0; i < V; ++i) sum[i] += x[a][i];
-                }
-        }
-        p += many;
-        if (real < many) break;
+                    for (int i = 0; i < V; ++i) sum[i] += x[a][i];
+            }
     }
     if (ALL) finish_up_to(r_end);
     if (any) {
-        if (!ALL && (p >= s.n || __builtin_amdgcn_readfirstlane(s.keys[p]) != r)) finish();
+        if (!ALL && (end >= s.n || __builtin_amdgcn_readfirstlane(s.keys[end]) != r)) finish();
         else if (in) *reinterpret_cast<Pack<float, V>*>(s.tail + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
     }
     if (column == 0 && lane == 0) s.joined[w] = joins;
 }
 
-// Rows that several stretches share: their sums, joined in the order of the stretches.  A workgroup looks at four stretches; where
-// such a row ends in one, its waves take equal parts of the stretches before.
-constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64, kJoinStretches = 4;
+// Rows that several stretches share: their sums, joined in the order of the stretches.  A wave looks at the row that ends in its
+// stretch, if one does, and adds up a few parts by itself; the waves of a workgroup share the parts of longer rows.
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
+constexpr uint32_t kJoinAlone = 16;
 template <typename T, int V, bool ADD>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
     constexpr bool ALL = !ADD;
     __shared__ Pack<float, V> part[kJoinWaves][64];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t col = (blockIdx.y * 64 + lane) * V;
+    __shared__ uint32_t row_of[kJoinWaves], from_of[kJoinWaves];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t col = (blockIdx.y * 64 + lane) * V, w0 = blockIdx.x * kJoinWaves;
     const bool in = col < s.dim;
-    for (uint32_t w = blockIdx.x * kJoinStretches; w < (blockIdx.x + 1) * kJoinStretches && w < s.stretches; ++w) {
-        const uint32_t r = s.joined[w];
-        if (r == kNoRow) continue;
-        const uint32_t first = search(s.n, [&](uint64_t j) { return s.keys[j] < r; });
-        const uint32_t from = static_cast<uint32_t>((static_cast<uint64_t>(first) + (ALL ? r : 0)) / s.stretch), many = w - from;
-        const uint32_t each = (many + kJoinWaves - 1) / kJoinWaves;
-        const uint32_t a = from + min(many, wave * each), b = from + min(many, (wave + 1) * each);
-        float sum[V] = {};
-        if (in) {
+    const auto add_up = [&](float (&sum)[V], uint32_t a, uint32_t b) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+        if (in)
 #pragma unroll 8
             for (uint32_t i = a; i < b; ++i) {
                 float x[V];
@@ -414,15 +429,9 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) sum[v] += x[v];
             }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int v = 0; v < V; ++v) part[wave][lane].v[v] = sum[v];
-        __syncthreads();
-        if (wave != 0 || !in) continue;
-        for (int o = 1; o < kJoinWaves; ++o)
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += part[o][lane].v[v];
+    };
+    const auto finish = [&](float (&sum)[V], uint32_t w, uint32_t r) {
+        if (!in) return;
         float x[V];
         load_up<float, V>(x, s.head + static_cast<uint64_t>(w) * s.dim_up + col);
 #pragma unroll
@@ -431,6 +440,37 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
         Pack<T, V> there;
         if (ADD) there = *reinterpret_cast<const Pack<T, V>*>(to);
         store_row<T, V, ADD>(to, there, sum, s.scale);
+    };
+    float sum[V];
+    uint32_t r = w0 + wave < s.stretches ? __builtin_amdgcn_readfirstlane(s.joined[w0 + wave]) : kNoRow, from = 0;
+    if (r != kNoRow) {
+        const uint32_t first = search(s.n, [&](uint64_t j) { return s.keys[j] < r; });
+        from = static_cast<uint32_t>((static_cast<uint64_t>(first) + (ALL ? r : 0)) / s.stretch);
+        if (w0 + wave - from <= kJoinAlone) {
+            add_up(sum, from, w0 + wave);
+            finish(sum, w0 + wave, r);
+            r = kNoRow;
+        }
+    }
+    if (lane == 0) {
+        row_of[wave] = r;
+        from_of[wave] = from;
+    }
+    __syncthreads();
+    for (int q = 0; q < kJoinWaves; ++q) {
+        const uint32_t row = row_of[q], begin = from_of[q], many = w0 + q - begin, each = (many + kJoinWaves - 1) / kJoinWaves;
+        if (row == kNoRow) continue;
+        add_up(sum, begin + min(many, wave * each), begin + min(many, (wave + 1) * each));
+#pragma unroll
+        for (int v = 0; v < V; ++v) part[wave][lane].v[v] = sum[v];
+        __syncthreads();
+        if (wave == 0) {
+            for (int o = 1; o < kJoinWaves; ++o)
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[v] += part[o][lane].v[v];
+            finish(sum, w0 + q, row);
+        }
+        __syncthreads();
     }
 }
 
@@ -454,9 +494,10 @@ GradientPlan plan_gradient(size_t n, size_t vocab, size_t dim, void* workspace) 
     g.chunk = static_cast<uint32_t>(ceil_div(ceil_div(n, kMostChunks), kTile) * kTile);
     g.chunks = n <= kOneMost ? 1 : static_cast<uint32_t>(ceil_div(n, g.chunk));
     g.dim_up = static_cast<uint32_t>((dim + 7) / 8 * 8);
-    // 64 places to a stretch; fewer where that leaves the GPU without waves, at least 8 (below that the joining costs more)
+    // 32 places to a stretch (65536 tokens, 131072 x 1024 rows: 16 151 us, 32 153, 64 161, 128 165); fewer where that leaves the GPU
+    // without waves, at least 8 (below that the joining costs more)
     const uint64_t columns = ceil_div(dim, 256);
-    g.stretch = static_cast<uint32_t>(std::min<uint64_t>(64, std::max<uint64_t>(8, (n + vocab) * columns / 8192)));
+    g.stretch = static_cast<uint32_t>(std::min<uint64_t>(32, std::max<uint64_t>(8, (n + vocab) * columns / 8192)));
     g.stretches_all = static_cast<uint32_t>(ceil_div(n + vocab, g.stretch));
     g.stretches_add = static_cast<uint32_t>(ceil_div(n, g.stretch));
     Carve c(workspace);
@@ -479,8 +520,8 @@ blink_status_t sort_tokens(const Token* tokens, uint32_t n, uint32_t vocab, cons
     if (n <= kOneMost) {
         *where = 0;
         if (n <= kFewMost)
-            return launch(embedding_sort_one<Token, kFewThreads>, dim3(1), dim3(kFewThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
-        return launch(embedding_sort_one<Token, kOneThreads>, dim3(1), dim3(kOneThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
+            return launch(embedding_sort_few<Token>, dim3(static_cast<uint32_t>(ceil_div(n, 64))), dim3(kFewThreads), stream, tokens, n, vocab, g.key[0], g.place[0]);
+        return launch(embedding_sort_one<Token>, dim3(1), dim3(kOneThreads), stream, tokens, n, vocab, g.bits, g.passes, g.key[0], g.place[0]);
     }
     for (int pass = 0; pass < g.passes; ++pass) {
         const Token* const from = pass == 0 ? tokens : nullptr;
@@ -500,7 +541,7 @@ blink_status_t run_sums(Sums s, bool add, hipStream_t stream) {
     if (groups > 0x3fffffff) return BLINK_EINVAL;
     BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, dim3(static_cast<uint32_t>(groups)), dim3(kSumThreads), stream, s));
     if (s.n < 2 || s.stretches < 2) return BLINK_OK;   // no row lies in two stretches
-    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kJoinStretches)), s.columns);
+    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kJoinWaves)), s.columns);
     return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, grid, dim3(kJoinThreads), stream, s);
 }
 
