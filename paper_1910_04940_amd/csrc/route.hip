@@ -10,12 +10,13 @@
 // A token is counted if it is kept and not all of its logits are -inf.
 //
 // L lanes hold a token, N logits each; a wave holds 64 / L tokens and goes through tokens in strides of the grid, so that the
-// sums over tokens stay in registers until its end.  Workgroups leave their sums in the workspace, a second kernel adds
+// sums over tokens stay in registers until its end.  Every lane puts its logits in order by a network of exchanges; the k largest are
+// then the k largest of the lanes' first ones in turn, at a cost that hardly depends on N.  Workgroups leave their sums in the workspace, a second kernel adds
 // them up in order.  Both kernels over the logits read them once.
 #include "operators_api.hpp"
 
 #include <algorithm>
-#include <cmath>
+#include <type_traits>
 
 namespace blink {
 namespace {
@@ -26,10 +27,10 @@ constexpr float kInf = __builtin_inff();
 
 // ---- lanes of a token: L neighbours, L a power of two -----------------------------------------------------------------------
 // op(own value, the other half's), for halves of 1, 2, 4 ... lanes, each of which holds one value by then.
-template <int L, typename F>
-__device__ inline float over_lanes(float x, F op) {
-    const auto dpp = [](float v, auto control) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+template <int L, typename X, typename F>
+__device__ inline X over_lanes(X x, F op) {
+    const auto dpp = [](X v, auto control) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
     };
     if constexpr (L > 1) x = op(x, dpp(x, std::integral_constant<int, 0xB1>()));    // quad_perm 1 0 3 2
     if constexpr (L > 2) x = op(x, dpp(x, std::integral_constant<int, 0x4E>()));    // quad_perm 2 3 0 1
@@ -38,12 +39,12 @@ __device__ inline float over_lanes(float x, F op) {
     if constexpr (L > 16) {
         const unsigned v = __builtin_bit_cast(unsigned, x);
         const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        x = op(__builtin_bit_cast(float, static_cast<unsigned>(both[0])), __builtin_bit_cast(float, static_cast<unsigned>(both[1])));
+        x = op(__builtin_bit_cast(X, static_cast<unsigned>(both[0])), __builtin_bit_cast(X, static_cast<unsigned>(both[1])));
     }
     if constexpr (L > 32) {
         const unsigned v = __builtin_bit_cast(unsigned, x);
         const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        x = op(__builtin_bit_cast(float, static_cast<unsigned>(both[0])), __builtin_bit_cast(float, static_cast<unsigned>(both[1])));
+        x = op(__builtin_bit_cast(X, static_cast<unsigned>(both[0])), __builtin_bit_cast(X, static_cast<unsigned>(both[1])));
     }
     return x;
 }
@@ -56,26 +57,24 @@ __device__ inline float lanes_sum(float x) {
     return over_lanes<L>(x, [](float a, float b) { return a + b; });
 }
 template <int L>
-__device__ inline int lanes_min(int x) {   // of numbers below 2^23, as the floats that they are exactly
-    return static_cast<int>(over_lanes<L>(static_cast<float>(x), [](float a, float b) { return __builtin_fminf(a, b); }));
+__device__ inline unsigned lanes_max(unsigned x) {
+    return over_lanes<L>(x, [](unsigned a, unsigned b) { return a > b ? a : b; });
+}
+template <int L>
+__device__ inline unsigned lanes_min(unsigned x) {
+    return over_lanes<L>(x, [](unsigned a, unsigned b) { return a < b ? a : b; });
 }
 
-// Logits [lane * N, lane * N + N) of a token, -inf past the last.  WIDE: 16 bytes at a time.
-template <typename T, int N, bool WIDE>
+// Logits [first, first + N) of a token, -inf past the last; V of them at a time.
+template <typename T, int N, int V>
 __device__ inline void load_logits(float (&x)[N], const T* row, int first, int experts) {
-    if constexpr (WIDE) {
-        constexpr int V = 16 / sizeof(T) < N ? 16 / sizeof(T) : N;
 #pragma unroll
-        for (int i = 0; i < N; i += V) {
-            Pack<T, V> y;
-            const bool in = first + i < experts;
-            if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + first + i);
+    for (int i = 0; i < N; i += V) {
+        Pack<T, V> y;
+        const bool in = first + i < experts;
+        if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + first + i);
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[i + v] = in ? static_cast<float>(y.v[v]) : -kInf;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = first + i < experts ? static_cast<float>(row[first + i]) : -kInf;
+        for (int v = 0; v < V; ++v) x[i + v] = in ? static_cast<float>(y.v[v]) : -kInf;
     }
 }
 
@@ -119,10 +118,97 @@ struct Route {
     float* sums;
 };
 
-template <typename T, int L, int N, bool WIDE>
+// ---- the largest, in order --------------------------------------------------------------------------------------------------
+// A logit as a whole number of the same order, above 0 unless it is -inf, a NaN or past the last; equal logits, 0 and -0 among
+// them, are in the order of their index.  16-bit logits have room for the index below them, so one number is both.
+constexpr uint32_t kLowest = 0x007fffff;   // of -inf, as a 32-bit float
+
+__device__ inline uint32_t ordered(uint32_t bits) { return bits ^ (static_cast<uint32_t>(static_cast<int32_t>(bits) >> 31) | 0x80000000u); }
+__device__ inline uint32_t in_order(uint32_t o) { return o >> 31 ? o ^ 0x80000000u : ~o; }   // the bits again
+
+template <typename T>
+struct Key {   // a 16-bit logit and its index
+    static constexpr bool kBrain = std::is_same<T, __bf16>::value;
+    uint32_t v = 0;
+    __device__ static Key of(float x, uint32_t index) {
+        uint32_t bits;   // (adding 0 makes 0 of -0)
+        if constexpr (kBrain) bits = __builtin_bit_cast(uint32_t, x + 0.0f);
+        else bits = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<T>(x + 0.0f))) << 16;
+        Key k;
+        k.v = (ordered(bits) & 0xffff0000u) | (0xffffu - index);
+        return k;
+    }
+    static constexpr uint32_t kNone = kBrain ? 0x007fffff : 0x03ffffff;   // -inf's, of whatever index
+    __device__ bool valid() const { return v > kNone; }
+    __device__ uint32_t index() const { return 0xffffu - (v & 0xffffu); }
+    __device__ float value() const { return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(in_order(v & 0xffff0000u | 0xffffu) >> 16))); }
+    __device__ static void order(Key& a, Key& b) {   // a the larger
+        const uint32_t x = a.v, y = b.v;
+        a.v = x > y ? x : y;
+        b.v = x > y ? y : x;
+    }
+    template <int L>
+    __device__ static Key best(Key mine, bool* won) {
+        Key k;
+        k.v = lanes_max<L>(mine.v);
+        *won = k.v == mine.v;
+        return k;
+    }
+};
+template <>
+struct Key<float> {
+    uint32_t v = 0, i = 0xffffu;
+    __device__ static Key of(float x, uint32_t index) {
+        Key k;
+        k.v = ordered(__builtin_bit_cast(uint32_t, x + 0.0f));
+        k.i = index;
+        return k;
+    }
+    __device__ bool valid() const { return v > kLowest; }
+    __device__ uint32_t index() const { return i; }
+    __device__ float value() const { return __builtin_bit_cast(float, in_order(v)); }
+    __device__ static void order(Key& a, Key& b) {
+        const Key x = a, y = b;
+        const bool swap = y.v > x.v || (y.v == x.v && y.i < x.i);
+        a.v = swap ? y.v : x.v;
+        a.i = swap ? y.i : x.i;
+        b.v = swap ? x.v : y.v;
+        b.i = swap ? x.i : y.i;
+    }
+    template <int L>
+    __device__ static Key best(Key mine, bool* won) {
+        Key k;
+        k.v = lanes_max<L>(mine.v);
+        k.i = lanes_min<L>(mine.v == k.v ? mine.i : 0xffffu);
+        *won = k.v == mine.v && k.i == mine.i;
+        return k;
+    }
+};
+
+// Eight keys, the largest first (Batcher's odd-even merge sort, 19 exchanges).
+template <typename K>
+__device__ inline void sort8(K (&k)[8]) {
+    constexpr int pair[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                                 {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+    for (int e = 0; e < 19; ++e) K::order(k[pair[e][0]], k[pair[e][1]]);
+}
+// The same of eight that rise and then fall, or the other way round (12 exchanges).
+template <typename K>
+__device__ inline void merge8(K (&k)[8]) {
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(i & d)) K::order(k[i], k[i + d]);
+}
+
+// M: how many of its N logits a lane has to know in order, as many as k at the least or all; V logits to a load.
+template <typename T, int L, int N, int M, int V>
 __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     __shared__ int32_t count[L * N + 1];
     __shared__ float part[kWaves][L * N + 1];
+    using K = Key<T>;
     const int t = threadIdx.x, wave = t >> 6, lane = t & (L - 1), first = lane * N;
     for (int i = t; i <= L * N; i += kThreads) count[i] = 0;
     __syncthreads();
@@ -131,12 +217,31 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     const uint32_t step = gridDim.x * (kThreads / L);
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const bool keep = !a.keep || a.keep[token];
-        float x[N], free[N];
-        if (keep) load_logits<T, N, WIDE>(x, static_cast<const T*>(a.logits) + token * a.stride, first, a.experts);
+        float x[N];
+        if (keep) load_logits<T, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, first, a.experts);
+        else
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (!keep) x[i] = -kInf;
-            free[i] = x[i] == x[i] ? x[i] : -kInf;   // a NaN is not chosen
+            for (int i = 0; i < N; ++i) x[i] = -kInf;
+        K own[8], more[8];   // in order, `more` after `own`
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) nan |= __builtin_isunordered(x[i], x[i + 1]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) own[i] = K::of(x[i], first + i);
+        if constexpr (N == 16)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) more[i] = K::of(x[8 + i], first + 8 + i);
+        if (nan)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (x[i] != x[i]) (i < 8 ? own : more)[i % 8].v = 0;   // not chosen
+        sort8(own);
+        if constexpr (N == 16) {
+            sort8(more);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) K::order(own[i], more[7 - i]);
+            merge8(own);
+            if constexpr (M == 16) merge8(more);
         }
         float most, scale, lse;
         const bool any = softmax<L, N>(x, &most, &scale, &lse);
@@ -144,39 +249,38 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
         for (int i = 0; i < N; ++i) total[i] += x[i];
         z += lse * lse;
         counted += any;
-        // k times the largest that is left; lane j % L keeps the j-th until L are there
-        float sum = 0.0f, weight = 0.0f;
-        int which = -1;
+        // k times the largest of the lanes' first; lane j % L keeps the j-th until L are there
+        float sum = 0.0f;
+        K mine;
         for (int j = 0; j < a.k; ++j) {
-            float best = -kInf;
+            bool won;
+            const K best = K::template best<L>(own[0], &won);
+            if (won) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) best = __builtin_fmaxf(best, free[i]);
-            best = lanes_max<L>(best);
-            int at = 1 << 20;
+                for (int i = 0; i < 7; ++i) own[i] = own[i + 1];
+                if constexpr (M == 16) {
+                    own[7] = more[0];
 #pragma unroll
-            for (int i = N - 1; i >= 0; --i) at = free[i] == best ? first + i : at;
-            at = lanes_min<L>(at);
-            const bool found = best > -kInf;
-#pragma unroll
-            for (int i = 0; i < N; ++i) free[i] = first + i == at ? -kInf : free[i];
-            const float p = found ? power(best - most) * scale : 0.0f;
-            sum += p;
-            if (lane == j % L) {
-                which = found ? at : -1;
-                weight = p;
-                if (found) atomicAdd(&count[at], 1);
+                    for (int i = 0; i < 7; ++i) more[i] = more[i + 1];
+                    more[7] = K();
+                } else
+                    own[7] = K();
             }
+            if (lane == j % L) mine = best;
             if (j % L == L - 1 || j == a.k - 1) {
                 const int slot = j / L * L + lane;
+                const bool found = slot <= j && mine.valid();
+                const float p = found ? power(mine.value() - most) * scale : 0.0f;
+                if (a.normalize) sum += lanes_sum<L>(p);
+                if (found) atomicAdd(&count[mine.index()], 1);
                 if (slot <= j) {
-                    const uint64_t to = token * a.k + slot;
-                    a.chosen[to] = which;
-                    a.weights[to] = a.normalize && a.k <= L ? (any ? weight / sum : 0.0f) : weight;
+                    a.chosen[token * a.k + slot] = found ? static_cast<int32_t>(mine.index()) : -1;
+                    a.weights[token * a.k + slot] = a.normalize && a.k <= L && any ? p / sum : p;
                 }
             }
         }
-        if (a.normalize && a.k > L)
-            for (int j = lane; j < a.k; j += L) a.weights[token * a.k + j] = any ? a.weights[token * a.k + j] / sum : 0.0f;
+        if (a.normalize && a.k > L && any)
+            for (int j = lane; j < a.k; j += L) a.weights[token * a.k + j] /= sum;
     }
     // the wave's sums, token groups side by side first
 #pragma unroll
@@ -203,27 +307,33 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     }
 }
 
-// Adds up what the workgroups left: 64 columns to a workgroup, every wave a part of the rows, in 64 bits.
-constexpr int kAddThreads = 1024;
+// Adds up what the workgroups left, in 64 bits: eight columns to a workgroup, so that it has many loads under way at once.
+constexpr int kAddThreads = 1024, kAddColumns = 8;
 __global__ __launch_bounds__(kAddThreads) void route_add(const int32_t* counts, const float* sums, uint32_t groups, int columns, int32_t* count, float* sum) {
-    __shared__ double s[kAddThreads / 64][64];
-    __shared__ int32_t c[kAddThreads / 64][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = blockIdx.x * 64 + lane;
+    __shared__ double s[kAddThreads / 64][kAddColumns];
+    __shared__ int32_t c[kAddThreads / 64][kAddColumns];
+    const int t = threadIdx.x, at = t % kAddColumns, column = blockIdx.x * kAddColumns + at;
     double total = 0.0;
     int32_t many = 0;
     if (column < columns)
 #pragma unroll 4
-        for (uint32_t g = wave; g < groups; g += kAddThreads / 64) {
+        for (uint32_t g = t / kAddColumns; g < groups; g += kAddThreads / kAddColumns) {
             total += sums[static_cast<uint64_t>(g) * columns + column];
             many += counts[static_cast<uint64_t>(g) * columns + column];
         }
-    s[wave][lane] = total;
-    c[wave][lane] = many;
+    for (int d = kAddColumns; d < 64; d <<= 1) {
+        total += __shfl_xor(total, d);
+        many += __shfl_xor(many, d);
+    }
+    if ((t & 63) < kAddColumns) {
+        s[t >> 6][at] = total;
+        c[t >> 6][at] = many;
+    }
     __syncthreads();
-    if (wave != 0 || column >= columns) return;
+    if (t >= kAddColumns || column >= columns) return;
     for (int w = 1; w < kAddThreads / 64; ++w) {
-        total += s[w][lane];
-        many += c[w][lane];
+        total += s[w][at];
+        many += c[w][at];
     }
     sum[column] = static_cast<float>(total);
     count[column] = many;
@@ -257,7 +367,7 @@ struct RouteGradient {
     uint64_t out_stride;
 };
 
-template <typename T, int L, int N, bool WIDE>
+template <typename T, int L, int N, int V>
 __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGradient a) {
     __shared__ float by_weight[kThreads / L][L * N];   // what the weights' gradient adds to d, of the token that the lanes hold
     const int t = threadIdx.x, lane = t & (L - 1), first = lane * N;
@@ -273,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         const bool keep = !a.keep || a.keep[token];
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         float x[N], d[N];
-        if (keep) load_logits<T, N, WIDE>(x, row, first, a.experts);
+        if (keep) load_logits<T, N, V>(x, row, first, a.experts);
         if (!keep)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = -kInf;
@@ -312,42 +422,48 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         for (int i = 0; i < N; ++i) dot += x[i] * d[i];
         dot = lanes_sum<L>(dot) - by_lse * lse;
         T* const out = static_cast<T*>(a.out) + token * a.out_stride;
-        if constexpr (WIDE) {
-            constexpr int V = 16 / sizeof(T) < N ? 16 / sizeof(T) : N;
 #pragma unroll
-            for (int i = 0; i < N; i += V) {
-                Pack<T, V> y;
+        for (int i = 0; i < N; i += V) {
+            Pack<T, V> y;
 #pragma unroll
-                for (int v = 0; v < V; ++v) y.v[v] = static_cast<T>(any ? x[i + v] * (d[i + v] - dot) : 0.0f);
-                if (first + i < a.experts) *reinterpret_cast<Pack<T, V>*>(out + first + i) = y;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (first + i < a.experts) out[first + i] = static_cast<T>(any ? x[i] * (d[i] - dot) : 0.0f);
+            for (int v = 0; v < V; ++v) y.v[v] = static_cast<T>(any ? x[i + v] * (d[i + v] - dot) : 0.0f);
+            if (first + i < a.experts) *reinterpret_cast<Pack<T, V>*>(out + first + i) = y;
         }
     }
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
-// Eight logits to a lane (16 where 64 lanes of eight do not hold the token): f is called with the lanes and that number.
+// Sixteen logits to a lane (eight where they are all): f is called with the lanes and that number.  More lanes with eight each spend
+// more on what they do together: 262144 x 256, k = 8: 208 us with eight, by comparing all of them k times.
 template <typename F>
 blink_status_t with_lanes(int experts, F f) {
     using std::integral_constant;
-    using Eight = integral_constant<int, 8>;
-    if (experts <= 8) return f(integral_constant<int, 1>(), Eight());
-    if (experts <= 16) return f(integral_constant<int, 2>(), Eight());
-    if (experts <= 32) return f(integral_constant<int, 4>(), Eight());
-    if (experts <= 64) return f(integral_constant<int, 8>(), Eight());
-    if (experts <= 128) return f(integral_constant<int, 16>(), Eight());
-    if (experts <= 256) return f(integral_constant<int, 32>(), Eight());
-    if (experts <= 512) return f(integral_constant<int, 64>(), Eight());
-    return f(integral_constant<int, 64>(), integral_constant<int, 16>());
+    using Sixteen = integral_constant<int, 16>;
+    if (experts <= 8) return f(integral_constant<int, 1>(), integral_constant<int, 8>());
+    if (experts <= 16) return f(integral_constant<int, 1>(), Sixteen());
+    if (experts <= 32) return f(integral_constant<int, 2>(), Sixteen());
+    if (experts <= 64) return f(integral_constant<int, 4>(), Sixteen());
+    if (experts <= 128) return f(integral_constant<int, 8>(), Sixteen());
+    if (experts <= 256) return f(integral_constant<int, 16>(), Sixteen());
+    if (experts <= 512) return f(integral_constant<int, 32>(), Sixteen());
+    return f(integral_constant<int, 64>(), Sixteen());
+}
+
+// Calls f with the logits of a load: 16 bytes, 4 where those fit, one.
+template <typename T, typename F>
+blink_status_t with_load(int experts, size_t stride, const void* p, size_t other_stride, const void* q, F f) {
+    const auto fits = [&](size_t v) {
+        return experts % v == 0 && stride % v == 0 && other_stride % v == 0 && aligned(p, v * sizeof(T)) && aligned(q, v * sizeof(T));
+    };
+    constexpr int kWide = 16 / sizeof(T), kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (fits(kWide)) return f(std::integral_constant<int, kWide>());
+    if (fits(kTwo)) return f(std::integral_constant<int, kTwo>());
+    return f(std::integral_constant<int, 1>());
 }
 
 uint32_t lanes_of(int experts) {
     uint32_t l = 1;
-    while (l < 64 && static_cast<int>(l * 8) < experts) l <<= 1;
+    while (static_cast<int>(l * 16) < experts) l <<= 1;
     return l;
 }
 uint32_t groups_of(size_t tokens, int experts) {
@@ -377,15 +493,15 @@ blink_status_t route(const void* logits, blink_dtype_t dtype, size_t tokens, int
     }
     BLINK_TRY(with_float(dtype, [&](auto type) {
         using T = decltype(type);
-        constexpr size_t V = 16 / sizeof(T);
-        const bool wide = experts % V == 0 && stride % V == 0 && aligned(logits, 16);
-        return with_lanes(experts, [&](auto l, auto n) {
-            constexpr int L = decltype(l)::value, N = decltype(n)::value;
-            return launch(wide ? route_choose<T, L, N, true> : route_choose<T, L, N, false>, dim3(groups), dim3(kThreads), stream, a);
+        return with_load<T>(experts, stride, logits, stride, logits, [&](auto v) {
+            return with_lanes(experts, [&](auto l, auto n) {
+                constexpr int L = decltype(l)::value, N = decltype(n)::value, V = decltype(v)::value;
+                return launch(k <= 8 ? route_choose<T, L, N, 8, V> : route_choose<T, L, N, N, V>, dim3(groups), dim3(kThreads), stream, a);
+            });
         });
     }));
     if (groups == 1) return BLINK_OK;
-    return launch(route_add, dim3(static_cast<uint32_t>(ceil_div(experts + 1, 64))), dim3(kAddThreads), stream, a.counts, a.sums, groups, experts + 1,
+    return launch(route_add, dim3(static_cast<uint32_t>(ceil_div(experts + 1, kAddColumns))), dim3(kAddThreads), stream, a.counts, a.sums, groups, experts + 1,
                   counts, sums);
 }
 
@@ -403,11 +519,11 @@ blink_status_t route_gradient(const void* logits, blink_dtype_t dtype, size_t to
     const uint32_t groups = static_cast<uint32_t>(std::min<uint64_t>(4 * kMostGroups, ceil_div(tokens, kThreads / lanes_of(experts))));
     return with_float(dtype, [&](auto type) {
         using T = decltype(type);
-        constexpr size_t V = 16 / sizeof(T);
-        const bool wide = experts % V == 0 && stride % V == 0 && out_stride % V == 0 && aligned(logits, 16) && aligned(out, 16);
-        return with_lanes(experts, [&](auto l, auto n) {
-            constexpr int L = decltype(l)::value, N = decltype(n)::value;
-            return launch(wide ? route_gradient_kernel<T, L, N, true> : route_gradient_kernel<T, L, N, false>, dim3(groups), dim3(kThreads), stream, a);
+        return with_load<T>(experts, stride, logits, out_stride, out, [&](auto v) {
+            return with_lanes(experts, [&](auto l, auto n) {
+                constexpr int L = decltype(l)::value, N = decltype(n)::value, V = decltype(v)::value;
+                return launch(route_gradient_kernel<T, L, N, V>, dim3(groups), dim3(kThreads), stream, a);
+            });
         });
     });
 }
