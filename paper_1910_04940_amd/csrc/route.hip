@@ -66,21 +66,25 @@ __device__ inline unsigned lanes_min(unsigned x) {
 }
 
 // Logits [first, first + N) of a token, -inf past the last; V of them at a time.
-template <typename T, int N, int V>
+template <typename T, int L, int N, int V>
 __device__ inline void load_logits(float (&x)[N], const T* row, int first, int experts) {
+    const auto load = [&](auto all) {
 #pragma unroll
-    for (int i = 0; i < N; i += V) {
-        Pack<T, V> y;
-        const bool in = first + i < experts;
-        if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + first + i);
+        for (int i = 0; i < N; i += V) {
+            Pack<T, V> y;
+            const bool in = decltype(all)::value || first + i < experts;
+            if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + first + i);
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[i + v] = in ? static_cast<float>(y.v[v]) : -kInf;
-    }
+            for (int v = 0; v < V; ++v) x[i + v] = in ? static_cast<float>(y.v[v]) : -kInf;
+        }
+    };
+    if (experts == L * N) load(std::true_type());
+    else load(std::false_type());
 }
 
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }   // e^x, 0 for -inf
 
-// Softmax of a token: x becomes p.  False if all logits are -inf (p is then 0).  A NaN, or +inf, makes p NaN.
+// Softmax of a token: x becomes p / scale.  False if all logits are -inf (p is then 0).  A NaN, or +inf, makes p NaN.
 template <int L, int N>
 __device__ inline bool softmax(float (&x)[N], float* most, float* scale, float* lse) {
     float m = -kInf;
@@ -96,11 +100,8 @@ __device__ inline bool softmax(float (&x)[N], float* most, float* scale, float* 
     }
     s = lanes_sum<L>(s);
     const bool any = s != 0.0f;   // at least 1, or NaN
-    const float r = any ? 1.0f / s : 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] *= r;
     *most = from;
-    *scale = r;
+    *scale = any ? 1.0f / s : 0.0f;
     *lse = any ? from + logf(s) : 0.0f;
     return any;
 }
@@ -142,6 +143,10 @@ struct Key {   // a 16-bit logit and its index
     __device__ bool valid() const { return v > kNone; }
     __device__ uint32_t index() const { return 0xffffu - (v & 0xffffu); }
     __device__ float value() const { return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(in_order(v & 0xffff0000u | 0xffffu) >> 16))); }
+    __device__ static Key pick(bool first, Key a, Key b) {
+        a.v = first ? a.v : b.v;
+        return a;
+    }
     __device__ static void order(Key& a, Key& b) {   // a the larger
         const uint32_t x = a.v, y = b.v;
         a.v = x > y ? x : y;
@@ -167,6 +172,11 @@ struct Key<float> {
     __device__ bool valid() const { return v > kLowest; }
     __device__ uint32_t index() const { return i; }
     __device__ float value() const { return __builtin_bit_cast(float, in_order(v)); }
+    __device__ static Key pick(bool first, Key a, Key b) {
+        a.v = first ? a.v : b.v;
+        a.i = first ? a.i : b.i;
+        return a;
+    }
     __device__ static void order(Key& a, Key& b) {
         const Key x = a, y = b;
         const bool swap = y.v > x.v || (y.v == x.v && y.i < x.i);
@@ -218,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const bool keep = !a.keep || a.keep[token];
         float x[N];
-        if (keep) load_logits<T, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, first, a.experts);
+        if (keep) load_logits<T, L, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, first, a.experts);
         else
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = -kInf;
@@ -246,41 +256,65 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
         float most, scale, lse;
         const bool any = softmax<L, N>(x, &most, &scale, &lse);
 #pragma unroll
-        for (int i = 0; i < N; ++i) total[i] += x[i];
+        for (int i = 0; i < N; ++i) total[i] = __builtin_fmaf(x[i], scale, total[i]);
         z += lse * lse;
         counted += any;
-        // k times the largest of the lanes' first; lane j % L keeps the j-th until L are there
-        float sum = 0.0f;
-        K mine;
-        for (int j = 0; j < a.k; ++j) {
-            bool won;
-            const K best = K::template best<L>(own[0], &won);
-            if (won) {
+        // k times the largest of the lanes' first; lane j % L keeps the j-th
+        const auto write = [&](K key, int slot, float p) {
+            const bool found = key.valid();
+            if (found) atomicAdd(&count[key.index()], 1);
+            a.chosen[token * a.k + slot] = found ? static_cast<int32_t>(key.index()) : -1;
+            a.weights[token * a.k + slot] = p;
+        };
+        const auto weight = [&](K key) { return key.valid() ? power(key.value() - most) * scale : 0.0f; };
+        if constexpr (M == 8) {   // (k is at most 8: what the j-th leaves behind of a lane's keys gets shorter)
+            constexpr int kMine = (8 + L - 1) / L;
+            K mine[kMine];
 #pragma unroll
-                for (int i = 0; i < 7; ++i) own[i] = own[i + 1];
-                if constexpr (M == 16) {
-                    own[7] = more[0];
+            for (int j = 0; j < 8; ++j) {
+                if (j >= a.k) break;
+                bool won;
+                const K best = K::template best<L>(own[0], &won);
 #pragma unroll
-                    for (int i = 0; i < 7; ++i) more[i] = more[i + 1];
-                    more[7] = K();
-                } else
-                    own[7] = K();
+                for (int i = 0; i < 7 - j; ++i) own[i] = K::pick(won, own[i + 1], own[i]);
+                mine[j / L] = K::pick(lane == j % L, best, mine[j / L]);
             }
-            if (lane == j % L) mine = best;
-            if (j % L == L - 1 || j == a.k - 1) {
-                const int slot = j / L * L + lane;
-                const bool found = slot <= j && mine.valid();
-                const float p = found ? power(mine.value() - most) * scale : 0.0f;
-                if (a.normalize) sum += lanes_sum<L>(p);
-                if (found) atomicAdd(&count[mine.index()], 1);
-                if (slot <= j) {
-                    a.chosen[token * a.k + slot] = found ? static_cast<int32_t>(mine.index()) : -1;
-                    a.weights[token * a.k + slot] = a.normalize && a.k <= L && any ? p / sum : p;
+            float p[kMine], sum = 0.0f;
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) {
+                p[m] = m * L + lane < a.k ? weight(mine[m]) : 0.0f;
+                sum += p[m];
+            }
+            const float by = a.normalize && any ? 1.0f / lanes_sum<L>(sum) : 1.0f;
+#pragma unroll
+            for (int m = 0; m < kMine; ++m)
+                if (m * L + lane < a.k) write(mine[m], m * L + lane, p[m] * by);
+        } else {
+            float sum = 0.0f;
+            for (int from = 0; from < a.k; from += L) {
+                K mine;
+                for (int j = from; j < a.k && j < from + L; ++j) {
+                    bool won;
+                    const K best = K::template best<L>(own[0], &won);
+                    if (won) {
+#pragma unroll
+                        for (int i = 0; i < 7; ++i) own[i] = own[i + 1];
+                        own[7] = more[0];
+#pragma unroll
+                        for (int i = 0; i < 7; ++i) more[i] = more[i + 1];
+                        more[7] = K();
+                    }
+                    mine = K::pick(lane == j - from, best, mine);
                 }
+                const float p = from + lane < a.k ? weight(mine) : 0.0f;
+                sum += p;
+                if (from + lane < a.k) write(mine, from + lane, p);
+            }
+            if (a.normalize && any) {
+                const float by = 1.0f / lanes_sum<L>(sum);
+                for (int j = lane; j < a.k; j += L) a.weights[token * a.k + j] *= by;   // (its own)
             }
         }
-        if (a.normalize && a.k > L && any)
-            for (int j = lane; j < a.k; j += L) a.weights[token * a.k + j] /= sum;
     }
     // the wave's sums, token groups side by side first
 #pragma unroll
@@ -369,9 +403,14 @@ struct RouteGradient {
 
 template <typename T, int L, int N, int V>
 __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGradient a) {
-    __shared__ float by_weight[kThreads / L][L * N];   // what the weights' gradient adds to d, of the token that the lanes hold
+    // what the weights' gradient adds to d, of the tokens that the lanes hold; four neighbours of each lane side by side, and 0
+    // wherever no token's choice is being added
+    __shared__ __align__(16) float by_weight[kThreads / L][L * N];
     const int t = threadIdx.x, lane = t & (L - 1), first = lane * N;
     float* const add = by_weight[t / L];
+    const auto place = [](int e) { return ((e % N / 4) * L + e / N) * 4 + e % 4; };
+#pragma unroll
+    for (int i = 0; i < N; ++i) add[place(first + i)] = 0.0f;
     const float up = a.grad_loss ? *a.grad_loss : 1.0f;
     const float n = static_cast<float>(a.counts[a.experts] > 0 ? a.counts[a.experts] : 1);
     float by_p[N];
@@ -383,50 +422,67 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         const bool keep = !a.keep || a.keep[token];
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         float x[N], d[N];
-        if (keep) load_logits<T, N, V>(x, row, first, a.experts);
-        if (!keep)
+        // this lane's first choice travels with the logits
+        const bool adds = a.grad_weights && keep;
+        const auto choice = [&](int j, int* e, float* g) {
+            *e = j < a.k ? a.chosen[token * a.k + j] : -1;
+            *g = j < a.k ? a.grad_weights[token * a.k + j] : 0.0f;
+            if (*e >= a.experts) *e = -1;
+        };
+        int e0 = -1;
+        float g0 = 0.0f;
+        if (adds) choice(lane, &e0, &g0);
+        if (keep) load_logits<T, L, N, V>(x, row, first, a.experts);
+        else
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = -kInf;
         float most, scale, lse;
         const bool any = softmax<L, N>(x, &most, &scale, &lse);
 #pragma unroll
         for (int i = 0; i < N; ++i) d[i] = by_p[i];
-        if (a.grad_weights && keep) {
+        if (adds) {
             // lanes of a token are lanes of one wave, whose accesses to LDS happen in order
-#pragma unroll
-            for (int i = 0; i < N; ++i) add[first + i] = 0.0f;
-            float sum = 1.0f, dot = 0.0f;
+            const auto each = [&](auto f) {
+                if (e0 >= 0) f(e0, g0);
+                for (int j = lane + L; j < a.k; j += L) {
+                    int e;
+                    float g;
+                    choice(j, &e, &g);
+                    if (e >= 0) f(e, g);
+                }
+            };
+            float by = 1.0f, dot = 0.0f;
             if (a.normalize) {   // d of the chosen: (g - sum w g) / S
-                sum = 0.0f;
-                for (int j = lane; j < a.k; j += L) {
-                    const int e = a.chosen[token * a.k + j];
-                    if (e < 0 || e >= a.experts) continue;
+                float sum = 0.0f;
+                each([&](int e, float g) {
                     const float p = power(static_cast<float>(row[e]) - most) * scale;
                     sum += p;
-                    dot += p * a.grad_weights[token * a.k + j];
-                }
-                sum = lanes_sum<L>(sum);
-                dot = lanes_sum<L>(dot) / sum;
+                    dot = __builtin_fmaf(p, g, dot);
+                });
+                by = 1.0f / lanes_sum<L>(sum);
+                dot = lanes_sum<L>(dot) * by;
             }
-            wave_sync();
-            for (int j = lane; j < a.k; j += L) {
-                const int e = a.chosen[token * a.k + j];
-                if (e >= 0 && e < a.experts) add[e] = (a.grad_weights[token * a.k + j] - dot) / sum;
-            }
+            each([&](int e, float g) { add[place(e)] = (g - dot) * by; });
             wave_sync();
 #pragma unroll
-            for (int i = 0; i < N; ++i) d[i] += add[first + i];
+            for (int i = 0; i < N; ++i) d[i] += add[place(first + i)];
+            wave_sync();
+            each([&](int e, float) { add[place(e)] = 0.0f; });
+            wave_sync();
         }
         float dot = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) dot += x[i] * d[i];
-        dot = lanes_sum<L>(dot) - by_lse * lse;
+        for (int i = 0; i < N; ++i) dot = __builtin_fmaf(x[i], d[i], dot);
+        dot = lanes_sum<L>(dot) * scale - by_lse * lse;
         T* const out = static_cast<T*>(a.out) + token * a.out_stride;
 #pragma unroll
         for (int i = 0; i < N; i += V) {
             Pack<T, V> y;
 #pragma unroll
-            for (int v = 0; v < V; ++v) y.v[v] = static_cast<T>(any ? x[i + v] * (d[i + v] - dot) : 0.0f);
+            for (int v = 0; v < V; ++v) {
+                const float z = x[i + v] * scale * (d[i + v] - dot);
+                y.v[v] = static_cast<T>(any ? z : 0.0f);
+            }
             if (first + i < a.experts) *reinterpret_cast<Pack<T, V>*>(out + first + i) = y;
         }
     }
