@@ -21,21 +21,21 @@ namespace {
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
-constexpr int kRowUnits = 4;   // packs of one thread, their loads under way together
+constexpr int kRowUnits = 2;   // packs of one thread, their loads under way together (131072 x 2048: 115 us, 4 packs 119, 8 121)
 
 // A pack is V elements; a row has `packs` of them.  Places go out pack by pack through all rows, so short and long rows
 // fill the waves alike.
-template <typename In, typename Out, typename Token, int V>
+template <typename In, typename Out, typename Token, typename Unit, int V>
 __global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, uint64_t vocab, uint64_t table_stride, const Token* tokens,
-                                                              uint64_t units, uint32_t packs, float scale, Out* out, uint64_t out_stride) {
-    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kRowThreads * kRowUnits) + threadIdx.x;
+                                                              Unit units, uint32_t packs, float scale, Out* out, uint64_t out_stride, bool past) {
+    const Unit first = static_cast<Unit>(blockIdx.x) * (kRowThreads * kRowUnits) + threadIdx.x;   // (a Unit holds the grid's places)
     int64_t token[kRowUnits];
     uint64_t row[kRowUnits];
     uint32_t at[kRowUnits];
 #pragma unroll
     for (int u = 0; u < kRowUnits; ++u) {
-        const uint64_t unit = first + u * kRowThreads;
-        row[u] = unit >> 32 ? unit / packs : static_cast<uint32_t>(unit) / packs;
+        const Unit unit = first + u * kRowThreads;
+        row[u] = unit / packs;
         at[u] = static_cast<uint32_t>(unit - row[u] * packs) * V;
         token[u] = unit < units ? static_cast<int64_t>(tokens[row[u]]) : -1;
     }
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, u
             if constexpr (sizeof(Out) < 4) asm("" : "+v"(z));   // a 32-bit product: the mixed 16-bit one rounds it otherwise
             y.v[i] = static_cast<uint64_t>(token[u]) < vocab ? static_cast<Out>(z) : static_cast<Out>(0.0f);
         }
-        if (first + u * kRowThreads < units) store_past(reinterpret_cast<Pack<Out, V>*>(out + row[u] * out_stride + at[u]), y);
+        if (first + u * kRowThreads < units) store_result(past, reinterpret_cast<Pack<Out, V>*>(out + row[u] * out_stride + at[u]), y);
     }
 }
 
@@ -311,6 +311,7 @@ struct Sums {
     float *head, *tail;       // [stretch][dim]: what a stretch has of a row that began before it, of one that does not end in it
     uint32_t* joined;         // [stretch]: the row that began before the stretch and ends in it, or kNoRow
     uint32_t dim_up;          // elements of a row of head and tail
+    bool past;
 };
 constexpr uint32_t kNoRow = ~0u;
 
@@ -322,11 +323,10 @@ __device__ inline void load_up(float (&x)[V], const T* p) {
 }
 // The row's final sum: scaled, added to `y`, what is there, where ADD, rounded once.
 template <typename T, int V, bool ADD>
-__device__ inline void store_row(T* p, Pack<T, V> y, const float (&sum)[V], float scale) {
+__device__ inline void store_row(bool past, T* p, Pack<T, V> y, const float (&sum)[V], float scale) {
 #pragma unroll
     for (int i = 0; i < V; ++i) y.v[i] = static_cast<T>(ADD ? __builtin_fmaf(scale, sum[i], static_cast<float>(y.v[i])) : scale * sum[i]);
-    if (ADD) *reinterpret_cast<Pack<T, V>*>(p) = y;
-    else store_past(reinterpret_cast<Pack<T, V>*>(p), y);
+    store_result(past, reinterpret_cast<Pack<T, V>*>(p), y);
 }
 
 constexpr int kSumThreads = 256;
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
         if (begun) joins = r;
         if (in) {
             if (begun) *reinterpret_cast<Pack<float, V>*>(s.head + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
-            else if (ALL || any) store_row<T, V, ADD>(table + static_cast<uint64_t>(r) * s.table_stride, there, sum, s.scale);
+            else if (ALL || any) store_row<T, V, ADD>(s.past, table + static_cast<uint64_t>(r) * s.table_stride, there, sum, s.scale);
         }
         begun = any = false;
 #pragma unroll
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
         T* const to = static_cast<T*>(s.table) + static_cast<uint64_t>(r) * s.table_stride + col;
         Pack<T, V> there;
         if (ADD) there = *reinterpret_cast<const Pack<T, V>*>(to);
-        store_row<T, V, ADD>(to, there, sum, s.scale);
+        store_row<T, V, ADD>(s.past, to, there, sum, s.scale);
     };
     float sum[V];
     uint32_t r = w0 + wave < s.stretches ? __builtin_amdgcn_readfirstlane(s.joined[w0 + wave]) : kNoRow, from = 0;
@@ -565,9 +565,14 @@ blink_status_t embedding(const void* table, blink_dtype_t table_type, size_t voc
             if (blocks > 0x7fffffff) return BLINK_EINVAL;
             const auto with_token = [&](auto token) {
                 using Token = decltype(token);
-                const auto kernel = v == kMost ? embedding_rows<In, Out, Token, kMost> : embedding_rows<In, Out, Token, 1>;
-                return launch(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kRowThreads), stream, static_cast<const In*>(table), vocab, table_stride,
-                              static_cast<const Token*>(tokens), units, static_cast<uint32_t>(packs), scale, static_cast<Out*>(out), out_stride);
+                const auto go = [&](auto kernel) {
+                    return launch(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kRowThreads), stream, static_cast<const In*>(table), vocab, table_stride,
+                                  static_cast<const Token*>(tokens), units, static_cast<uint32_t>(packs), scale, static_cast<Out*>(out), out_stride,
+                                  passes_caches(n * dim * sizeof(Out)));
+                };
+                if (blocks * kRowThreads * kRowUnits >> 32)
+                    return v == kMost ? go(embedding_rows<In, Out, Token, uint64_t, kMost>) : go(embedding_rows<In, Out, Token, uint64_t, 1>);
+                return v == kMost ? go(embedding_rows<In, Out, Token, uint32_t, kMost>) : go(embedding_rows<In, Out, Token, uint32_t, 1>);
             };
             return token_type == BLINK_INT64 ? with_token(int64_t()) : with_token(int32_t());
         });
@@ -602,6 +607,7 @@ blink_status_t embedding_gradient(const void* tokens, blink_dtype_t token_type, 
     s.tail = g.tail;
     s.joined = g.joined;
     s.dim_up = g.dim_up;
+    s.past = !accumulate && passes_caches(vocab * dim * size_of(table_type));
     return with_float(grad_type, [&](auto from) {
         return with_float(table_type, [&](auto to) -> blink_status_t {
             using Grad = decltype(from);

@@ -65,15 +65,25 @@ __device__ inline unsigned lanes_min(unsigned x) {
     return over_lanes<L>(x, [](unsigned a, unsigned b) { return a < b ? a : b; });
 }
 
-// Logits [first, first + N) of a token, -inf past the last; V of them at a time.
+// The expert whose logit is a lane's i-th: 16 bytes of neighbours to a lane, then the next lane's, so that a load of the wave is one
+// piece.  How wide the loads really are changes nothing in it, so that sums do not depend on where a row starts.
+template <typename T>
+constexpr int kNeighbours = 16 / sizeof(T);
+template <typename T, int L>
+__device__ inline int expert_of(int lane, int i) {
+    return (i / kNeighbours<T> * L + lane) * kNeighbours<T> + i % kNeighbours<T>;
+}
+
+// A lane's logits, -inf past the last; V of them at a time.
 template <typename T, int L, int N, int V>
-__device__ inline void load_logits(float (&x)[N], const T* row, int first, int experts) {
+__device__ inline void load_logits(float (&x)[N], const T* row, int lane, int experts) {
     const auto load = [&](auto all) {
 #pragma unroll
         for (int i = 0; i < N; i += V) {
             Pack<T, V> y;
-            const bool in = decltype(all)::value || first + i < experts;
-            if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + first + i);
+            const int e = expert_of<T, L>(lane, i);
+            const bool in = decltype(all)::value || e < experts;
+            if (in) y = *reinterpret_cast<const Pack<T, V>*>(row + e);
 #pragma unroll
             for (int v = 0; v < V; ++v) x[i + v] = in ? static_cast<float>(y.v[v]) : -kInf;
         }
@@ -219,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     __shared__ int32_t count[L * N + 1];
     __shared__ float part[kWaves][L * N + 1];
     using K = Key<T>;
-    const int t = threadIdx.x, wave = t >> 6, lane = t & (L - 1), first = lane * N;
+    const int t = threadIdx.x, wave = t >> 6, lane = t & (L - 1);
     for (int i = t; i <= L * N; i += kThreads) count[i] = 0;
     __syncthreads();
     float total[N] = {}, z = 0.0f;
@@ -228,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const bool keep = !a.keep || a.keep[token];
         float x[N];
-        if (keep) load_logits<T, L, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, first, a.experts);
+        if (keep) load_logits<T, L, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, lane, a.experts);
         else
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = -kInf;
@@ -237,10 +247,10 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
 #pragma unroll
         for (int i = 0; i < N; i += 2) nan |= __builtin_isunordered(x[i], x[i + 1]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) own[i] = K::of(x[i], first + i);
+        for (int i = 0; i < 8; ++i) own[i] = K::of(x[i], expert_of<T, L>(lane, i));
         if constexpr (N == 16)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) more[i] = K::of(x[8 + i], first + 8 + i);
+            for (int i = 0; i < 8; ++i) more[i] = K::of(x[8 + i], expert_of<T, L>(lane, 8 + i));
         if (nan)
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -326,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     }
     if ((t & 63) < L)
 #pragma unroll
-        for (int i = 0; i < N; ++i) part[wave][first + i] = total[i];
+        for (int i = 0; i < N; ++i) part[wave][expert_of<T, L>(lane, i)] = total[i];
     if ((t & 63) == 0) {
         part[wave][L * N] = z;
         atomicAdd(&count[L * N], counted);
@@ -399,6 +409,7 @@ struct RouteGradient {
     float balance, z;
     void* out;
     uint64_t out_stride;
+    bool past;
 };
 
 template <typename T, int L, int N, int V>
@@ -406,16 +417,21 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
     // what the weights' gradient adds to d, of the tokens that the lanes hold; four neighbours of each lane side by side, and 0
     // wherever no token's choice is being added
     __shared__ __align__(16) float by_weight[kThreads / L][L * N];
-    const int t = threadIdx.x, lane = t & (L - 1), first = lane * N;
+    const int t = threadIdx.x, lane = t & (L - 1);
     float* const add = by_weight[t / L];
-    const auto place = [](int e) { return ((e % N / 4) * L + e / N) * 4 + e % 4; };
+    constexpr int G = kNeighbours<T>;
+    const auto place_at = [](int lane, int i) { return (i / 4 * L + lane) * 4 + i % 4; };
+    const auto place = [&](int e) { return place_at(e / G % L, e / (G * L) * G + e % G); };
 #pragma unroll
-    for (int i = 0; i < N; ++i) add[place(first + i)] = 0.0f;
+    for (int i = 0; i < N; ++i) add[place_at(lane, i)] = 0.0f;
     const float up = a.grad_loss ? *a.grad_loss : 1.0f;
     const float n = static_cast<float>(a.counts[a.experts] > 0 ? a.counts[a.experts] : 1);
     float by_p[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) by_p[i] = first + i < a.experts ? up * a.balance * a.experts / a.k * (a.counts[first + i] / n) / n : 0.0f;
+    for (int i = 0; i < N; ++i) {
+        const int e = expert_of<T, L>(lane, i);
+        by_p[i] = e < a.experts ? up * a.balance * a.experts / a.k * (a.counts[e] / n) / n : 0.0f;
+    }
     const float by_lse = 2.0f * up * a.z / n;
     const uint32_t step = gridDim.x * (kThreads / L);
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
@@ -432,7 +448,7 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         int e0 = -1;
         float g0 = 0.0f;
         if (adds) choice(lane, &e0, &g0);
-        if (keep) load_logits<T, L, N, V>(x, row, first, a.experts);
+        if (keep) load_logits<T, L, N, V>(x, row, lane, a.experts);
         else
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = -kInf;
@@ -465,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
             each([&](int e, float g) { add[place(e)] = (g - dot) * by; });
             wave_sync();
 #pragma unroll
-            for (int i = 0; i < N; ++i) d[i] += add[place(first + i)];
+            for (int i = 0; i < N; ++i) d[i] += add[place_at(lane, i)];
             wave_sync();
             each([&](int e, float) { add[place(e)] = 0.0f; });
             wave_sync();
@@ -473,17 +489,18 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         float dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) dot = __builtin_fmaf(x[i], d[i], dot);
-        dot = lanes_sum<L>(dot) * scale - by_lse * lse;
+        dot = (by_lse * lse - lanes_sum<L>(dot) * scale) * scale;
         T* const out = static_cast<T*>(a.out) + token * a.out_stride;
 #pragma unroll
         for (int i = 0; i < N; i += V) {
             Pack<T, V> y;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float z = x[i + v] * scale * (d[i + v] - dot);
+                const float z = x[i + v] * __builtin_fmaf(scale, d[i + v], dot);
                 y.v[v] = static_cast<T>(any ? z : 0.0f);
             }
-            if (first + i < a.experts) *reinterpret_cast<Pack<T, V>*>(out + first + i) = y;
+            const int e = expert_of<T, L>(lane, i);
+            if (e < a.experts) store_result(a.past, reinterpret_cast<Pack<T, V>*>(out + e), y);
         }
     }
 }
@@ -570,7 +587,7 @@ blink_status_t route_gradient(const void* logits, blink_dtype_t dtype, size_t to
                               float balance, float z, void* out, size_t out_stride, hipStream_t stream) {
     if (tokens == 0) return BLINK_OK;
     const RouteGradient a{logits, stride, keep, static_cast<uint32_t>(tokens), experts, k, normalize, chosen, grad_weights, counts, grad_loss,
-                          balance, z, out, out_stride};
+                          balance, z, out, out_stride, passes_caches(tokens * experts * size_of(dtype))};
     // no sums are kept from token to token: as many workgroups as there are tokens for, in the end
     const uint32_t groups = static_cast<uint32_t>(std::min<uint64_t>(4 * kMostGroups, ceil_div(tokens, kThreads / lanes_of(experts))));
     return with_float(dtype, [&](auto type) {
