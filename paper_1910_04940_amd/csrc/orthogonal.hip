@@ -51,31 +51,44 @@ struct Outer {
     float rate, keep;        // weights' = keep * weights - rate * result
 };
 
-// U's element, given the new momentum where there is one.
+// U's element from the gradient's and the new momentum's; from the caller's buffers.
+__device__ inline float update_of(const Outer& o, float g, float m) { return o.nesterov ? __builtin_fmaf(o.beta, m, g) : m; }
 template <typename In>
-__device__ inline float update_of(const Outer& o, uint64_t batch, uint32_t r, uint32_t c) {
+__device__ inline float update_at(const Outer& o, uint64_t batch, uint32_t r, uint32_t c) {
     const float g = static_cast<float>(static_cast<const In*>(o.in)[batch * o.in_batch + r * o.in_row + c]);
-    if (!o.momentum) return g;
-    const float m = o.momentum_out[(batch * o.rows + r) * o.cols + c];
-    return o.nesterov ? __builtin_fmaf(o.beta, m, g) : m;
+    return o.momentum ? update_of(o, g, o.momentum_out[(batch * o.rows + r) * o.cols + c]) : g;
 }
 
 // ---- the norm, and the momentum ------------------------------------------------------------------------------------------
-// A workgroup per part of a matrix; squares are added in 64 bits, where no 32-bit float's overflows or vanishes.
-constexpr int kNormThreads = 256, kNormMost = 256;
-template <typename In>
+// A workgroup per part of a matrix; squares are added in 64 bits, where no 32-bit float's overflows or vanishes.  V neighbours to a
+// thread at a time.
+constexpr int kNormThreads = 256, kNormMost = 1024;
+template <typename In, int V>
 __global__ __launch_bounds__(kNormThreads) void ortho_norm(const Outer o, double* parts) {
     __shared__ double wave_sum[kNormThreads / 64];
     const uint64_t batch = blockIdx.y, all = static_cast<uint64_t>(o.rows) * o.cols;
+    const uint32_t packs = o.cols / V;   // of a row
+    const uint64_t units = static_cast<uint64_t>(o.rows) * packs, step = static_cast<uint64_t>(gridDim.x) * kNormThreads;
     double s = 0.0;
-    for (uint64_t e = blockIdx.x * static_cast<uint64_t>(kNormThreads) + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kNormThreads) {
-        const uint32_t r = static_cast<uint32_t>(all >> 32 ? e / o.cols : static_cast<uint32_t>(e) / o.cols), c = static_cast<uint32_t>(e - static_cast<uint64_t>(r) * o.cols);
+#pragma unroll 4
+    for (uint64_t e = blockIdx.x * static_cast<uint64_t>(kNormThreads) + threadIdx.x; e < units; e += step) {
+        const uint32_t r = static_cast<uint32_t>(units >> 32 ? e / packs : static_cast<uint32_t>(e) / packs), c = static_cast<uint32_t>(e - static_cast<uint64_t>(r) * packs) * V;
+        const Pack<In, V> g = *reinterpret_cast<const Pack<In, V>*>(static_cast<const In*>(o.in) + batch * o.in_batch + r * o.in_row + c);
+        float u[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) u[v] = static_cast<float>(g.v[v]);
         if (o.momentum) {
-            const float g = static_cast<float>(static_cast<const In*>(o.in)[batch * o.in_batch + r * o.in_row + c]);
-            o.momentum_out[batch * all + e] = __builtin_fmaf(o.beta, o.momentum[batch * all + e], g);
+            const uint64_t at = batch * all + static_cast<uint64_t>(r) * o.cols + c;
+            Pack<float, V> m = *reinterpret_cast<const Pack<float, V>*>(o.momentum + at);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                m.v[v] = __builtin_fmaf(o.beta, m.v[v], u[v]);
+                u[v] = update_of(o, u[v], m.v[v]);
+            }
+            *reinterpret_cast<Pack<float, V>*>(o.momentum_out + at) = m;
         }
-        const double u = update_of<In>(o, batch, r, c);
-        s += u * u;
+#pragma unroll
+        for (int v = 0; v < V; ++v) s = __builtin_fma(static_cast<double>(u[v]), static_cast<double>(u[v]), s);
     }
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
@@ -129,6 +142,14 @@ __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool
     const int t = threadIdx.x;
     const uint64_t batch = blockIdx.z;
     const uint32_t i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+    // along the caller's contiguous index: X's columns, or its rows where U is tall
+    const uint32_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+    float u[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        const uint32_t r = r0 + q * 4 + t / 64, c = c0 + t % 64;
+        u[q] = r < o.rows && c < o.cols ? update_at<In>(o, batch, r, c) : 0.0f;
+    }
     if (t < 64) {
         double s = 0.0;
         for (uint32_t p = t; p < n_parts; p += 64) s += parts[batch * n_parts + p];
@@ -138,14 +159,11 @@ __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool
             factor = norm == 0.0 ? 0.0 : kScaleX / norm;
         }
     }
-    // along the caller's contiguous index: X's columns, or its rows where U is tall
-    const uint32_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-#pragma unroll 4
+#pragma unroll
     for (int q = 0; q < 16; ++q) {
         const uint32_t r = q * 4 + t / 64, c = t % 64;
-        const float u = r0 + r < o.rows && c0 + c < o.cols ? update_of<In>(o, batch, r0 + r, c0 + c) : 0.0f;
-        if (tall) tile[c][r] = u;
-        else tile[r][c] = u;
+        if (tall) tile[c][r] = u[q];
+        else tile[r][c] = u[q];
     }
     __syncthreads();
     const double f = factor;
@@ -176,7 +194,7 @@ struct Factors {
 
 // A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, or 64 where both operands are
 // single, so a row of a stage is 128 bytes (64 where it is single and the other is not).  Stages are copied to LDS by
-// the loads themselves, one ahead of the stage that is multiplied.  The eight 16-byte parts of a line lie in the order part ^
+// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 64).  The eight 16-byte parts of a line lie in the order part ^
 // line % 8, so that a block's 32 rows, read part by part, fall on all banks.
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
 struct Tile {
@@ -185,6 +203,8 @@ struct Tile {
     static constexpr int kLineP = PP == QP || PP ? 128 : 64, kLineQ = PP == QP || QP ? 128 : 64;   // bytes of a row's stage
     static constexpr int kBytesP = TM * kLineP, kBytesQ = TN * kLineQ, kBytes = kBytesP + kBytesQ;
     static constexpr int kWM = TM / WAVES_M, kWN = TN / WAVES_N, kBM = kWM / 32, kBN = kWN / 32;
+    static constexpr int kCopies = kBytes / 16 / kThreads;            // of a thread, for a stage
+    static constexpr int kAhead = TM <= 64 ? 3 : 1;                   // stages on their way while one is multiplied
     static constexpr int kBlock = 32 * 33 * 4;                        // bytes of a wave's block at the end
     static_assert(WAVES_M * WAVES_N * kBlock <= 2 * kBytes, "the blocks fit the stages");
 };
@@ -257,8 +277,9 @@ __device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
     using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
-    __shared__ __align__(1024) char even[S::kBytes];
-    __shared__ __align__(1024) char odd[S::kBytes];
+    // (arrays of their own, so that the compiler knows which loads a read has to wait for)
+    __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
+    __shared__ __align__(1024) char buf2[S::kAhead > 1 ? S::kBytes : 16], buf3[S::kAhead > 1 ? S::kBytes : 16];
     constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
     static_assert(!kSymmetric || TM == TN, "square tiles");
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / WAVES_N, wn = wave % WAVES_N;
@@ -274,8 +295,10 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
         while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
         tj = tile - ti * (ti + 1) / 2;
     } else {
-        ti = tile / f.tiles_n;
-        tj = tile - ti * f.tiles_n;
+        // eight rows of tiles at a time, column by column: the tiles that a die has at a time share few rows of both operands
+        const uint32_t tm = f.tiles / f.tiles_n, eights = tile / (8 * f.tiles_n), rows = min(8u, tm - eights * 8), in = tile - eights * 8 * f.tiles_n;
+        tj = in / rows;
+        ti = eights * 8 + in - tj * rows;
     }
     const uint32_t pitch_p = f.k * (PP ? 4 : 2), pitch_q = f.k * (QP ? 4 : 2);   // bytes
     const auto rows_of = [](const Half* from, uint64_t row, uint32_t pitch, int rows) {
@@ -288,29 +311,47 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
         copy_stage<TM, S::kLineP, S::kThreads>(p, from_p, pitch_p, stage * S::kLineP, to);
         copy_stage<TN, S::kLineQ, S::kThreads>(q, from_q, pitch_q, stage * S::kLineQ, to + S::kBytesP);
     };
-    const auto arrived = [] {   // this wave's copies; then everybody's
-        __builtin_amdgcn_s_waitcnt(0x0f70);
-        __syncthreads();
+    // The stage that is due has arrived, of this wave's copies and then of everybody's, and everybody has read the one before; `later` stages may
+    // still be on their way, for which __syncthreads would wait.
+    const auto arrived = [](auto later) {
+        constexpr int kMany = decltype(later)::value * S::kCopies;
+        static_assert(kMany < 64, "what the counter counts");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (kMany & 15) | (kMany >> 4 << 14));   // (copies in flight at most; no LDS access of its own)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
     const uint32_t stages = f.k / S::kStage;
-    copy(0, even);
+    const auto stage = [&](uint32_t s, char* at, char* free) {   // (past the last stage that one is copied again, so that the count stays; nobody reads it)
+        arrived(std::integral_constant<int, S::kAhead - 1>());
+        copy(min(s + S::kAhead, stages - 1), free);
+        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(at, acc, wm, wn);
+    };
+    copy(0, buf0);
     uint32_t s = 0;
-    for (; s + 1 < stages; s += 2) {
-        arrived();
-        copy(s + 1, odd);
-        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(even, acc, wm, wn);
-        arrived();
-        if (s + 2 < stages) copy(s + 2, even);
-        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(odd, acc, wm, wn);
+    if constexpr (S::kAhead == 1) {
+        for (; s + 1 < stages; s += 2) {
+            stage(s, buf0, buf1);
+            stage(s + 1, buf1, buf0);
+        }
+        if (s < stages) stage(s, buf0, buf1);
+    } else {
+        copy(min(1u, stages - 1), buf1);
+        copy(min(2u, stages - 1), buf2);
+        for (; s + 3 < stages; s += 4) {
+            stage(s, buf0, buf3);
+            stage(s + 1, buf1, buf0);
+            stage(s + 2, buf2, buf1);
+            stage(s + 3, buf3, buf2);
+        }
+        if (s < stages) stage(s, buf0, buf3);
+        if (s + 1 < stages) stage(s + 1, buf1, buf0);
+        if (s + 2 < stages) stage(s + 2, buf2, buf1);
     }
-    if (s < stages) {
-        arrived();
-        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(even, acc, wm, wn);
-    }
-    __syncthreads();
+    arrived(std::integral_constant<int, 0>());
     // 32 x 32 at a time through LDS, so that rows are written whole in both directions
     constexpr int kFits = S::kBytes / S::kBlock;
-    float* const block = reinterpret_cast<float*>((wave < kFits ? even : odd) + (wave < kFits ? wave : wave - kFits) * S::kBlock);
+    float* const block = reinterpret_cast<float*>((wave < kFits ? buf0 : buf1) + (wave < kFits ? wave : wave - kFits) * S::kBlock);
     const uint32_t i0 = ti * TM + wm * S::kWM, j0 = tj * TN + wn * S::kWN;
 #pragma unroll
     for (int bi = 0; bi < S::kBM; ++bi)
@@ -380,8 +421,8 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
     z.pair = dtype == BLINK_FP32;
-    // parts of 4096 elements, so that a part's sum costs no more than its loads
-    z.norm_parts = static_cast<uint32_t>(std::max<uint64_t>(1, std::min<uint64_t>(kNormMost, ceil_div(static_cast<uint64_t>(rows) * cols, 4096))));
+    // parts of 1024 elements at the least, four to a thread
+    z.norm_parts = static_cast<uint32_t>(std::max<uint64_t>(1, std::min<uint64_t>(kNormMost, ceil_div(static_cast<uint64_t>(rows) * cols, 1024))));
     return z;
 }
 
@@ -454,7 +495,10 @@ template <typename In, bool XP, Last LAST, typename Out>
 blink_status_t run_all(const Sizes& z, size_t batch, const Outer& o, const float* co, int steps, float eps, void* workspace, hipStream_t stream) {
     const Space s = space_of(z, batch, workspace);
     const bool tall = o.rows > o.cols;
-    BLINK_TRY(launch(ortho_norm<In>, dim3(z.norm_parts, static_cast<uint32_t>(batch)), dim3(kNormThreads), stream, o, s.parts));
+    constexpr size_t V = 16 / sizeof(float);
+    const bool wide = o.cols % V == 0 && o.in_row % V == 0 && (batch == 1 || o.in_batch % V == 0) && aligned(o.in, V * sizeof(In)) && aligned(o.momentum, 16) &&
+                      aligned(o.momentum_out, 16);
+    BLINK_TRY(launch(wide ? ortho_norm<In, V> : ortho_norm<In, 1>, dim3(z.norm_parts, static_cast<uint32_t>(batch)), dim3(kNormThreads), stream, o, s.parts));
     BLINK_TRY(launch(ortho_first<In, XP>, dim3(z.np / 64, z.mp / 64, static_cast<uint32_t>(batch)), dim3(kFirstThreads), stream, o, tall, s.parts, z.norm_parts, eps,
                      z.mp, z.np, s.x, s.xt[0]));
     if (z.tile == 256) return iterate<256, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
