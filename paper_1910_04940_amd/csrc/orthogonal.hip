@@ -194,8 +194,9 @@ struct Factors {
 
 // A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, or 64 where both operands are
 // single, so a row of a stage is 128 bytes (64 where it is single and the other is not).  Stages are copied to LDS by
-// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 64).  The eight 16-byte parts of a line lie in the order part ^
-// line % 8, so that a block's 32 rows, read part by part, fall on all banks.
+// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 64).  The sixteen 16-byte parts of 256 bytes lie in the order part ^
+// (line % 16), so that any 16 of a block's rows, read part by part, fall on all banks (in eights, 128 bytes a line: half of the LDS cycles were
+// conflicts).
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
 struct Tile {
     static constexpr int kThreads = WAVES_M * WAVES_N * 64;
@@ -211,25 +212,23 @@ struct Tile {
 
 template <int LINE>
 __device__ inline uint32_t slot_of(uint32_t row, uint32_t part) {   // byte offset of a part of a row
-    if constexpr (LINE == 128) return row * 128 + ((part ^ (row & 7)) * 16);
-    else {   // two rows to a line
-        const uint32_t line = row >> 1, at = (row & 1) * 4 + part;
-        return line * 128 + ((at ^ (line & 7)) * 16);
-    }
+    constexpr uint32_t kRows = 256 / LINE, kParts = LINE / 16;      // of 256 bytes
+    const uint32_t line = row / kRows, at = row % kRows * kParts + part;
+    return line * 256 + ((at ^ (line & 15)) * 16);
 }
 
 // Copies a stage of ROWS rows: every thread 16 bytes at a time, in the order of LDS, each from where its part is.  A thread's places
-// in the rounds are a whole number of eights of lines apart, so one offset serves them all.
+// in the rounds are a whole number of sixteens of lines apart, so one offset serves them all.
 template <int LINE>
 __device__ inline uint32_t first_offset(uint32_t pitch) {
-    const uint32_t t = threadIdx.x, line = t >> 3, slot = (t & 7) ^ (line & 7);
-    const uint32_t row = LINE == 128 ? line : line * 2 + (slot >> 2), part = LINE == 128 ? slot : slot & 3;
+    constexpr uint32_t kRows = 256 / LINE, kParts = LINE / 16;
+    const uint32_t t = threadIdx.x, line = t >> 4, at = (t & 15) ^ (line & 15), row = line * kRows + at / kParts, part = at % kParts;
     return row * pitch + part * 16;
 }
 template <int ROWS, int LINE, int THREADS>
 __device__ inline void copy_stage(__amdgpu_buffer_rsrc_t from, uint32_t offset, uint32_t pitch, uint32_t k_bytes, char* to) {
     constexpr int kTimes = ROWS * LINE / 16 / THREADS, kRows = ROWS / kTimes;   // rounds, rows of one
-    static_assert(kTimes * THREADS * 16 == ROWS * LINE && THREADS % 64 == 0, "whole rounds");
+    static_assert(kTimes * THREADS * 16 == ROWS * LINE && THREADS % 256 == 0, "whole rounds");
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int u = 0; u < kTimes; ++u)   // (a wave's lanes follow one another in LDS)
@@ -325,6 +324,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
     const auto stage = [&](uint32_t s, char* at, char* free) {   // (past the last stage that one is copied again, so that the count stays; nobody reads it)
         arrived(std::integral_constant<int, S::kAhead - 1>());
         copy(min(s + S::kAhead, stages - 1), free);
+        if constexpr (S::kAhead == 1) asm volatile("" ::: "memory");   // on their way before anything is read: the compiler would send them last
         multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(at, acc, wm, wn);
     };
     copy(0, buf0);
