@@ -73,6 +73,8 @@ _hip = None
 _call = lambda *arguments: None
 _at = dict.fromkeys(("blink_allreduce", "blink_allreduce_noalloc", "blink_broadcast", "blink_allgather", "blink_gather",
                      "blink_allreduce_op", "blink_reduce"), 0)
+# The operators likewise: name -> (the function of _blinkcall, the operator's address).
+_operators = {}
 
 
 def _load_hip_runtime() -> None:
@@ -184,6 +186,8 @@ def lib() -> C.CDLL:
         for name in _at:
             _at[name] = C.cast(getattr(L, name), vp).value
         _call = _blinkcall.call
+        for name in ("embedding", "embedding_gradient", "route", "route_loss", "route_gradient"):
+            _operators[name] = getattr(_blinkcall, name), C.cast(getattr(L, f"blink_{name}"), vp).value
     _lib = L
     return L
 

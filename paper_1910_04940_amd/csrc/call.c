@@ -1,9 +1,15 @@
-/* One collective call from Python: what binding.py would do with ctypes, in the usual case of a list of
+/* Calls from Python: what binding.py and operators.py would do with ctypes, in the usual case.
+ *
+ * A collective: a list of
  * tensors and plain integers.  A small payload takes the GPU 2 to 4 us and the C call 3; marshalling eight
  * tensors through ctypes took 1.1 us more (calls one after the other, 8 ranks x 16 KiB 4.6 us, 3.5 like this).
  *
  *   call(function, bufs, n_elems, dtype, schedule, stream[, redop]) -> status, or None where an argument is of
  *   another kind: the caller then goes through ctypes, which takes them all and reports what it does not take.
+ *
+ * An operator on tensors: reading their types, sizes and strides in Python and marshalling a dozen arguments took 4 us of a call
+ * (one row of a table 6.2 us like that, 4.0 here).  Each function takes the operator's address, the dict of the types seen so far
+ * (a tensor's dtype -> its code) and the operator's arguments in the order of operators.py; None where one is not as usual.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -77,8 +83,205 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
     return PyLong_FromLong((long)status);
 }
 
+/* ---- operators ------------------------------------------------------------------------------------------------------------ */
+static PyObject *dtype_name, *cuda_name, *shape_name, *stride_name, *contiguous_name, *numel_name;
+
+/* The usual case fails: no exception is left, and the caller goes the long way. */
+static int unusual(void) {
+    PyErr_Clear();
+    return 0;
+}
+static int attribute_is_true(PyObject* t, PyObject* name, int call) {
+    PyObject* const v = call ? PyObject_CallMethodNoArgs(t, name) : PyObject_GetAttr(t, name);
+    if (!v) return unusual();
+    const int yes = v == Py_True;
+    Py_DECREF(v);
+    return yes;
+}
+/* A tensor's address and type, if it is on the GPU. */
+static int tensor(PyObject* types, PyObject* t, void** at, long* code) {
+    PyObject* const dtype = PyObject_GetAttr(t, dtype_name);
+    if (!dtype) return unusual();
+    PyObject* const known = PyDict_GetItemWithError(types, dtype);
+    Py_DECREF(dtype);
+    if (!known) return unusual();
+    *code = PyLong_AsLong(known);
+    if (*code == -1 && PyErr_Occurred()) return unusual();
+    if (!attribute_is_true(t, cuda_name, 0)) return 0;
+    PyObject* const p = PyObject_CallMethodNoArgs(t, data_ptr_name);
+    if (!p) return unusual();
+    unsigned long long w = 0;
+    const int ok = word(p, &w);
+    Py_DECREF(p);
+    *at = (void*)w;
+    return ok;
+}
+static int pair_of(PyObject* tuple, Py_ssize_t* a, Py_ssize_t* b) {
+    int ok = 0;
+    if (tuple && PyTuple_Check(tuple) && PyTuple_GET_SIZE(tuple) == 2) {
+        *a = PyLong_AsSsize_t(PyTuple_GET_ITEM(tuple, 0));
+        *b = PyLong_AsSsize_t(PyTuple_GET_ITEM(tuple, 1));
+        ok = !PyErr_Occurred() && *a >= 0 && *b >= 0;
+    }
+    Py_XDECREF(tuple);
+    return ok ? 1 : unusual();
+}
+/* A matrix whose rows are contiguous. */
+typedef struct {
+    void* at;
+    long code;
+    Py_ssize_t rows, cols, stride;
+} matrix_t;
+static int matrix(PyObject* types, PyObject* t, matrix_t* m) {
+    Py_ssize_t one;
+    if (!tensor(types, t, &m->at, &m->code) || !pair_of(PyObject_GetAttr(t, shape_name), &m->rows, &m->cols) ||
+        !pair_of(PyObject_CallMethodNoArgs(t, stride_name), &m->stride, &one) || (m->cols > 1 && one != 1))
+        return 0;
+    if (m->rows <= 1 && m->stride < m->cols) m->stride = m->cols;
+    return 1;
+}
+/* A contiguous tensor of `elements` (any number: -1, which is then set) of that type (any of the two for tokens). */
+static int whole(PyObject* types, PyObject* t, long code, long or_code, Py_ssize_t* elements, void** at, long* is) {
+    long c;
+    if (!tensor(types, t, at, &c) || (c != code && c != or_code) || !attribute_is_true(t, contiguous_name, 1)) return 0;
+    PyObject* const n = PyObject_CallMethodNoArgs(t, numel_name);
+    if (!n) return unusual();
+    const Py_ssize_t many = PyLong_AsSsize_t(n);
+    Py_DECREF(n);
+    if (many < 0) return unusual();
+    if (*elements >= 0 && many != *elements) return 0;
+    *elements = many;
+    if (is) *is = c;
+    return 1;
+}
+/* The same with two dimensions. */
+static int table(PyObject* types, PyObject* t, long code, Py_ssize_t rows, Py_ssize_t cols, void** at) {
+    Py_ssize_t r, c, n = rows * cols;
+    return pair_of(PyObject_GetAttr(t, shape_name), &r, &c) && r == rows && c == cols && whole(types, t, code, code, &n, at, NULL);
+}
+static int space(PyObject* types, PyObject* t, void** at, Py_ssize_t* bytes) {   /* of bytes, or none */
+    *at = NULL;
+    *bytes = 0;
+    if (t == Py_None) return 1;
+    *bytes = -1;
+    return whole(types, t, -1, -1, bytes, at, NULL);
+}
+static int number(PyObject* o, float* out) {
+    if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return 0;
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) return unusual();
+    *out = (float)v;
+    return 1;
+}
+static int truth(PyObject* o, int* out) {
+    *out = o == Py_True;
+    return o == Py_True || o == Py_False;
+}
+static int small(PyObject* o, int* out) {
+    unsigned long long w;
+    if (!word(o, &w) || w > 0x7fffffff) return 0;
+    *out = (int)w;
+    return 1;
+}
+#define USUAL(condition) if (!(condition)) Py_RETURN_NONE
+#define TAKES(n)                                                          \
+    if (nargs != (n) || !PyDict_CheckExact(args[1])) Py_RETURN_NONE;      \
+    PyObject* const types = args[1];                                      \
+    unsigned long long fn, stream;                                        \
+    (void)self;                                                           \
+    USUAL(word(args[0], &fn) && fn != 0 && word(args[(n) - 1], &stream))
+#define RUN(call)                          \
+    blink_status_t status;                 \
+    Py_BEGIN_ALLOW_THREADS status = call;  \
+    Py_END_ALLOW_THREADS return PyLong_FromLong((long)status)
+
+/* table, tokens, out, scale, stream */
+static PyObject* embedding(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(7);
+    matrix_t t, o;
+    Py_ssize_t n = -1;
+    void* tokens;
+    long token;
+    float scale;
+    USUAL(matrix(types, args[2], &t) && whole(types, args[3], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[4], &o) &&
+          o.rows == n && o.cols == t.cols && number(args[5], &scale) && t.code > 0 && o.code > 0);
+    RUN(((__typeof__(&blink_embedding))fn)(t.at, (blink_dtype_t)t.code, (size_t)t.rows, (size_t)t.cols, (size_t)t.stride, tokens, (blink_dtype_t)token,
+                                           (size_t)n, scale, o.at, (blink_dtype_t)o.code, (size_t)o.stride, (void*)stream));
+}
+
+/* tokens, grad_out, grad_table, workspace, scale, accumulate, stream */
+static PyObject* embedding_gradient(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(9);
+    matrix_t g, t;
+    Py_ssize_t n = -1, size;
+    void *tokens, *work;
+    long token;
+    float scale;
+    int accumulate;
+    USUAL(whole(types, args[2], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[3], &g) && matrix(types, args[4], &t) && g.rows == n &&
+          g.cols == t.cols && space(types, args[5], &work, &size) && number(args[6], &scale) && truth(args[7], &accumulate) && t.code > 0 && g.code > 0);
+    RUN(((__typeof__(&blink_embedding_gradient))fn)(tokens, (blink_dtype_t)token, (size_t)n, g.at, (blink_dtype_t)g.code, (size_t)g.stride, scale, accumulate,
+                                                    t.at, (blink_dtype_t)t.code, (size_t)t.rows, (size_t)t.cols, (size_t)t.stride, work, (size_t)size,
+                                                    (void*)stream));
+}
+
+/* logits, k, chosen, weights, counts, sums, workspace, keep, normalize, stream */
+static PyObject* route(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(12);
+    matrix_t x;
+    Py_ssize_t size, n, e;
+    void *chosen, *weights, *counts, *sums, *work, *keep = NULL;
+    int k, normalize;
+    USUAL(matrix(types, args[2], &x) && x.code > 0 && x.cols < 0x7fffffff && small(args[3], &k));
+    n = x.rows;
+    e = x.cols + 1;
+    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && table(types, args[5], BLINK_FP32, n, k, &weights) &&
+          whole(types, args[6], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) && whole(types, args[7], BLINK_FP32, BLINK_FP32, &e, &sums, NULL) &&
+          space(types, args[8], &work, &size) && (args[9] == Py_None || whole(types, args[9], -1, -1, &n, &keep, NULL)) && truth(args[10], &normalize));
+    RUN(((__typeof__(&blink_route))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k, normalize, chosen, weights, counts,
+                                       sums, work, (size_t)size, (void*)stream));
+}
+
+/* counts, sums, k, loss, balance, z, stream */
+static PyObject* route_loss(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(9);
+    Py_ssize_t e = -1, three = 3;
+    void *counts, *sums, *loss;
+    int k;
+    float balance, z;
+    USUAL(whole(types, args[2], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) && e > 0 && e <= 0x7fffffff &&
+          whole(types, args[3], BLINK_FP32, BLINK_FP32, &e, &sums, NULL) && small(args[4], &k) &&
+          whole(types, args[5], BLINK_FP32, BLINK_FP32, &three, &loss, NULL) && number(args[6], &balance) && number(args[7], &z));
+    RUN(((__typeof__(&blink_route_loss))fn)(counts, sums, (int)(e - 1), k, balance, z, loss, (void*)stream));
+}
+
+/* logits, k, chosen, counts, grad_logits, keep, normalize, grad_weights, grad_loss, balance, z, stream */
+static PyObject* route_gradient(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(14);
+    matrix_t x, g;
+    Py_ssize_t n, e, one = 1;
+    void *chosen, *counts, *keep = NULL, *by_weight = NULL, *up = NULL;
+    int k, normalize;
+    float balance, z;
+    USUAL(matrix(types, args[2], &x) && x.code > 0 && x.cols < 0x7fffffff && small(args[3], &k) && matrix(types, args[6], &g) && g.code == x.code &&
+          g.rows == x.rows && g.cols == x.cols);
+    n = x.rows;
+    e = x.cols + 1;
+    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && whole(types, args[5], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) &&
+          (args[7] == Py_None || whole(types, args[7], -1, -1, &n, &keep, NULL)) && truth(args[8], &normalize) &&
+          (args[9] == Py_None || table(types, args[9], BLINK_FP32, n, k, &by_weight)) &&
+          (args[10] == Py_None || whole(types, args[10], BLINK_FP32, BLINK_FP32, &one, &up, NULL)) && number(args[11], &balance) && number(args[12], &z));
+    RUN(((__typeof__(&blink_route_gradient))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k, normalize, chosen, by_weight,
+                                                counts, up, balance, z, g.at, (size_t)g.stride, (void*)stream));
+}
+
 static PyMethodDef methods[] = {
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, NULL},
+    {"embedding", (PyCFunction)(void (*)(void))embedding, METH_FASTCALL, NULL},
+    {"embedding_gradient", (PyCFunction)(void (*)(void))embedding_gradient, METH_FASTCALL, NULL},
+    {"route", (PyCFunction)(void (*)(void))route, METH_FASTCALL, NULL},
+    {"route_loss", (PyCFunction)(void (*)(void))route_loss, METH_FASTCALL, NULL},
+    {"route_gradient", (PyCFunction)(void (*)(void))route_gradient, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blinkcall", NULL, 0, methods, NULL, NULL, NULL, NULL};
@@ -86,6 +289,12 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blinkcall", NULL, 0
 PyMODINIT_FUNC PyInit__blinkcall(void) {
     data_ptr_name = PyUnicode_InternFromString("data_ptr");
     address_name = PyUnicode_InternFromString("_address");
-    if (!data_ptr_name || !address_name) return NULL;
+    dtype_name = PyUnicode_InternFromString("dtype");
+    cuda_name = PyUnicode_InternFromString("is_cuda");
+    shape_name = PyUnicode_InternFromString("shape");
+    stride_name = PyUnicode_InternFromString("stride");
+    contiguous_name = PyUnicode_InternFromString("is_contiguous");
+    numel_name = PyUnicode_InternFromString("numel");
+    if (!data_ptr_name || !address_name || !dtype_name || !cuda_name || !shape_name || !stride_name || !contiguous_name || !numel_name) return NULL;
     return PyModule_Create(&module);
 }

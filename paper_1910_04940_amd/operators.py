@@ -17,6 +17,16 @@ BLINK_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
 _CODES = {"torch.float32": BLINK_FP32, "torch.bfloat16": BLINK_BF16, "torch.float16": BLINK_FP16, "torch.int32": BLINK_INT32,
           "torch.int64": BLINK_INT64, "torch.bool": -1, "torch.uint8": -1}
 _seen = {}   # a tensor's dtype -> its code, once asked
+_operators = binding._operators
+
+
+# A small operator takes the GPU 2 to 5 us, less than a wasteful call takes here: what is as usual (tensors of types seen before, plain
+# numbers) goes to the library through _blinkcall, which then returns a status; anything else, and what is not allowed, the longer way below.
+def _usual(name: str, *arguments):
+    native = _operators.get(name)
+    return None if native is None else native[0](native[1], _seen, *arguments)
+
+
 _FLOAT, _TOKEN, _BYTE, _INT32, _FP32 = (BLINK_FP32, BLINK_BF16, BLINK_FP16), (BLINK_INT32, BLINK_INT64), (-1,), (BLINK_INT32,), (BLINK_FP32,)
 
 
@@ -63,6 +73,11 @@ def _space(t) -> Tuple[Optional[int], int]:
 
 def blink_embedding(table, tokens, out, scale: float = 1.0, stream: int = 0) -> None:
     """out[i] = scale * table[tokens[i]]; zeros where the token is outside the table."""
+    status = _usual("embedding", table, tokens, out, scale, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_embedding")
     at, kind, vocab, dim, stride = _rows(table, "table", _FLOAT)
     token = _code(tokens, "tokens", _TOKEN)
     n = tokens.numel()
@@ -80,6 +95,11 @@ def blink_embedding_gradient_workspace(n_tokens: int, vocab: int, dim: int) -> i
 
 def blink_embedding_gradient(tokens, grad_out, grad_table, workspace, scale: float = 1.0, accumulate: bool = False, stream: int = 0) -> None:
     """grad_table[v] = scale * sum of grad_out[i] over the tokens that are v, added to what is there if `accumulate`."""
+    status = _usual("embedding_gradient", tokens, grad_out, grad_table, workspace, scale, accumulate, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_embedding_gradient")
     token = _code(tokens, "tokens", _TOKEN)
     n = tokens.numel()
     if not tokens.is_contiguous():
@@ -99,6 +119,11 @@ def blink_route_workspace(n_tokens: int, n_experts: int) -> int:
 
 def blink_route(logits, k: int, chosen, weights, counts, sums, workspace, keep=None, normalize: bool = False, stream: int = 0) -> None:
     """The k largest logits of every token; per-expert counts and sums of probabilities."""
+    status = _usual("route", logits, k, chosen, weights, counts, sums, workspace, keep, normalize, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route")
     at, kind, n, experts, stride = _rows(logits, "logits", _FLOAT)
     kept = None if keep is None else _whole(keep, "keep", _BYTE, (n,))
     space, size = _space(workspace)
@@ -111,6 +136,11 @@ def blink_route(logits, k: int, chosen, weights, counts, sums, workspace, keep=N
 
 def blink_route_loss(counts, sums, k: int, loss, balance: float = 0.0, z: float = 0.0, stream: int = 0) -> None:
     """loss = (both, the balance loss, the logits' loss) from counts and sums, over all ranks."""
+    status = _usual("route_loss", counts, sums, k, loss, balance, z, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route_loss")
     experts = counts.numel() - 1
     status = (binding._lib or binding.lib()).blink_route_loss(_whole(counts, "counts", _INT32, (experts + 1,)), _whole(sums, "sums", _FP32, (experts + 1,)), experts,
                                                               k, balance, z, _whole(loss, "loss", _FP32, (3,)), stream)
@@ -121,6 +151,11 @@ def blink_route_loss(counts, sums, k: int, loss, balance: float = 0.0, z: float 
 def blink_route_gradient(logits, k: int, chosen, counts, grad_logits, keep=None, normalize: bool = False, grad_weights=None, grad_loss=None,
                          balance: float = 0.0, z: float = 0.0, stream: int = 0) -> None:
     """Gradient of the logits: of the loss (times grad_loss[0]) and through the weights."""
+    status = _usual("route_gradient", logits, k, chosen, counts, grad_logits, keep, normalize, grad_weights, grad_loss, balance, z, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route_gradient")
     at, kind, n, experts, stride = _rows(logits, "logits", _FLOAT)
     to, out_kind, _, _, out_stride = _rows(grad_logits, "grad_logits", _FLOAT, n, experts)
     if out_kind != kind:
