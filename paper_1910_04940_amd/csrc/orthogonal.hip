@@ -272,43 +272,50 @@ __device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES
     }
 }
 
-// XP: X's own rows are pairs (and A's and B's).
-template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
-__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
-    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
-    // (arrays of their own, so that the compiler knows which loads a read has to wait for)
-    __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
-    __shared__ __align__(1024) char buf2[S::kAhead > 1 ? S::kBytes : 16], buf3[S::kAhead > 1 ? S::kBytes : 16];
-    constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
-    static_assert(!kSymmetric || TM == TN, "square tiles");
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / WAVES_N, wn = wave % WAVES_N;
-    // workgroups go round the eight dies in turn: each die gets a run of neighbouring tiles
-    const uint32_t per = gridDim.x >> 3, bid = blockIdx.x;
-    const uint32_t place = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
-    const uint64_t batch = place / f.tiles;
-    const uint32_t tile = place - static_cast<uint32_t>(batch) * f.tiles;
+// The tile of a product that a place in the grid stands for.
+struct Place {
+    uint64_t batch;
     uint32_t ti, tj;
-    if (kSymmetric) {   // rows of the triangle: row i has i + 1 tiles
-        ti = static_cast<uint32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
-        while (ti * (ti + 1) / 2 > tile) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
-        tj = tile - ti * (ti + 1) / 2;
+};
+template <bool SYMMETRIC>
+__device__ inline Place place_of(uint32_t place, uint32_t tiles, uint32_t tiles_n) {
+    Place r;
+    r.batch = place / tiles;
+    const uint32_t tile = place - static_cast<uint32_t>(r.batch) * tiles;
+    if (SYMMETRIC) {   // rows of the triangle: row i has i + 1 tiles
+        uint32_t i = static_cast<uint32_t>((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+        while (i * (i + 1) / 2 > tile) --i;
+        while ((i + 1) * (i + 2) / 2 <= tile) ++i;
+        r.ti = i;
+        r.tj = tile - i * (i + 1) / 2;
     } else {
         // eight rows of tiles at a time, column by column: the tiles that a die has at a time share few rows of both operands
-        const uint32_t tm = f.tiles / f.tiles_n, eights = tile / (8 * f.tiles_n), rows = min(8u, tm - eights * 8), in = tile - eights * 8 * f.tiles_n;
-        tj = in / rows;
-        ti = eights * 8 + in - tj * rows;
+        const uint32_t tm = tiles / tiles_n, eights = tile / (8 * tiles_n), rows = min(8u, tm - eights * 8), in = tile - eights * 8 * tiles_n;
+        r.tj = in / rows;
+        r.ti = eights * 8 + in - r.tj * rows;
     }
+    return r;
+}
+// Workgroups go round the eight dies in turn: each die gets a run of neighbouring places.
+__device__ inline uint32_t die_run() {
+    const uint32_t per = gridDim.x >> 3, bid = blockIdx.x;
+    return bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
+}
+
+// Adds stages [from, to) of a tile's product to acc.
+template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+__device__ inline void accumulate(const Factors& f, const Place& at, uint32_t from, uint32_t to, char* buf0, char* buf1, char* buf2, char* buf3,
+                                  Float16v (&acc)[TM / WAVES_M / 32][TN / WAVES_N / 32], int wm, int wn) {
+    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
     const uint32_t pitch_p = f.k * (PP ? 4 : 2), pitch_q = f.k * (QP ? 4 : 2);   // bytes
-    const auto rows_of = [](const Half* from, uint64_t row, uint32_t pitch, int rows) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(from)) + row * pitch, 0, rows * pitch, 0x00020000);
+    const auto rows_of = [](const Half* first, uint64_t row, uint32_t pitch, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(first)) + row * pitch, 0, rows * pitch, 0x00020000);
     };
-    const auto p = rows_of(f.p, batch * f.mp + ti * TM, pitch_p, TM), q = rows_of(f.q, batch * f.np + tj * TN, pitch_q, TN);
+    const auto p = rows_of(f.p, at.batch * f.mp + at.ti * TM, pitch_p, TM), q = rows_of(f.q, at.batch * f.np + at.tj * TN, pitch_q, TN);
     const uint32_t from_p = first_offset<S::kLineP>(pitch_p), from_q = first_offset<S::kLineQ>(pitch_q);
-    Float16v acc[S::kBM][S::kBN] = {};
-    const auto copy = [&](uint32_t stage, char* to) {
-        copy_stage<TM, S::kLineP, S::kThreads>(p, from_p, pitch_p, stage * S::kLineP, to);
-        copy_stage<TN, S::kLineQ, S::kThreads>(q, from_q, pitch_q, stage * S::kLineQ, to + S::kBytesP);
+    const auto copy = [&](uint32_t stage, char* to_buf) {
+        copy_stage<TM, S::kLineP, S::kThreads>(p, from_p, pitch_p, stage * S::kLineP, to_buf);
+        copy_stage<TN, S::kLineQ, S::kThreads>(q, from_q, pitch_q, stage * S::kLineQ, to_buf + S::kBytesP);
     };
     // The stage that is due has arrived, of this wave's copies and then of everybody's, and everybody has read the one before; `later` stages may
     // still be on their way, for which __syncthreads would wait.
@@ -320,88 +327,176 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const uint32_t stages = f.k / S::kStage;
-    const auto stage = [&](uint32_t s, char* at, char* free) {   // (past the last stage that one is copied again, so that the count stays; nobody reads it)
+    const auto stage = [&](uint32_t s, char* now, char* free) {   // (past the last stage that one is copied again, so that the count stays; nobody reads it)
         arrived(std::integral_constant<int, S::kAhead - 1>());
-        copy(min(s + S::kAhead, stages - 1), free);
+        copy(min(s + S::kAhead, to - 1), free);
         if constexpr (S::kAhead == 1) asm volatile("" ::: "memory");   // on their way before anything is read: the compiler would send them last
-        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(at, acc, wm, wn);
+        multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(now, acc, wm, wn);
     };
-    copy(0, buf0);
-    uint32_t s = 0;
+    copy(from, buf0);
+    uint32_t s = from;
     if constexpr (S::kAhead == 1) {
-        for (; s + 1 < stages; s += 2) {
+        for (; s + 1 < to; s += 2) {
             stage(s, buf0, buf1);
             stage(s + 1, buf1, buf0);
         }
-        if (s < stages) stage(s, buf0, buf1);
+        if (s < to) stage(s, buf0, buf1);
     } else {
-        copy(min(1u, stages - 1), buf1);
-        copy(min(2u, stages - 1), buf2);
-        for (; s + 3 < stages; s += 4) {
+        copy(min(from + 1, to - 1), buf1);
+        copy(min(from + 2, to - 1), buf2);
+        for (; s + 3 < to; s += 4) {
             stage(s, buf0, buf3);
             stage(s + 1, buf1, buf0);
             stage(s + 2, buf2, buf1);
             stage(s + 3, buf3, buf2);
         }
-        if (s < stages) stage(s, buf0, buf3);
-        if (s + 1 < stages) stage(s + 1, buf1, buf0);
-        if (s + 2 < stages) stage(s + 2, buf2, buf1);
+        if (s < to) stage(s, buf0, buf3);
+        if (s + 1 < to) stage(s + 1, buf1, buf0);
+        if (s + 2 < to) stage(s + 2, buf2, buf1);
     }
     arrived(std::integral_constant<int, 0>());
-    // 32 x 32 at a time through LDS, so that rows are written whole in both directions
-    constexpr int kFits = S::kBytes / S::kBlock;
-    float* const block = reinterpret_cast<float*>((wave < kFits ? buf0 : buf1) + (wave < kFits ? wave : wave - kFits) * S::kBlock);
-    const uint32_t i0 = ti * TM + wm * S::kWM, j0 = tj * TN + wn * S::kWN;
+}
+
+// Writes 32 x 32 of a product from row i and column j on, through 32 x 33 floats of LDS that are the wave's own, so that rows are written whole in both
+// directions.  mirrored: the tile has another one on the other side of the diagonal (A and B).
+template <bool XP, Product WHAT, Last LAST, typename Out>
+__device__ inline void write_block(const Factors& f, const Outer& o, bool tall, uint64_t batch, uint32_t i, uint32_t j, bool mirrored, const Float16v& acc, float* block) {
+    constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
+    const int lane = threadIdx.x & 63;
+    wave_sync();
 #pragma unroll
-    for (int bi = 0; bi < S::kBM; ++bi)
-#pragma unroll
-        for (int bj = 0; bj < S::kBN; ++bj) {
-            const uint32_t i = i0 + bi * 32, j = j0 + bj * 32;
-            wave_sync();
-#pragma unroll
-            for (int r = 0; r < 16; ++r) block[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * 33 + (lane & 31)] = acc[bi][bj][r] * f.c2;
-            wave_sync();
-            if constexpr (WHAT == kApplyLast) {
+    for (int r = 0; r < 16; ++r) block[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * 33 + (lane & 31)] = acc[r] * f.c2;
+    wave_sync();
+    if constexpr (WHAT == kApplyLast) {
 #pragma unroll 4
-                for (int u = 0; u < 16; ++u) {
-                    const uint32_t r = u * 2 + (lane >> 5), c = lane & 31;   // of the caller's matrix
-                    const float v = tall ? block[c * 33 + r] : block[r * 33 + c];
-                    const uint32_t row = (tall ? j : i) + r, col = (tall ? i : j) + c;
-                    if (row < o.rows && col < o.cols) {
-                        if constexpr (LAST == kWeights) {
-                            const uint64_t at = (batch * o.rows + row) * o.cols + col;
-                            o.weights_out[at] = __builtin_fmaf(-o.rate, v, o.keep * o.weights[at]);
-                        } else {
-                            static_cast<Out*>(o.out)[batch * o.out_batch + row * o.out_row + col] = static_cast<Out>(v);
-                        }
-                    }
-                }
-            } else {
-                const uint32_t r = lane >> 1, c = (lane & 1) * 16;
-                float v[16];
-#pragma unroll
-                for (int u = 0; u < 16; ++u) v[u] = block[r * 33 + c + u];
-                if constexpr (WHAT == kSquare) {
-                    float a[16];
-                    load16<XP>(a, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
-#pragma unroll
-                    for (int u = 0; u < 16; ++u) {
-                        v[u] = __builtin_fmaf(f.c1, a[u], v[u]) + (i + r == j + c + u ? f.c0 : 0.0f);
-                        block[r * 33 + c + u] = v[u];
-                    }
-                    wave_sync();
-                }
-                store16<XP>(f.out + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c, v);
-                // the transpose: of A and B the tile on the other side of the diagonal
-                if (!kSymmetric || ti != tj) {
-#pragma unroll
-                    for (int u = 0; u < 16; ++u) v[u] = block[(c + u) * 33 + r];
-                    if constexpr (kSymmetric) store16<XP>(f.out + (batch * f.mp + j + r) * f.np * (XP ? 2 : 1), i + c, v);
-                    else store16<true>(f.out_t + (batch * f.np + j + r) * f.mp * 2, i + c, v);
+        for (int u = 0; u < 16; ++u) {
+            const uint32_t r = u * 2 + (lane >> 5), c = lane & 31;   // of the caller's matrix
+            const float v = tall ? block[c * 33 + r] : block[r * 33 + c];
+            const uint32_t row = (tall ? j : i) + r, col = (tall ? i : j) + c;
+            if (row < o.rows && col < o.cols) {
+                if constexpr (LAST == kWeights) {
+                    const uint64_t at = (batch * o.rows + row) * o.cols + col;
+                    o.weights_out[at] = __builtin_fmaf(-o.rate, v, o.keep * o.weights[at]);
+                } else {
+                    static_cast<Out*>(o.out)[batch * o.out_batch + row * o.out_row + col] = static_cast<Out>(v);
                 }
             }
         }
+    } else {
+        const uint32_t r = lane >> 1, c = (lane & 1) * 16;
+        float v[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = block[r * 33 + c + u];
+        if constexpr (WHAT == kSquare) {
+            float a[16];
+            load16<XP>(a, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                v[u] = __builtin_fmaf(f.c1, a[u], v[u]) + (i + r == j + c + u ? f.c0 : 0.0f);
+                block[r * 33 + c + u] = v[u];
+            }
+            wave_sync();
+        }
+        store16<XP>(f.out + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c, v);
+        if (!kSymmetric || mirrored) {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = block[(c + u) * 33 + r];
+            if constexpr (kSymmetric) store16<XP>(f.out + (batch * f.mp + j + r) * f.np * (XP ? 2 : 1), i + c, v);
+            else store16<true>(f.out_t + (batch * f.np + j + r) * f.mp * 2, i + c, v);
+        }
+    }
+}
+
+// XP: X's own rows are pairs (and A's and B's).
+template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
+    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
+    // (arrays of their own, so that the compiler knows which loads a read has to wait for)
+    __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
+    __shared__ __align__(1024) char buf2[S::kAhead > 1 ? S::kBytes : 16], buf3[S::kAhead > 1 ? S::kBytes : 16];
+    constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
+    static_assert(!kSymmetric || TM == TN, "square tiles");
+    const int wave = threadIdx.x >> 6, wm = wave / WAVES_N, wn = wave % WAVES_N;
+    const Place at = place_of<kSymmetric>(die_run(), f.tiles, f.tiles_n);
+    Float16v acc[S::kBM][S::kBN] = {};
+    accumulate<TM, TN, WAVES_M, WAVES_N, PP, QP>(f, at, 0, f.k / S::kStage, buf0, buf1, buf2, buf3, acc, wm, wn);
+    constexpr int kFits = S::kBytes / S::kBlock;
+    float* const block = reinterpret_cast<float*>((wave < kFits ? buf0 : buf1) + (wave < kFits ? wave : wave - kFits) * S::kBlock);
+#pragma unroll
+    for (int bi = 0; bi < S::kBM; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < S::kBN; ++bj)
+            write_block<XP, WHAT, LAST, Out>(f, o, tall, at.batch, at.ti * TM + wm * S::kWM + bi * 32, at.tj * TN + wn * S::kWN + bj * 32, at.ti != at.tj, acc[bi][bj],
+                                             block);
+}
+
+// ---- symmetric products with fewer tiles than compute units -------------------------------------------------------------------
+// The stages of all tiles in one line, an equal run of them to every workgroup (never longer than a tile, so it touches two at most); a
+// run's sums go to the workspace in 32 bits, and a second kernel adds a tile's together in order.
+constexpr uint32_t kRuns = 256;
+constexpr size_t kPartFloats = 256 * 256;   // a run has two of them
+struct Runs {
+    float* parts;
+    uint32_t stages, tiles;   // stages of a tile, tiles of all matrices
+    __host__ __device__ uint64_t begin(uint32_t run) const { return static_cast<uint64_t>(run) * stages * tiles / kRuns; }
+};
+using Whole = Tile<256, 256, 2, 4, true, true>;
+constexpr int kPartBlocks = 64;             // of 32 x 32
+
+template <bool PP>
+__global__ __launch_bounds__(Whole::kThreads) void ortho_runs(const Factors f, const Runs runs) {
+    using S = Tile<256, 256, 2, 4, PP, PP>;
+    __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / 4, wn = wave % 4;
+    const uint32_t run = die_run();
+    uint64_t u = runs.begin(run);
+    const uint64_t end = runs.begin(run + 1);
+    for (uint32_t part = run * 2; u < end; ++part) {
+        const uint32_t tile = static_cast<uint32_t>(u / runs.stages), from = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * runs.stages);
+        const uint32_t to = static_cast<uint32_t>(min(static_cast<uint64_t>(runs.stages), from + (end - u)));
+        Float16v acc[S::kBM][S::kBN] = {};
+        accumulate<256, 256, 2, 4, PP, PP>(f, place_of<true>(tile, f.tiles, f.tiles_n), from, to, buf0, buf1, buf0, buf1, acc, wm, wn);
+        Pack<float, 4>* const out = reinterpret_cast<Pack<float, 4>*>(runs.parts + part * kPartFloats) + wave * (S::kBM * S::kBN * 256) + lane;
+#pragma unroll
+        for (int b = 0; b < S::kBM * S::kBN; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Pack<float, 4> y;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) y.v[v] = acc[b / S::kBN][b % S::kBN][r * 4 + v];
+                out[(b * 4 + r) * 64] = y;
+            }
+        u += to - from;
+    }
+}
+
+constexpr int kGatherThreads = 256;
+template <bool XP, Product WHAT>
+__global__ __launch_bounds__(kGatherThreads) void ortho_gather(const Factors f, const Runs runs) {
+    using S = Whole;
+    __shared__ float blocks[kGatherThreads / 64][32 * 33];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t tile = blockIdx.x / (kPartBlocks / (kGatherThreads / 64)), b = blockIdx.x % (kPartBlocks / (kGatherThreads / 64)) * (kGatherThreads / 64) + wave;
+    const Place at = place_of<true>(tile, f.tiles, f.tiles_n);
+    const uint64_t first = static_cast<uint64_t>(tile) * runs.stages, last = first + runs.stages - 1;
+    uint32_t run = static_cast<uint32_t>(first * kRuns / (static_cast<uint64_t>(runs.stages) * runs.tiles));
+    while (runs.begin(run) > first) --run;
+    while (runs.begin(run + 1) <= first) ++run;
+    Float16v acc = {};
+    for (; run < kRuns && runs.begin(run) <= last; ++run) {
+        if (runs.begin(run) == runs.begin(run + 1)) continue;        // (more runs than stages)
+        const uint32_t part = run * 2 + (runs.begin(run) < first);   // a run's second tile is one that it began before
+        const Pack<float, 4>* const in = reinterpret_cast<const Pack<float, 4>*>(runs.parts + part * kPartFloats) + b * 256 + lane;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const Pack<float, 4> y = in[r * 64];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[r * 4 + v] += y.v[v];
+        }
+    }
+    const uint32_t w = b / (S::kBM * S::kBN), in_wave = b % (S::kBM * S::kBN);   // in the order of ortho_runs
+    write_block<XP, WHAT, kNone, float>(f, Outer{}, false, at.batch, at.ti * 256 + w / 4 * S::kWM + in_wave / S::kBN * 32, at.tj * 256 + w % 4 * S::kWN + in_wave % S::kBN * 32,
+                                        at.ti != at.tj, acc, blocks[wave]);
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------------
@@ -426,7 +521,15 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     return z;
 }
 
+// Whether a symmetric product over k is done in runs: the compute units that its tiles leave idle gain (256 - tiles) / 256 of a tile's
+// stages at about 2 us each, the sums that go through the workspace cost about 0.13 us for each run and tile.
+bool in_runs(const Sizes& z, uint64_t batch, uint64_t k) {
+    const uint64_t side = z.mp / 256, tiles = batch * side * (side + 1) / 2, stages = k / (z.pair ? 32 : 64);
+    return z.tile == 256 && tiles <= kRuns && (kRuns - tiles) * stages > 17 * (kRuns + tiles);
+}
+
 struct Space {
+    float* sums;
     double* parts;
     Half *x, *xt[2], *a, *b;
     size_t bytes;
@@ -435,6 +538,7 @@ Space space_of(const Sizes& z, size_t batch, void* workspace) {
     Space s;
     Carve c(workspace);
     const size_t mn = batch * z.mp * z.np, mm = batch * z.mp * z.mp, one = z.pair ? 2 : 1;
+    s.sums = c.take<float>(in_runs(z, batch, z.np) ? kRuns * 2 * kPartFloats : 0);   // (if the square is, which is over fewer, so is A)
     s.parts = c.take<double>(batch * z.norm_parts);
     s.x = c.take<Half>(mn * one);
     for (Half*& t : s.xt) t = c.take<Half>(mn * 2);
@@ -458,6 +562,21 @@ blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t b
     return launch(ortho_product<T, T, kM, kN, XP, kQ, XP, WHAT, LAST, Out>, dim3(static_cast<uint32_t>(groups)), dim3(kM * kN * 64), stream, g, o, tall);
 }
 
+// A or B, of tiles of T.
+template <int T, bool XP, Product WHAT>
+blink_status_t run_symmetric(const Sizes& z, const Space& s, const Factors& f, size_t batch, hipStream_t stream) {
+    if constexpr (T == 256)
+        if (in_runs(z, batch, f.k)) {
+            Factors g = f;
+            g.tiles_n = f.mp / 256;
+            g.tiles = g.tiles_n * (g.tiles_n + 1) / 2;
+            const Runs runs{s.sums, f.k / (XP ? 32 : 64), static_cast<uint32_t>(g.tiles * batch)};
+            BLINK_TRY(launch(ortho_runs<XP>, dim3(kRuns), dim3(Whole::kThreads), stream, g, runs));
+            return launch(ortho_gather<XP, WHAT>, dim3(runs.tiles * (kPartBlocks / (kGatherThreads / 64))), dim3(kGatherThreads), stream, g, runs);
+        }
+    return run_product<T, XP, WHAT, kNone, float>(f, Outer{}, false, batch, stream);
+}
+
 template <int T, bool XP, Last LAST, typename Out>
 blink_status_t iterate(const Sizes& z, const Space& s, const Outer& o, bool tall, size_t batch, const float* co, int steps, hipStream_t stream) {
     for (int step = 0; step < steps; ++step, co += 3) {
@@ -467,14 +586,14 @@ blink_status_t iterate(const Sizes& z, const Space& s, const Outer& o, bool tall
         f.k = z.np;
         f.out = s.a;
         f.c2 = kScaleA / (kScaleX * kScaleX);
-        BLINK_TRY((run_product<T, XP, kGram, kNone, float>(f, o, tall, batch, stream)));
+        BLINK_TRY((run_symmetric<T, XP, kGram>(z, s, f, batch, stream)));
         f.p = f.q = f.a = s.a;
         f.k = z.mp;
         f.out = s.b;
         f.c0 = co[0] * kScaleB;
         f.c1 = co[1] * (kScaleB / kScaleA);
         f.c2 = co[2] * (kScaleB / (kScaleA * kScaleA));
-        BLINK_TRY((run_product<T, XP, kSquare, kNone, float>(f, o, tall, batch, stream)));
+        BLINK_TRY((run_symmetric<T, XP, kSquare>(z, s, f, batch, stream)));
         f.p = s.b;
         f.q = s.xt[step & 1];
         f.np = z.np;

@@ -81,6 +81,16 @@ def test_many_large_tiles(dtype):
         _check(_run(m), m)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(3500, 3600), (3700, 3333), (760, 16_300), (2, 2300, 2500)])
+def test_fewer_tiles_on_the_diagonals_side_than_compute_units(shape, dtype):
+    """Products whose symmetric half does not fill the GPU: their stages are dealt out in runs, some of them empty for 760 rows."""
+    m = _matrix(shape, dtype, 4)
+    got = _run(m)
+    _check(got, m)
+    assert torch.equal(got.view(torch.uint8), _run(m).view(torch.uint8))
+
+
 @pytest.mark.parametrize("scale", [1e-37, 1e-18, 1.0, 1e18, 1e36])
 def test_sizes_of_elements(scale):
     """Squares of the elements pass the range of 32-bit floats at both ends; eps is 0."""
