@@ -138,7 +138,7 @@ template <typename In, bool PAIR>
 __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool tall, const double* parts, uint32_t n_parts, float eps, uint32_t mp, uint32_t np,
                                                              Half* x, Half* xt) {
     __shared__ float tile[64][65];
-    __shared__ double factor;   // its product with an element is a 32-bit float, itself it may be past their range
+    __shared__ double wave_sum[kFirstThreads / 64];
     const int t = threadIdx.x;
     const uint64_t batch = blockIdx.z;
     const uint32_t i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
@@ -150,15 +150,12 @@ __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool
         const uint32_t r = r0 + q * 4 + t / 64, c = c0 + t % 64;
         u[q] = r < o.rows && c < o.cols ? update_at<In>(o, batch, r, c) : 0.0f;
     }
-    if (t < 64) {
-        double s = 0.0;
-        for (uint32_t p = t; p < n_parts; p += 64) s += parts[batch * n_parts + p];
-        for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-        if (t == 0) {   // a matrix of zeros, its norm and eps both 0, stays one
-            const double norm = sqrt(s) + eps;
-            factor = norm == 0.0 ? 0.0 : kScaleX / norm;
-        }
-    }
+    static_assert(kNormMost % kFirstThreads == 0, "every part once");
+    double s = 0.0;
+#pragma unroll
+    for (uint32_t p = 0; p < kNormMost; p += kFirstThreads) s += p + t < n_parts ? parts[batch * n_parts + p + t] : 0.0;
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if (t % 64 == 0) wave_sum[t / 64] = s;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
         const uint32_t r = q * 4 + t / 64, c = t % 64;
@@ -166,7 +163,10 @@ __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool
         else tile[r][c] = u[q];
     }
     __syncthreads();
-    const double f = factor;
+    double sum = 0.0;
+    for (int w = 0; w < kFirstThreads / 64; ++w) sum += wave_sum[w];
+    // a matrix of zeros, its norm and eps both 0, stays one; f may be past the range of 32-bit floats, its products with elements are in it
+    const double norm = sqrt(sum) + eps, f = norm == 0.0 ? 0.0 : kScaleX / norm;
     const uint32_t row = t / 4, col = t % 4 * 16;
     constexpr uint32_t kX = PAIR ? 2 : 1;
     float v[16];
@@ -363,36 +363,40 @@ template <bool XP, Product WHAT, Last LAST, typename Out>
 __device__ inline void write_block(const Factors& f, const Outer& o, bool tall, uint64_t batch, uint32_t i, uint32_t j, bool mirrored, const Float16v& acc, float* block) {
     constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
     const int lane = threadIdx.x & 63;
+    // what has to be read travels while the block goes through LDS
+    float old[16];
+    const uint32_t r = lane >> 1, c = (lane & 1) * 16;
+    if constexpr (WHAT == kSquare) load16<XP>(old, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
+    const uint32_t row0 = (tall ? j : i) + (lane >> 5), col = (tall ? i : j) + (lane & 31);   // of the caller's matrix
+    if constexpr (LAST == kWeights)
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+            old[u] = row0 + u * 2 < o.rows && col < o.cols ? o.weights[(batch * o.rows + row0 + u * 2) * o.cols + col] : 0.0f;
     wave_sync();
 #pragma unroll
     for (int r = 0; r < 16; ++r) block[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * 33 + (lane & 31)] = acc[r] * f.c2;
     wave_sync();
     if constexpr (WHAT == kApplyLast) {
-#pragma unroll 4
+#pragma unroll
         for (int u = 0; u < 16; ++u) {
-            const uint32_t r = u * 2 + (lane >> 5), c = lane & 31;   // of the caller's matrix
+            const uint32_t r = u * 2 + (lane >> 5), c = lane & 31, row = row0 + u * 2;
             const float v = tall ? block[c * 33 + r] : block[r * 33 + c];
-            const uint32_t row = (tall ? j : i) + r, col = (tall ? i : j) + c;
             if (row < o.rows && col < o.cols) {
                 if constexpr (LAST == kWeights) {
-                    const uint64_t at = (batch * o.rows + row) * o.cols + col;
-                    o.weights_out[at] = __builtin_fmaf(-o.rate, v, o.keep * o.weights[at]);
+                    o.weights_out[(batch * o.rows + row) * o.cols + col] = __builtin_fmaf(-o.rate, v, o.keep * old[u]);
                 } else {
                     static_cast<Out*>(o.out)[batch * o.out_batch + row * o.out_row + col] = static_cast<Out>(v);
                 }
             }
         }
     } else {
-        const uint32_t r = lane >> 1, c = (lane & 1) * 16;
         float v[16];
 #pragma unroll
         for (int u = 0; u < 16; ++u) v[u] = block[r * 33 + c + u];
         if constexpr (WHAT == kSquare) {
-            float a[16];
-            load16<XP>(a, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
 #pragma unroll
             for (int u = 0; u < 16; ++u) {
-                v[u] = __builtin_fmaf(f.c1, a[u], v[u]) + (i + r == j + c + u ? f.c0 : 0.0f);
+                v[u] = __builtin_fmaf(f.c1, old[u], v[u]) + (i + r == j + c + u ? f.c0 : 0.0f);
                 block[r * 33 + c + u] = v[u];
             }
             wave_sync();
@@ -516,8 +520,9 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
     z.pair = dtype == BLINK_FP32;
-    // parts of 1024 elements at the least, four to a thread
-    z.norm_parts = static_cast<uint32_t>(std::max<uint64_t>(1, std::min<uint64_t>(kNormMost, ceil_div(static_cast<uint64_t>(rows) * cols, 1024))));
+    // parts of 1024 elements at the least, four to a thread, and about 4096 workgroups in all at the most
+    const uint64_t parts = std::min<uint64_t>(ceil_div(static_cast<uint64_t>(rows) * cols, 1024), std::max<uint64_t>(16, 4096 / batch));
+    z.norm_parts = static_cast<uint32_t>(std::min<uint64_t>(kNormMost, parts));
     return z;
 }
 
