@@ -194,7 +194,8 @@ struct Factors {
 
 // A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, or 64 where both operands are
 // single, so a row of a stage is 128 bytes (64 where it is single and the other is not).  Stages are copied to LDS by
-// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 64).  The sixteen 16-byte parts of 256 bytes lie in the order part ^
+// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 128
+// and 64; with one ahead 2048 x 2048 took 742 us in tiles of 128, with three 663).  The sixteen 16-byte parts of 256 bytes lie in the order part ^
 // (line % 16), so that any 16 of a block's rows, read part by part, fall on all banks (in eights, 128 bytes a line: half of the LDS cycles were
 // conflicts).
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
@@ -205,7 +206,7 @@ struct Tile {
     static constexpr int kBytesP = TM * kLineP, kBytesQ = TN * kLineQ, kBytes = kBytesP + kBytesQ;
     static constexpr int kWM = TM / WAVES_M, kWN = TN / WAVES_N, kBM = kWM / 32, kBN = kWN / 32;
     static constexpr int kCopies = kBytes / 16 / kThreads;            // of a thread, for a stage
-    static constexpr int kAhead = TM <= 64 ? 3 : 1;                   // stages on their way while one is multiplied
+    static constexpr int kAhead = TM <= 128 ? 3 : 1;                  // stages on their way while one is multiplied
     static constexpr int kBlock = 32 * 33 * 4;                        // bytes of a wave's block at the end
     static_assert(WAVES_M * WAVES_N * kBlock <= 2 * kBytes, "the blocks fit the stages");
 };
@@ -510,13 +511,16 @@ struct Sizes {
     bool pair;
 };
 
-// Tiles of 256 keep the matrix instructions busiest, if there are about as many as compute units; smaller ones fill the GPU.
+// Tiles of 256 keep the matrix instructions busiest, if there are about as many as compute units (a symmetric product that has fewer is done
+// in runs); tiles of 128 if the symmetric products have half as many.  us, 32-bit, tiles of 64 / 128 / 256: 1024 x 4096 388 / 559 /
+// 702, 1536 x 1536 432 / 443 / 813, 4 of 1024 x 1024 429 / 401 / 739, 2048 x 4096 1253 / 1043 / 1237, 4096 x 4096 5735 / 4306 / 3747.
 Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     Sizes z;
     z.m = static_cast<uint32_t>(std::min(rows, cols));
     z.n = static_cast<uint32_t>(std::max(rows, cols));
     const auto tiles = [&](uint64_t t) { return batch * ceil_div(z.m, t) * ceil_div(z.n, t); };
-    z.tile = tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+    const uint64_t side = ceil_div(z.m, 128);
+    z.tile = tiles(256) >= 192 ? 256 : batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
     z.pair = dtype == BLINK_FP32;
@@ -557,7 +561,7 @@ Space space_of(const Sizes& z, size_t batch, void* workspace) {
 template <int T, bool XP, Product WHAT, Last LAST, typename Out>
 blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t batch, hipStream_t stream) {
     constexpr bool kQ = XP || WHAT == kApply || WHAT == kApplyLast;
-    constexpr int kM = 2, kN = T == 256 ? 4 : 2;
+    constexpr int kM = 2, kN = T >= 128 ? 4 : 2;
     Factors g = f;
     const uint32_t tm = f.mp / T, tn = f.np / T;
     g.tiles_n = tn;
