@@ -13,6 +13,11 @@ bool is_token(blink_dtype_t t) { return t == BLINK_INT32 || t == BLINK_INT64; }
 bool buffer_ok(const void* p, size_t elements, size_t size) { return elements == 0 || (p && blink::aligned(p, size)); }
 bool workspace_ok(const void* p, size_t has, size_t needs) { return needs == 0 || (p && has >= needs && blink::aligned(p, 256)); }
 
+// Whether matrices that are written do not overlap: one after the other, or their rows in turn.
+bool apart(size_t batch, size_t rows, size_t cols, size_t row_stride, size_t batch_stride) {
+    return batch_stride >= (rows - 1) * row_stride + cols || (batch_stride >= cols && row_stride >= (batch - 1) * batch_stride + cols);
+}
+
 }  // namespace
 
 extern "C" {
@@ -88,7 +93,7 @@ blink_status_t blink_orthogonalize(const void* matrix, blink_dtype_t dtype, size
                                    const float* coefficients, int steps, float eps, void* out, size_t out_row_stride, size_t out_batch_stride, void* workspace,
                                    size_t workspace_bytes, void* stream) {
     const size_t needs = blink_orthogonalize_workspace(batch, rows, cols, dtype);
-    if (needs == 0 || row_stride < cols || out_row_stride < cols || (batch > 1 && out_batch_stride < (rows - 1) * out_row_stride + cols) || steps < 1 ||
+    if (needs == 0 || row_stride < cols || out_row_stride < cols || (batch > 1 && !apart(batch, rows, cols, out_row_stride, out_batch_stride)) || steps < 1 ||
         steps > kMostSteps || !coefficients || !blink::coefficients_fit(coefficients, steps) || !(eps >= 0) || !std::isfinite(eps) ||
         !buffer_ok(matrix, 1, blink::size_of(dtype)) || !buffer_ok(out, 1, blink::size_of(dtype)) || !workspace_ok(workspace, workspace_bytes, needs))
         return BLINK_EINVAL;

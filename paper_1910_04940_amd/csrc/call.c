@@ -84,7 +84,7 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 /* ---- operators ------------------------------------------------------------------------------------------------------------ */
-static PyObject *dtype_name, *cuda_name, *shape_name, *stride_name, *contiguous_name, *numel_name;
+static PyObject *dtype_name, *cuda_name, *shape_name, *stride_name, *contiguous_name, *numel_name, *nbytes_name;
 
 /* The usual case fails: no exception is left, and the caller goes the long way. */
 static int unusual(void) {
@@ -98,6 +98,12 @@ static int attribute_is_true(PyObject* t, PyObject* name, int call) {
     Py_DECREF(v);
     return yes;
 }
+static int word_of(PyObject* o, unsigned long long* out) {   /* (o is given up) */
+    if (!o) return unusual();
+    const int ok = word(o, out);
+    Py_DECREF(o);
+    return ok;
+}
 /* A tensor's address and type, if it is on the GPU. */
 static int tensor(PyObject* types, PyObject* t, void** at, long* code) {
     PyObject* const dtype = PyObject_GetAttr(t, dtype_name);
@@ -108,11 +114,8 @@ static int tensor(PyObject* types, PyObject* t, void** at, long* code) {
     *code = PyLong_AsLong(known);
     if (*code == -1 && PyErr_Occurred()) return unusual();
     if (!attribute_is_true(t, cuda_name, 0)) return 0;
-    PyObject* const p = PyObject_CallMethodNoArgs(t, data_ptr_name);
-    if (!p) return unusual();
     unsigned long long w = 0;
-    const int ok = word(p, &w);
-    Py_DECREF(p);
+    const int ok = word_of(PyObject_CallMethodNoArgs(t, data_ptr_name), &w);
     *at = (void*)w;
     return ok;
 }
@@ -159,12 +162,14 @@ static int table(PyObject* types, PyObject* t, long code, Py_ssize_t rows, Py_ss
     Py_ssize_t r, c, n = rows * cols;
     return pair_of(PyObject_GetAttr(t, shape_name), &r, &c) && r == rows && c == cols && whole(types, t, code, code, &n, at, NULL);
 }
-static int space(PyObject* types, PyObject* t, void** at, Py_ssize_t* bytes) {   /* of bytes, or none */
-    *at = NULL;
-    *bytes = 0;
-    if (t == Py_None) return 1;
-    *bytes = -1;
-    return whole(types, t, -1, -1, bytes, at, NULL);
+static int space(PyObject* t, void** at, Py_ssize_t* bytes) {   /* a contiguous tensor of any type, or none */
+    unsigned long long p = 0, n = 0;
+    if (t != Py_None && !(attribute_is_true(t, cuda_name, 0) && attribute_is_true(t, contiguous_name, 1) &&
+                          word_of(PyObject_CallMethodNoArgs(t, data_ptr_name), &p) && word_of(PyObject_GetAttr(t, nbytes_name), &n)))
+        return 0;
+    *at = (void*)p;
+    *bytes = (Py_ssize_t)n;
+    return 1;
 }
 static int number(PyObject* o, float* out) {
     if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return 0;
@@ -219,7 +224,7 @@ static PyObject* embedding_gradient(PyObject* self, PyObject* const* args, Py_ss
     float scale;
     int accumulate;
     USUAL(whole(types, args[2], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[3], &g) && matrix(types, args[4], &t) && g.rows == n &&
-          g.cols == t.cols && space(types, args[5], &work, &size) && number(args[6], &scale) && truth(args[7], &accumulate) && t.code > 0 && g.code > 0);
+          g.cols == t.cols && space(args[5], &work, &size) && number(args[6], &scale) && truth(args[7], &accumulate) && t.code > 0 && g.code > 0);
     RUN(((__typeof__(&blink_embedding_gradient))fn)(tokens, (blink_dtype_t)token, (size_t)n, g.at, (blink_dtype_t)g.code, (size_t)g.stride, scale, accumulate,
                                                     t.at, (blink_dtype_t)t.code, (size_t)t.rows, (size_t)t.cols, (size_t)t.stride, work, (size_t)size,
                                                     (void*)stream));
@@ -237,7 +242,7 @@ static PyObject* route(PyObject* self, PyObject* const* args, Py_ssize_t nargs) 
     e = x.cols + 1;
     USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && table(types, args[5], BLINK_FP32, n, k, &weights) &&
           whole(types, args[6], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) && whole(types, args[7], BLINK_FP32, BLINK_FP32, &e, &sums, NULL) &&
-          space(types, args[8], &work, &size) && (args[9] == Py_None || whole(types, args[9], -1, -1, &n, &keep, NULL)) && truth(args[10], &normalize));
+          space(args[8], &work, &size) && (args[9] == Py_None || whole(types, args[9], -1, -1, &n, &keep, NULL)) && truth(args[10], &normalize));
     RUN(((__typeof__(&blink_route))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k, normalize, chosen, weights, counts,
                                        sums, work, (size_t)size, (void*)stream));
 }
@@ -295,6 +300,7 @@ PyMODINIT_FUNC PyInit__blinkcall(void) {
     stride_name = PyUnicode_InternFromString("stride");
     contiguous_name = PyUnicode_InternFromString("is_contiguous");
     numel_name = PyUnicode_InternFromString("numel");
-    if (!data_ptr_name || !address_name || !dtype_name || !cuda_name || !shape_name || !stride_name || !contiguous_name || !numel_name) return NULL;
+    nbytes_name = PyUnicode_InternFromString("nbytes");
+    if (!data_ptr_name || !address_name || !dtype_name || !cuda_name || !shape_name || !stride_name || !contiguous_name || !numel_name || !nbytes_name) return NULL;
     return PyModule_Create(&module);
 }

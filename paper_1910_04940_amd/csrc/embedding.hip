@@ -190,6 +190,7 @@ __global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* t
 
 // More tokens: at most kMostChunks chunks of whole tiles, a workgroup to each.  A pass counts the digits of every chunk, then
 // every workgroup adds up what it needs of the counts (two launches a pass; a third that scans them cost 4.5 us), and moves its items.
+// (Counting the next digits while moving, by atomics on all chunks' counts, takes longer than the launch it saves: frequent tokens share a count.)
 constexpr int kTileThreads = 512, kTileItems = 2, kTile = kTileThreads * kTileItems, kMostChunks = 256;
 static_assert(kDigits <= kTileThreads, "a thread per digit");
 
@@ -353,6 +354,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     const uint32_t last = p > 0 ? s.keys[p - 1] : kNoRow;
     const uint32_t many = __popcll(__ballot(there_is && (ALL ? p + lane + static_cast<uint64_t>(key) < d1 : p + lane < d1))), end = p + many;
     const uint32_t real = __popcll(__ballot(lane < many && key < s.vocab));   // padding comes last
+    const uint32_t next = !ALL && end < s.n ? s.keys[end] : kNoRow;             // the next stretch's first row
     const uint32_t r_end = static_cast<uint32_t>(ALL ? d1 - end : s.vocab);   // rows below it end here (ALL)
     uint32_t r = static_cast<uint32_t>(ALL ? d0 - p : __builtin_amdgcn_readfirstlane(key));
     bool begun = p > 0 && r < s.vocab && __builtin_amdgcn_readfirstlane(last) == r;   // the row has positions in an earlier stretch
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     }
     if (ALL) finish_up_to(r_end);
     if (any) {
-        if (!ALL && (end >= s.n || __builtin_amdgcn_readfirstlane(s.keys[end]) != r)) finish();
+        if (!ALL && __builtin_amdgcn_readfirstlane(next) != r) finish();
         else if (in) *reinterpret_cast<Pack<float, V>*>(s.tail + static_cast<uint64_t>(w) * s.dim_up + col) = *reinterpret_cast<Pack<float, V>*>(sum);
     }
     if (column == 0 && lane == 0) s.joined[w] = joins;

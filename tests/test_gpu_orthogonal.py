@@ -146,6 +146,13 @@ def test_views_and_in_place(dtype, tall):
     assert torch.equal(got[0], got[2])
 
 
+def test_rows_of_matrices_in_turn():
+    m = _matrix((3, 70, 90), torch.float32, 19)
+    out = torch.empty(70, 3, 90, device="cuda").permute(1, 0, 2)
+    _run(m, out)
+    assert torch.equal(out, _run(m))
+
+
 @pytest.mark.parametrize("steps", [((1.5, -0.5, 0.0),), ((1.875, -1.25, 0.375),) * 3, ((3.4445, -4.7750, 2.0315),) * 2 + ((1.5, -0.5, 0.0),) * 4])
 def test_other_coefficients(steps):
     m = _matrix((100, 140), torch.float32, 12)
