@@ -238,10 +238,10 @@ __global__ __launch_bounds__(kThreads) void route_choose(const Route a) {
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const bool keep = !a.keep || a.keep[token];
         float x[N];
-        if (keep) load_logits<T, L, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, lane, a.experts);
-        else
+        load_logits<T, L, N, V>(x, static_cast<const T*>(a.logits) + token * a.stride, lane, a.experts);   // (beside `keep`, not after it)
+        if (a.keep)
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = -kInf;
+            for (int i = 0; i < N; ++i) x[i] = keep ? x[i] : -kInf;
         K own[8], more[8];   // in order, `more` after `own`
         bool nan = false;
 #pragma unroll
@@ -439,7 +439,6 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         float x[N], d[N];
         // this lane's first choice travels with the logits
-        const bool adds = a.grad_weights && keep;
         const auto choice = [&](int j, int* e, float* g) {
             *e = j < a.k ? a.chosen[token * a.k + j] : -1;
             *g = j < a.k ? a.grad_weights[token * a.k + j] : 0.0f;
@@ -447,16 +446,16 @@ __global__ __launch_bounds__(kThreads) void route_gradient_kernel(const RouteGra
         };
         int e0 = -1;
         float g0 = 0.0f;
-        if (adds) choice(lane, &e0, &g0);
-        if (keep) load_logits<T, L, N, V>(x, row, lane, a.experts);
-        else
+        if (a.grad_weights) choice(lane, &e0, &g0);
+        load_logits<T, L, N, V>(x, row, lane, a.experts);
+        if (a.keep)
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = -kInf;
+            for (int i = 0; i < N; ++i) x[i] = keep ? x[i] : -kInf;
         float most, scale, lse;
         const bool any = softmax<L, N>(x, &most, &scale, &lse);
 #pragma unroll
         for (int i = 0; i < N; ++i) d[i] = by_p[i];
-        if (adds) {
+        if (a.grad_weights && keep) {
             // lanes of a token are lanes of one wave, whose accesses to LDS happen in order
             const auto each = [&](auto f) {
                 if (e0 >= 0) f(e0, g0);
