@@ -383,13 +383,24 @@ __global__ __launch_bounds__(kAddThreads) void route_add(const int32_t* counts, 
     count[column] = many;
 }
 
-__global__ __launch_bounds__(64) void route_loss_kernel(const int32_t* counts, const float* sums, int experts, int k, double balance, double z, float* loss) {
+constexpr int kLossThreads = 256;   // at most four experts to a thread, their loads under way together
+__global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const int32_t* counts, const float* sums, int experts, int k, double balance, double z, float* loss) {
+    __shared__ double part[kLossThreads / 64];
+    const int32_t tokens = counts[experts];
+    const float squares = sums[experts];
     double s = 0.0;
-    for (int e = threadIdx.x; e < experts; e += 64) s += static_cast<double>(counts[e]) * sums[e];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int e = u * kLossThreads + threadIdx.x;
+        if (e < experts) s += static_cast<double>(counts[e]) * sums[e];
+    }
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
     if (threadIdx.x != 0) return;
-    const double n = counts[experts];
-    const double b = n > 0 ? balance * experts / k * s / (n * n) : 0.0, l = n > 0 ? z * sums[experts] / n : 0.0;
+    for (int w = 1; w < kLossThreads / 64; ++w) s += part[w];
+    const double n = tokens;
+    const double b = n > 0 ? balance * experts / k * s / (n * n) : 0.0, l = n > 0 ? z * squares / n : 0.0;
     loss[0] = static_cast<float>(b + l);
     loss[1] = static_cast<float>(b);
     loss[2] = static_cast<float>(l);
@@ -578,7 +589,7 @@ blink_status_t route(const void* logits, blink_dtype_t dtype, size_t tokens, int
 }
 
 blink_status_t route_loss(const int32_t* counts, const float* sums, int experts, int k, float balance, float z, float* loss, hipStream_t stream) {
-    return launch(route_loss_kernel, dim3(1), dim3(64), stream, counts, sums, experts, k, static_cast<double>(balance), static_cast<double>(z), loss);
+    return launch(route_loss_kernel, dim3(1), dim3(kLossThreads), stream, counts, sums, experts, k, static_cast<double>(balance), static_cast<double>(z), loss);
 }
 
 blink_status_t route_gradient(const void* logits, blink_dtype_t dtype, size_t tokens, int experts, size_t stride, const uint8_t* keep, int k,
