@@ -24,7 +24,7 @@ constexpr int kRowThreads = 256;
 constexpr int kRowUnits = 2;   // packs of one thread, their loads under way together (131072 x 2048: 115 us, 4 packs 119, 8 121)
 
 // A pack is V elements; a row has `packs` of them.  Places go out pack by pack through all rows, so short and long rows
-// fill the waves alike.
+// fill the waves alike.  Bound by memory: 131072 rows of 2048 bfloat16 118 us, 6.8 TB/s with the table partly in the memory-side cache; one row 2.0 us.
 template <typename In, typename Out, typename Token, typename Unit, int V>
 __global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, uint64_t vocab, uint64_t table_stride, const Token* tokens,
                                                               Unit units, uint32_t packs, float scale, Out* out, uint64_t out_stride, bool past) {
@@ -110,7 +110,7 @@ __device__ inline uint32_t key_of(Token token, uint32_t vocab) {
 }
 
 // A token's place is the number of tokens that come before it.  Up to 2048 tokens are counted against one another, 64 tokens to a
-// workgroup, a part of the list to each of its waves: no passes that wait for one another (509 tokens: two passes of the next kernel 8.1 us).
+// workgroup, a part of the list to each of its waves: no passes that wait for one another (509 tokens 4.8 us, two passes of the next kernel 8.1).
 constexpr int kFewThreads = 256, kFewMost = 2048;
 template <typename Token>
 __global__ __launch_bounds__(kFewThreads) void embedding_sort_few(const Token* tokens, uint32_t n, uint32_t vocab, uint32_t* key_out, uint32_t* pos_out) {
@@ -190,6 +190,7 @@ __global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* t
 
 // More tokens: at most kMostChunks chunks of whole tiles, a workgroup to each.  A pass counts the digits of every chunk, then
 // every workgroup adds up what it needs of the counts (two launches a pass; a third that scans them cost 4.5 us), and moves its items.
+// Bound by latency: 65536 tokens, two passes of 64 chunks, 4.6 us to count and 7.4 to move each.
 // (Counting the next digits while moving, by atomics on all chunks' counts, takes longer than the launch it saves: frequent tokens share a count.)
 constexpr int kTileThreads = 512, kTileItems = 2, kTile = kTileThreads * kTileItems, kMostChunks = 256;
 static_assert(kDigits <= kTileThreads, "a thread per digit");
@@ -335,6 +336,7 @@ constexpr int kSumAhead = 8;   // rows of a sum whose loads are under way togeth
 
 // A wave: 64 V columns of the rows of its stretch, V to a lane; the next wave has the columns after them, so that a workgroup
 // writes rows in one piece.  ALL: rows that no token names are written as zeros, else (ADD too) left alone.
+// Bound by memory: 65536 rows of 1024 bfloat16 into 131072 of 32-bit floats 117 us, 5.7 TB/s; added to 5003 x 1001, 509 tokens, 7.1 us, latency.
 template <typename Grad, typename T, int V, bool ADD>
 __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     constexpr bool ALL = !ADD;
@@ -409,7 +411,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
 }
 
 // Rows that several stretches share: their sums, joined in the order of the stretches.  A wave looks at the row that ends in its
-// stretch, if one does, and adds up a few parts by itself; the waves of a workgroup share the parts of longer rows.
+// stretch, if one does, and adds up a few parts by itself; the waves of a workgroup share the parts of longer rows.  Bound by latency: 10 us
+// for a batch's gradient as above, where the most frequent token has 120 parts.
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 constexpr uint32_t kJoinAlone = 16;
 template <typename T, int V, bool ADD>

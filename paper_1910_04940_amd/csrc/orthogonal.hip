@@ -61,7 +61,7 @@ __device__ inline float update_at(const Outer& o, uint64_t batch, uint32_t r, ui
 
 // ---- the norm, and the momentum ------------------------------------------------------------------------------------------
 // A workgroup per part of a matrix; squares are added in 64 bits, where no 32-bit float's overflows or vanishes.  V neighbours to a
-// thread at a time.
+// thread at a time.  Bound by memory: a step's 8192 x 4096 of 32 bits 69 us, 5.8 TB/s.
 constexpr int kNormThreads = 256, kNormMost = 1024;
 template <typename In, int V>
 __global__ __launch_bounds__(kNormThreads) void ortho_norm(const Outer o, double* parts) {
@@ -132,7 +132,8 @@ __device__ inline void load16(float (&v)[16], const Half* row, uint32_t j) {
 }
 
 // ---- X and its transpose from U ------------------------------------------------------------------------------------------------
-// 64 x 64 of X to a workgroup.  X's own rows are pairs where PAIR, its transpose's always are.
+// 64 x 64 of X to a workgroup.  X's own rows are pairs where PAIR, its transpose's always are.  Bound by memory: 8192 x 4096 of 32 bits 136
+// us, 3.9 TB/s.
 constexpr int kFirstThreads = 256;
 template <typename In, bool PAIR>
 __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool tall, const double* parts, uint32_t n_parts, float eps, uint32_t mp, uint32_t np,
@@ -412,7 +413,9 @@ __device__ inline void write_block(const Factors& f, const Outer& o, bool tall, 
     }
 }
 
-// XP: X's own rows are pairs (and A's and B's).
+// A tile of a product to a workgroup.  XP: X's own rows are pairs (and A's and B's).  Tiles of 256 are bound by the matrix instructions at
+// the clock that power allows: B X of 8192 x 4096 pairs 670 us, 1.23 PFLOP/s of products, 71 % busy at 1.73 GHz (16-bit library product
+// of 8192 cubed 1.39); small ones by latency, 3 to 10 us.
 template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
     using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
@@ -437,7 +440,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
 
 // ---- symmetric products with fewer tiles than compute units -------------------------------------------------------------------
 // The stages of all tiles in one line, an equal run of them to every workgroup (never longer than a tile, so it touches two at most); a
-// run's sums go to the workspace in 32 bits, and a second kernel adds a tile's together in order.
+// run's sums go to the workspace in 32 bits, and a second kernel adds a tile's together in order.  136 tiles of 256 stages: 500 us a tile to
+// a workgroup, 360 + 36 in runs.
 constexpr uint32_t kRuns = 256;
 constexpr size_t kPartFloats = 256 * 256;   // a run has two of them
 struct Runs {
