@@ -152,6 +152,25 @@ def test_gradient_of_one_row_for_all_tokens_and_of_views():
     assert (whole[:, dim:] == 3.0).all()
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_a_gradient_past_32_bits(accumulate):
+    """A table of more than 2^32 elements: the rows that tokens name, and others beside them."""
+    vocab, dim, n = 1_100_000, 4096, 3000
+    table = torch.full((vocab, dim), 2.0, dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(3)
+    tokens = torch.from_numpy(np.concatenate([rng.integers(vocab - 500, vocab, n - 1000), rng.integers(0, vocab, 1000)])).cuda()
+    grad = torch.randint(-3, 4, (n, dim), device="cuda").bfloat16()
+    _gradient(tokens, grad, table, 0.5, accumulate)
+    named = torch.unique(tokens)
+    want = torch.zeros(len(named), dim, device="cuda").index_add_(0, torch.searchsorted(named, tokens), 0.5 * grad.float()) + (2.0 if accumulate else 0.0)
+    assert torch.equal(table[named].float(), want)      # small whole numbers and halves: exact
+    others = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    others[named] = False
+    for lo in range(0, vocab, 100_000):
+        part = others[lo:lo + 100_000]
+        assert (table[lo:lo + 100_000][part] == (2.0 if accumulate else 0.0)).all()
+
+
 def test_padding_keeps_nan_out():
     tokens = torch.tensor([0, -1, 2, 5, 0], device="cuda")
     grad = torch.ones(5, 8, device="cuda")

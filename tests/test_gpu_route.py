@@ -213,6 +213,20 @@ def test_views(dtype):
             assert torch.equal(getattr(run, name), getattr(plain, name))
 
 
+def test_logits_past_32_bits():
+    """More than 2^31 logits: the last tokens as they come out of a call of their own, given the same counts."""
+    t, e, k, last = 2_200_000, 1000, 2, 700
+    g = torch.Generator("cuda").manual_seed(5)
+    part = (2 * torch.randn(t // 20, e, generator=g, device="cuda")).bfloat16()
+    logits = part.repeat(20, 1)
+    run = Run(logits, k)
+    tail = Run(logits[-last:].contiguous(), k, counts=run.counts)
+    assert torch.equal(run.chosen[-last:], tail.chosen) and torch.equal(run.weights[-last:], tail.weights) and torch.equal(run.grad[-last:], tail.grad)
+    once = Run(part, k)
+    assert torch.equal(run.counts, once.counts * 20)
+    assert ((run.sums - once.sums * 20).abs() <= 2 * t / 1024 * 2.0 ** -24 * run.sums).all()     # a workgroup adds up to t / 1024 of them
+
+
 def test_ranks_add_up_to_the_whole_batch():
     """Counts and sums of four ranks, summed by the collectives, give the whole batch's loss and every rank's part of its gradient."""
     import synth_inputs as si
