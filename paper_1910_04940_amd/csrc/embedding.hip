@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kOneThreads) void embedding_sort_one(const Token* t
 
 // More tokens: at most kMostChunks chunks of whole tiles, a workgroup to each.  A pass counts the digits of every chunk, then
 // every workgroup adds up what it needs of the counts (two launches a pass; a third that scans them cost 4.5 us), and moves its items.
-// Bound by latency: 65536 tokens, two passes of 64 chunks, 4.6 us to count and 7.4 to move each.
+// Bound by latency: 65536 tokens, two passes of 64 chunks, 4.6 us to count and 6.9 to move each.
 // (Counting the next digits while moving, by atomics on all chunks' counts, takes longer than the launch it saves: frequent tokens share a count.)
 constexpr int kTileThreads = 512, kTileItems = 2, kTile = kTileThreads * kTileItems, kMostChunks = 256;
 static_assert(kDigits <= kTileThreads, "a thread per digit");
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kTileThreads) void embedding_sort_move(const Token*
     // where each digit begins: after the smaller digits of all chunks and its own of the chunks before
     uint32_t own = 0, ahead = 0;
     if (t < digits)
-#pragma unroll 16
+#pragma unroll 32
         for (uint32_t c = 0; c < gridDim.x; ++c) {
             const uint32_t many = all_counts[(c << bits) + t];
             own += many;

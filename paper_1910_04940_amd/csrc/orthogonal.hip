@@ -8,10 +8,10 @@
 //
 // Numerics.  The products run on the 16-bit matrix instructions with sums in 32 bits.  An error in A or B is relative to X and
 // stays so; one in X lies across the small singular values, which a step makes up to a times larger, so X needs more
-// bits than the result has.  X is kept as a pair of 16-bit floats, hi = round(x) and lo = round(x - hi), 22 bits together.  For a
-// 32-bit matrix so are A and B, and a product is the sum of three: hi hi + hi lo + lo hi.  Against 64 bits (1024 x
-// 1024, five steps): relative error 2e-7 like that, 1e-5 with 32-bit floats throughout.  For a 16-bit matrix, whose result is rounded to
-// 8 or 11 bits, A and B are single 16-bit floats, A from X's hi alone: 9e-4 before the rounding, where bfloat16 throughout
+// bits than the result has.  X is kept as a pair of 16-bit floats, hi = round(x) and lo = round(x - hi), 22 bits together.  For
+// matrices of 32 bits and of 16-bit floats so are A and B, and a product is the sum of three: hi hi + hi lo + lo hi.  Against 64 bits
+// (1024 x 1024, five steps): relative error 2e-7 like that, 1e-5 with 32-bit floats throughout.  For bfloat16, whose results are rounded to
+// 8 bits, 1.7e-3, A and B are single 16-bit floats, A from X's hi alone: 9e-4 before that rounding, where bfloat16 throughout
 // has 9e-3.  Everything is scaled by powers of two, so that what is stored lies in the middle of the 16-bit range.
 //
 // Layout.  All three products are sums over the contiguous index of both operands: A = X X', A A = A A', X B' with B'
@@ -527,7 +527,7 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     z.tile = tiles(256) >= 192 ? 256 : batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
-    z.pair = dtype == BLINK_FP32;
+    z.pair = dtype != BLINK_BF16;
     // parts of 1024 elements at the least, four to a thread, and about 4096 workgroups in all at the most
     const uint64_t parts = std::min<uint64_t>(ceil_div(static_cast<uint64_t>(rows) * cols, 1024), std::max<uint64_t>(16, 4096 / batch));
     z.norm_parts = static_cast<uint32_t>(std::min<uint64_t>(kNormMost, parts));
@@ -561,7 +561,7 @@ Space space_of(const Sizes& z, size_t batch, void* workspace) {
     return s;
 }
 
-// T: the tile's edge.  XP: the three factors' rows are pairs (a 32-bit matrix), else only those of X's transpose are.
+// T: the tile's edge.  XP: the three factors' rows are pairs, else only those of X's transpose are (bfloat16).
 template <int T, bool XP, Product WHAT, Last LAST, typename Out>
 blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t batch, hipStream_t stream) {
     constexpr bool kQ = XP || WHAT == kApply || WHAT == kApplyLast;
@@ -675,7 +675,7 @@ blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, 
     const Sizes z = sizes_of(batch, rows, cols, dtype);
     if (dtype == BLINK_FP32) return run_all<float, true, kMatrix, float>(z, batch, o, co, steps, eps, workspace, stream);
     if (dtype == BLINK_BF16) return run_all<__bf16, false, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream);
-    return run_all<Half, false, kMatrix, Half>(z, batch, o, co, steps, eps, workspace, stream);
+    return run_all<Half, true, kMatrix, Half>(z, batch, o, co, steps, eps, workspace, stream);
 }
 
 blink_status_t orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out, const void* grad,

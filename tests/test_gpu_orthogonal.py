@@ -98,6 +98,15 @@ def test_sizes_of_elements(scale):
     _check(_run(m, eps=0.0), m, eps=0.0)
 
 
+@pytest.mark.parametrize("shape", [(256, 300), (700, 260), (1, 900), (130, 64)])
+def test_halves_lose_nothing_but_their_rounding(shape):
+    """A 16-bit float's result is off by its own rounding, half a unit in 11 bits at the most, and by what a 32-bit matrix's is."""
+    m = _matrix(shape, torch.float16, 23)
+    want = _want(m)
+    off = float(torch.linalg.matrix_norm(_run(m).double() - want))
+    assert off <= _allowed(want, torch.float32, shape) + UNIT[torch.float16] * float(torch.linalg.matrix_norm(want))
+
+
 def test_singular_values_move_to_one():
     m = _matrix((96, 160), torch.float32, 7)
     s = torch.linalg.svdvals(_run(m).double())
