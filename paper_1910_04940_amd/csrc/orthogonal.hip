@@ -527,7 +527,9 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     z.tile = tiles(256) >= 192 ? 256 : batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
-    z.pair = dtype != BLINK_BF16;
+    // bfloat16 with few rows in pairs too: single factors' errors, 1.3 times the result's own rounding or less above that, reach 2 times at 32
+    // rows, where few numbers make up each, and there the products cost no more than their launches
+    z.pair = dtype != BLINK_BF16 || z.m < 64;
     // parts of 1024 elements at the least, four to a thread, and about 4096 workgroups in all at the most
     const uint64_t parts = std::min<uint64_t>(ceil_div(static_cast<uint64_t>(rows) * cols, 1024), std::max<uint64_t>(16, 4096 / batch));
     z.norm_parts = static_cast<uint32_t>(std::min<uint64_t>(kNormMost, parts));
@@ -674,7 +676,9 @@ blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, 
     o.out_batch = out_batch;
     const Sizes z = sizes_of(batch, rows, cols, dtype);
     if (dtype == BLINK_FP32) return run_all<float, true, kMatrix, float>(z, batch, o, co, steps, eps, workspace, stream);
-    if (dtype == BLINK_BF16) return run_all<__bf16, false, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream);
+    if (dtype == BLINK_BF16)
+        return z.pair ? run_all<__bf16, true, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream)
+                      : run_all<__bf16, false, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream);
     return run_all<Half, true, kMatrix, Half>(z, batch, o, co, steps, eps, workspace, stream);
 }
 

@@ -107,6 +107,16 @@ def test_halves_lose_nothing_but_their_rounding(shape):
     assert off <= _allowed(want, torch.float32, shape) + UNIT[torch.float16] * float(torch.linalg.matrix_norm(want))
 
 
+@pytest.mark.parametrize("shape", [(16, 900), (33, 2000), (64, 64), (3760, 32), (65, 70), (200, 333), (500, 520)])
+def test_bfloat16_is_near_its_rounding(shape):
+    """What the single factors add is below the result's own rounding, whose root mean square is its largest error over the square root of 3 at
+    most: together at most root 2 of it."""
+    m = _matrix(shape, torch.bfloat16, 29)
+    want = _want(m)
+    off = float(torch.linalg.matrix_norm(_run(m).double() - want))
+    assert off <= math.sqrt(2.0 / 3.0) * UNIT[torch.bfloat16] * float(torch.linalg.matrix_norm(want))
+
+
 def test_singular_values_move_to_one():
     m = _matrix((96, 160), torch.float32, 7)
     s = torch.linalg.svdvals(_run(m).double())
