@@ -499,7 +499,7 @@ void blink_miad_free(blink_miad_t* m);
  *   - workspace: device memory of at least the bytes that the *_workspace function returns
  *     for the call's sizes (0: none is needed, or the sizes are refused), 256-byte aligned,
  *     with any contents; the call's own until it has run.
- *   - Results are the same from call to call: no number is added by an atomic.
+ *   - Results are the same from call to call: atomics add nothing but whole numbers.
  *   - Outputs may not overlap inputs, except where "in place" is said.
  *   - Floating types are FP32, BF16, FP16; sums are formed in 32 bits or more and rounded once.
  */

@@ -37,7 +37,7 @@ def test_one_step_against_autograd():
     loss = -(own * weights).sum() / n + trainer.balance * e / 2 / n / n * (counts * p.sum(0)).sum() + trainer.z / n * (torch.logsumexp(logits, 1) ** 2).sum()
     loss.backward()
     got = trainer.step(rate=0.0).double().sum()
-    assert abs(float(got - loss)) < 1e-5
+    assert abs(float(got - loss.detach())) < 1e-5
     split = 60 * 24
     for r in range(3):
         for part, want in ((trainer.grad[r][:split].view(60, 24), table.grad), (trainer.grad[r][split:].view(24, 8), router.grad)):

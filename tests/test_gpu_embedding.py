@@ -132,6 +132,20 @@ def test_gradient(n, vocab, dim, kind, grad_type, table_type, accumulate):
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n,vocab,dim,kind", [(262_144, 3000, 8, "uneven"), (300_001, 600_000, 4, "uneven"), (550_000, 40, 8, "padded"), (9_000, 1 << 20, 4, "spread"),
+                                              (262_145, 200, 16, "one")])
+def test_gradient_of_long_lists(n, vocab, dim, kind, accumulate):
+    """Chunks of several tiles, three sorting passes, one token for all."""
+    g = torch.Generator("cuda").manual_seed(n)
+    tokens = _tokens(kind, n, vocab, 9)
+    grad = torch.randn(n, dim, generator=g, device="cuda")
+    before = torch.randn(vocab, dim, generator=g, device="cuda") if accumulate else torch.full((vocab, dim), float("nan"), device="cuda")
+    got = before.clone()
+    _gradient(tokens, grad, got, 0.5, accumulate)
+    _check(tokens, grad, before, got, 0.5, accumulate)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_without_tokens(accumulate):
     table = torch.randn(100, 24, device="cuda")
     before = table.clone()
