@@ -545,7 +545,8 @@ blink_status_t run_sums(Sums s, bool add, hipStream_t stream) {
     const uint64_t groups = ceil_div(static_cast<uint64_t>(s.stretches) * s.columns, kSumThreads / 64);
     if (groups > 0x3fffffff) return BLINK_EINVAL;
     BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, dim3(static_cast<uint32_t>(groups)), dim3(kSumThreads), stream, s));
-    if (s.n < 2 || s.stretches < 2) return BLINK_OK;   // no row lies in two stretches
+    // no row lies in two stretches: one position alone has one place, but next to that a row's end has one of its own where all rows are written
+    if (s.n < (add ? 2u : 1u) || s.stretches < 2) return BLINK_OK;
     const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kJoinWaves)), s.columns);
     return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, grid, dim3(kJoinThreads), stream, s);
 }

@@ -146,6 +146,25 @@ def test_gradient_of_long_lists(n, vocab, dim, kind, accumulate):
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("vocab,dim", [(64, 64), (300, 5), (300_000, 8)])
+def test_gradient_of_one_token(vocab, dim, accumulate):
+    """Wherever the token's row lies among the places that a wave takes (8 of them for the short tables, 32 for the long one), its
+    position and the row's end beside one another or not; and one token that is padding."""
+    grad = torch.arange(1.0, dim + 1, device="cuda").reshape(1, dim)
+    before = torch.arange(float(vocab), device="cuda")[:, None] + torch.zeros(1, dim, device="cuda") if accumulate else torch.full((vocab, dim), float("nan"), device="cuda")
+    wrong = []
+    for token in [*range(64), vocab - 2, vocab - 1, vocab, -1]:
+        got = before.clone()
+        _gradient(torch.tensor([token], device="cuda"), grad, got, 0.5, accumulate)
+        want = before.clone() if accumulate else torch.zeros(vocab, dim, device="cuda")
+        if 0 <= token < vocab:
+            want[token] = want[token] + 0.5 * grad[0]     # halves of small whole numbers: exact
+        if not torch.equal(got, want):
+            wrong.append(token)
+    assert wrong == []
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_without_tokens(accumulate):
     table = torch.randn(100, 24, device="cuda")
     before = table.clone()
