@@ -551,8 +551,8 @@ blink_status_t blink_route_gradient(const void* logits, blink_dtype_t dtype, siz
  * coefficients a, b, c (host, 3 * steps): X <- a X + (b A + c A A) X with A = X X' (of the
  * transpose where rows > cols).  EINVAL where the coefficients let singular values that
  * start in [0, 1] pass 1.95 or the polynomial a + b s^2 + c s^4 pass 7.75.  dtype: of the matrix and the
- * result.  FP32 and FP16 are computed to 32 bits' accuracy, BF16 to its own.  In place: out may be the matrix.  Matrices
- * that are written lie one after the other, or their rows in turn. */
+ * result, which is rounded to it once: for every type X, A and B are held in 22 bits and their sums in 32, with errors like those of 32-bit
+ * floats throughout.  In place: out may be the matrix.  Matrices that are written lie one after the other, or their rows in turn. */
 size_t blink_orthogonalize_workspace(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype);
 blink_status_t blink_orthogonalize(const void* matrix, blink_dtype_t dtype, size_t batch, size_t rows, size_t cols,
                                    size_t row_stride, size_t batch_stride, const float* coefficients, int steps, float eps,

@@ -6,13 +6,12 @@
 // Bound by matrix products: m^2 n + m^3 + 2 m^2 n multiplications and additions a step, A and B being symmetric: of
 // those only the tiles on and below the diagonal are computed.
 //
-// Numerics.  The products run on the 16-bit matrix instructions with sums in 32 bits.  An error in A or B is relative to X and
-// stays so; one in X lies across the small singular values, which a step makes up to a times larger, so X needs more
-// bits than the result has.  X is kept as a pair of 16-bit floats, hi = round(x) and lo = round(x - hi), 22 bits together.  For
-// matrices of 32 bits and of 16-bit floats so are A and B, and a product is the sum of three: hi hi + hi lo + lo hi.  Against 64 bits
-// (1024 x 1024, five steps): relative error 2e-7 like that, 1e-5 with 32-bit floats throughout.  For bfloat16, whose results are rounded to
-// 8 bits, 1.7e-3, A and B are single 16-bit floats, A from X's hi alone: 9e-4 before that rounding, where bfloat16 throughout
-// has 9e-3.  Everything is scaled by powers of two, so that what is stored lies in the middle of the 16-bit range.
+// Numerics.  The products run on the 16-bit matrix instructions with sums in 32 bits.  X, A and B of every type of matrix are kept as
+// pairs of 16-bit floats, hi = round(x) and lo = round(x - hi), 22 bits together, and a product is the sum of three: hi hi + hi lo + lo hi.  An
+// error in A or B is relative to X and stays so; one in X lies across the small singular values, which a step makes up to a times
+// larger.  Against 64 bits, five steps: 16 of 1024 x 1024 2.1e-6 of the result's norm, with 32-bit floats throughout 3.1e-6.  Single 16-bit A and
+// B would do for no type: 9e-4 by themselves, more than half of what rounding the result to bfloat16's 8 bits adds (1.7e-3).  Everything is scaled
+// by powers of two, so that what is stored lies in the middle of the 16-bit range.
 //
 // Layout.  All three products are sums over the contiguous index of both operands: A = X X', A A = A A', X B' with B'
 // = B, so X is kept both ways round (X for the first, its transpose for the third).  A row of pairs is a sequence of groups of 128
@@ -101,41 +100,35 @@ __global__ __launch_bounds__(kNormThreads) void ortho_norm(const Outer o, double
 
 // ---- 16-bit storage ----------------------------------------------------------------------------------------------------------
 // Sixteen values of a row from column j (a multiple of 16) on.
-template <bool PAIR>
 __device__ inline void store16(Half* row, uint32_t j, const float (&v)[16]) {
     Half8 h[2], l[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const Half hi = static_cast<Half>(v[i]);
         h[i / 8][i % 8] = hi;
-        if (PAIR) l[i / 8][i % 8] = static_cast<Half>(v[i] - static_cast<float>(hi));
+        l[i / 8][i % 8] = static_cast<Half>(v[i] - static_cast<float>(hi));
     }
-    Half* const at = PAIR ? row + (j >> 5) * 64 + (j & 31) : row + j;
+    Half* const at = row + (j >> 5) * 64 + (j & 31);
     *reinterpret_cast<Half8*>(at) = h[0];
     *reinterpret_cast<Half8*>(at + 8) = h[1];
-    if (PAIR) {
-        *reinterpret_cast<Half8*>(at + 32) = l[0];
-        *reinterpret_cast<Half8*>(at + 40) = l[1];
-    }
+    *reinterpret_cast<Half8*>(at + 32) = l[0];
+    *reinterpret_cast<Half8*>(at + 40) = l[1];
 }
-template <bool PAIR>
 __device__ inline void load16(float (&v)[16], const Half* row, uint32_t j) {
-    const Half* const at = PAIR ? row + (j >> 5) * 64 + (j & 31) : row + j;
+    const Half* const at = row + (j >> 5) * 64 + (j & 31);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const Half8 h = *reinterpret_cast<const Half8*>(at + 8 * q);
-        Half8 l = {};
-        if (PAIR) l = *reinterpret_cast<const Half8*>(at + 32 + 8 * q);
+        const Half8 h = *reinterpret_cast<const Half8*>(at + 8 * q), l = *reinterpret_cast<const Half8*>(at + 32 + 8 * q);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * q + i] = static_cast<float>(h[i]) + (PAIR ? static_cast<float>(l[i]) : 0.0f);
+        for (int i = 0; i < 8; ++i) v[8 * q + i] = static_cast<float>(h[i]) + static_cast<float>(l[i]);
     }
 }
 
 // ---- X and its transpose from U ------------------------------------------------------------------------------------------------
-// 64 x 64 of X to a workgroup.  X's own rows are pairs where PAIR, its transpose's always are.  Bound by memory: 8192 x 4096 of 32 bits 136
+// 64 x 64 of X to a workgroup.  Bound by memory: 8192 x 4096 of 32 bits 136
 // us, 3.9 TB/s.
 constexpr int kFirstThreads = 256;
-template <typename In, bool PAIR>
+template <typename In>
 __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool tall, const double* parts, uint32_t n_parts, float eps, uint32_t mp, uint32_t np,
                                                              Half* x, Half* xt) {
     __shared__ float tile[64][65];
@@ -169,14 +162,13 @@ __global__ __launch_bounds__(kFirstThreads) void ortho_first(const Outer o, bool
     // a matrix of zeros, its norm and eps both 0, stays one; f may be past the range of 32-bit floats, its products with elements are in it
     const double norm = sqrt(sum) + eps, f = norm == 0.0 ? 0.0 : kScaleX / norm;
     const uint32_t row = t / 4, col = t % 4 * 16;
-    constexpr uint32_t kX = PAIR ? 2 : 1;
     float v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(tile[row][col + i] * f);
-    store16<PAIR>(x + (batch * mp + i0 + row) * np * kX, j0 + col, v);
+    store16(x + (batch * mp + i0 + row) * np * 2, j0 + col, v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(tile[col + i][row] * f);
-    store16<true>(xt + (batch * np + j0 + row) * mp * 2, i0 + col, v);
+    store16(xt + (batch * np + j0 + row) * mp * 2, i0 + col, v);
 }
 
 // ---- the products --------------------------------------------------------------------------------------------------------------
@@ -193,18 +185,17 @@ struct Factors {
     uint32_t part;         // stages of a part of a long sum (tiles of 128 and 64)
 };
 
-// A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, or 64 where both operands are
-// single, so a row of a stage is 128 bytes (64 where it is single and the other is not).  Stages are copied to LDS by
-// the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 128
+// A workgroup's tile is TM x TN, its waves' WM x WN of 32 x 32 blocks each; a stage is 32 of k, a row of it 128 bytes.  Stages are copied to
+// LDS by the loads themselves, one ahead of the stage that is multiplied, three where a stage takes less time than its copy (tiles of 128
 // and 64; with one ahead 2048 x 2048 took 742 us in tiles of 128, with three 663).  The sixteen 16-byte parts of 256 bytes lie in the order part ^
 // (line % 16), so that any 16 of a block's rows, read part by part, fall on all banks (in eights, 128 bytes a line: half of the LDS cycles were
 // conflicts).
-template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+constexpr int kStage = 32;   // of k
+constexpr int kLine = 128;   // bytes of a row's stage
+template <int TM, int TN, int WAVES_M, int WAVES_N>
 struct Tile {
     static constexpr int kThreads = WAVES_M * WAVES_N * 64;
-    static constexpr int kStage = PP || QP ? 32 : 64;                 // of k
-    static constexpr int kLineP = PP == QP || PP ? 128 : 64, kLineQ = PP == QP || QP ? 128 : 64;   // bytes of a row's stage
-    static constexpr int kBytesP = TM * kLineP, kBytesQ = TN * kLineQ, kBytes = kBytesP + kBytesQ;
+    static constexpr int kBytesP = TM * kLine, kBytes = kBytesP + TN * kLine;
     static constexpr int kWM = TM / WAVES_M, kWN = TN / WAVES_N, kBM = kWM / 32, kBN = kWN / 32;
     static constexpr int kCopies = kBytes / 16 / kThreads;            // of a thread, for a stage
     static constexpr int kAhead = TM <= 128 ? 3 : 1;                  // stages on their way while one is multiplied
@@ -212,54 +203,51 @@ struct Tile {
     static_assert(WAVES_M * WAVES_N * kBlock <= 2 * kBytes, "the blocks fit the stages");
 };
 
-template <int LINE>
+constexpr uint32_t kRows = 256 / kLine, kParts = kLine / 16;        // of 256 bytes; of a row
 __device__ inline uint32_t slot_of(uint32_t row, uint32_t part) {   // byte offset of a part of a row
-    constexpr uint32_t kRows = 256 / LINE, kParts = LINE / 16;      // of 256 bytes
     const uint32_t line = row / kRows, at = row % kRows * kParts + part;
     return line * 256 + ((at ^ (line & 15)) * 16);
 }
 
 // Copies a stage of ROWS rows: every thread 16 bytes at a time, in the order of LDS, each from where its part is.  A thread's places
 // in the rounds are a whole number of sixteens of lines apart, so one offset serves them all.
-template <int LINE>
 __device__ inline uint32_t first_offset(uint32_t pitch) {
-    constexpr uint32_t kRows = 256 / LINE, kParts = LINE / 16;
     const uint32_t t = threadIdx.x, line = t >> 4, at = (t & 15) ^ (line & 15), row = line * kRows + at / kParts, part = at % kParts;
     return row * pitch + part * 16;
 }
-template <int ROWS, int LINE, int THREADS>
+template <int ROWS, int THREADS>
 __device__ inline void copy_stage(__amdgpu_buffer_rsrc_t from, uint32_t offset, uint32_t pitch, uint32_t k_bytes, char* to) {
-    constexpr int kTimes = ROWS * LINE / 16 / THREADS, kRows = ROWS / kTimes;   // rounds, rows of one
-    static_assert(kTimes * THREADS * 16 == ROWS * LINE && THREADS % 256 == 0, "whole rounds");
+    constexpr int kTimes = ROWS * kLine / 16 / THREADS, kRound = ROWS / kTimes;   // rounds, rows of one
+    static_assert(kTimes * THREADS * 16 == ROWS * kLine && THREADS % 256 == 0, "whole rounds");
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int u = 0; u < kTimes; ++u)   // (a wave's lanes follow one another in LDS)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (u * THREADS + wave * 64) * 16), 16, offset,
-                                                 k_bytes + u * kRows * pitch, 0, 0);
+                                                 k_bytes + u * kRound * pitch, 0, 0);
 }
 
-template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+template <int TM, int TN, int WAVES_M, int WAVES_N>
 __device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES_M / 32][TN / WAVES_N / 32],
                                       Float16v (&low)[TM / WAVES_M / 32][TN / WAVES_N / 32], int wm, int wn) {
-    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
+    using S = Tile<TM, TN, WAVES_M, WAVES_N>;
     const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
     const char* const p = at;
     const char* const q = at + S::kBytesP;
 #pragma unroll
-    for (int ks = 0; ks < S::kStage / 16; ++ks) {   // 16 of k: two parts of 8
+    for (int ks = 0; ks < kStage / 16; ++ks) {   // 16 of k: two parts of 8
         const uint32_t part = ks * 2 + half;
         Half8 ph[S::kBM], pl[S::kBM], qh[S::kBN], ql[S::kBN];
 #pragma unroll
         for (int i = 0; i < S::kBM; ++i) {
             const uint32_t r = wm * S::kWM + i * 32 + row;
-            ph[i] = *reinterpret_cast<const Half8*>(p + slot_of<S::kLineP>(r, part));
-            if (PP) pl[i] = *reinterpret_cast<const Half8*>(p + slot_of<S::kLineP>(r, part + 4));
+            ph[i] = *reinterpret_cast<const Half8*>(p + slot_of(r, part));
+            pl[i] = *reinterpret_cast<const Half8*>(p + slot_of(r, part + 4));
         }
 #pragma unroll
         for (int j = 0; j < S::kBN; ++j) {
             const uint32_t r = wn * S::kWN + j * 32 + row;
-            qh[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part));
-            if (QP) ql[j] = *reinterpret_cast<const Half8*>(q + slot_of<S::kLineQ>(r, part + 4));
+            qh[j] = *reinterpret_cast<const Half8*>(q + slot_of(r, part));
+            ql[j] = *reinterpret_cast<const Half8*>(q + slot_of(r, part + 4));
         }
         // the same sums again only after all the others
 #pragma unroll
@@ -268,8 +256,8 @@ __device__ inline void multiply_stage(const char* at, Float16v (&acc)[TM / WAVES
             for (int i = 0; i < S::kBM; ++i)
 #pragma unroll
                 for (int j = 0; j < S::kBN; ++j) {
-                    if (QP && term == 0) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], low[i][j], 0, 0, 0);
-                    if (PP && term == 1) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], low[i][j], 0, 0, 0);
+                    if (term == 0) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], low[i][j], 0, 0, 0);
+                    if (term == 1) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], low[i][j], 0, 0, 0);
                     if (term == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
                 }
     }
@@ -306,19 +294,19 @@ __device__ inline uint32_t die_run() {
 }
 
 // Adds stages [from, to) of a tile's product to acc.
-template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP>
+template <int TM, int TN, int WAVES_M, int WAVES_N>
 __device__ inline void accumulate(const Factors& f, const Place& at, uint32_t from, uint32_t to, char* buf0, char* buf1, char* buf2, char* buf3,
                                   Float16v (&acc)[TM / WAVES_M / 32][TN / WAVES_N / 32], int wm, int wn) {
-    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
-    const uint32_t pitch_p = f.k * (PP ? 4 : 2), pitch_q = f.k * (QP ? 4 : 2);   // bytes
-    const auto rows_of = [](const Half* first, uint64_t row, uint32_t pitch, int rows) {
+    using S = Tile<TM, TN, WAVES_M, WAVES_N>;
+    const uint32_t pitch = f.k * 4;   // bytes of a row of pairs
+    const auto rows_of = [pitch](const Half* first, uint64_t row, int rows) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(first)) + row * pitch, 0, rows * pitch, 0x00020000);
     };
-    const auto p = rows_of(f.p, at.batch * f.mp + at.ti * TM, pitch_p, TM), q = rows_of(f.q, at.batch * f.np + at.tj * TN, pitch_q, TN);
-    const uint32_t from_p = first_offset<S::kLineP>(pitch_p), from_q = first_offset<S::kLineQ>(pitch_q);
+    const auto p = rows_of(f.p, at.batch * f.mp + at.ti * TM, TM), q = rows_of(f.q, at.batch * f.np + at.tj * TN, TN);
+    const uint32_t offset = first_offset(pitch);
     const auto copy = [&](uint32_t stage, char* to_buf) {
-        copy_stage<TM, S::kLineP, S::kThreads>(p, from_p, pitch_p, stage * S::kLineP, to_buf);
-        copy_stage<TN, S::kLineQ, S::kThreads>(q, from_q, pitch_q, stage * S::kLineQ, to_buf + S::kBytesP);
+        copy_stage<TM, S::kThreads>(p, offset, pitch, stage * kLine, to_buf);
+        copy_stage<TN, S::kThreads>(q, offset, pitch, stage * kLine, to_buf + S::kBytesP);
     };
     // The stage that is due has arrived, of this wave's copies and then of everybody's, and everybody has read the one before; `later` stages may
     // still be on their way, for which __syncthreads would wait.
@@ -338,9 +326,9 @@ __device__ inline void accumulate(const Factors& f, const Place& at, uint32_t fr
         copy(min(s + S::kAhead, to - 1), free);
         if constexpr (S::kAhead == 1) {
             asm volatile("" ::: "memory");   // on their way before anything is read: the compiler would send them last
-            multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(now, acc, acc, wm, wn);
+            multiply_stage<TM, TN, WAVES_M, WAVES_N>(now, acc, acc, wm, wn);
         } else
-            multiply_stage<TM, TN, WAVES_M, WAVES_N, PP, QP>(now, acc, low, wm, wn);
+            multiply_stage<TM, TN, WAVES_M, WAVES_N>(now, acc, low, wm, wn);
     };
     copy(from, buf0);
     uint32_t s = from;
@@ -362,23 +350,22 @@ __device__ inline void accumulate(const Factors& f, const Place& at, uint32_t fr
         if (s < to) stage(s, buf0, buf3);
         if (s + 1 < to) stage(s + 1, buf1, buf0);
         if (s + 2 < to) stage(s + 2, buf2, buf1);
-        if constexpr (PP || QP)
 #pragma unroll
-            for (int b = 0; b < S::kBM * S::kBN; ++b) acc[b / S::kBN][b % S::kBN] += low[b / S::kBN][b % S::kBN];
+        for (int b = 0; b < S::kBM * S::kBN; ++b) acc[b / S::kBN][b % S::kBN] += low[b / S::kBN][b % S::kBN];
     }
     arrived(std::integral_constant<int, 0>());
 }
 
 // Writes 32 x 32 of a product from row i and column j on, through 32 x 33 floats of LDS that are the wave's own, so that rows are written whole in both
 // directions.  mirrored: the tile has another one on the other side of the diagonal (A and B).
-template <bool XP, Product WHAT, Last LAST, typename Out>
+template <Product WHAT, Last LAST, typename Out>
 __device__ inline void write_block(const Factors& f, const Outer& o, bool tall, uint64_t batch, uint32_t i, uint32_t j, bool mirrored, const Float16v& acc, float* block) {
     constexpr bool kSymmetric = WHAT == kGram || WHAT == kSquare;
     const int lane = threadIdx.x & 63;
     // what has to be read travels while the block goes through LDS
     float old[16];
     const uint32_t r = lane >> 1, c = (lane & 1) * 16;
-    if constexpr (WHAT == kSquare) load16<XP>(old, f.a + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c);
+    if constexpr (WHAT == kSquare) load16(old, f.a + (batch * f.mp + i + r) * f.np * 2, j + c);
     const uint32_t row0 = (tall ? j : i) + (lane >> 5), col = (tall ? i : j) + (lane & 31);   // of the caller's matrix
     if constexpr (LAST == kWeights)
 #pragma unroll
@@ -413,22 +400,22 @@ __device__ inline void write_block(const Factors& f, const Outer& o, bool tall, 
             }
             wave_sync();
         }
-        store16<XP>(f.out + (batch * f.mp + i + r) * f.np * (XP ? 2 : 1), j + c, v);
+        store16(f.out + (batch * f.mp + i + r) * f.np * 2, j + c, v);
         if (!kSymmetric || mirrored) {
 #pragma unroll
             for (int u = 0; u < 16; ++u) v[u] = block[(c + u) * 33 + r];
-            if constexpr (kSymmetric) store16<XP>(f.out + (batch * f.mp + j + r) * f.np * (XP ? 2 : 1), i + c, v);
-            else store16<true>(f.out_t + (batch * f.np + j + r) * f.mp * 2, i + c, v);
+            if constexpr (kSymmetric) store16(f.out + (batch * f.mp + j + r) * f.np * 2, i + c, v);
+            else store16(f.out_t + (batch * f.np + j + r) * f.mp * 2, i + c, v);
         }
     }
 }
 
-// A tile of a product to a workgroup.  XP: X's own rows are pairs (and A's and B's).  Tiles of 256 are bound by the matrix instructions at
+// A tile of a product to a workgroup.  Tiles of 256 are bound by the matrix instructions at
 // the clock that power allows: B X of 8192 x 4096 pairs 670 us, 1.23 PFLOP/s of products, 71 % busy at 1.73 GHz (16-bit library product
 // of 8192 cubed 1.39); small ones by latency, 3 to 10 us.
-template <int TM, int TN, int WAVES_M, int WAVES_N, bool PP, bool QP, bool XP, Product WHAT, Last LAST, typename Out>
+template <int TM, int TN, int WAVES_M, int WAVES_N, Product WHAT, Last LAST, typename Out>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {
-    using S = Tile<TM, TN, WAVES_M, WAVES_N, PP, QP>;
+    using S = Tile<TM, TN, WAVES_M, WAVES_N>;
     // (arrays of their own, so that the compiler knows which loads a read has to wait for)
     __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
     __shared__ __align__(1024) char buf2[S::kAhead > 1 ? S::kBytes : 16], buf3[S::kAhead > 1 ? S::kBytes : 16];
@@ -437,12 +424,12 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
     const int wave = threadIdx.x >> 6, wm = wave / WAVES_N, wn = wave % WAVES_N;
     const Place at = place_of<kSymmetric>(die_run(), f.tiles, f.tiles_n);
     Float16v acc[S::kBM][S::kBN] = {};
-    const uint32_t stages = f.k / S::kStage;
-    accumulate<TM, TN, WAVES_M, WAVES_N, PP, QP>(f, at, 0, S::kAhead == 1 ? stages : min(f.part, stages), buf0, buf1, buf2, buf3, acc, wm, wn);
+    const uint32_t stages = f.k / kStage;
+    accumulate<TM, TN, WAVES_M, WAVES_N>(f, at, 0, S::kAhead == 1 ? stages : min(f.part, stages), buf0, buf1, buf2, buf3, acc, wm, wn);
     if constexpr (S::kAhead > 1)   // (parts of a long sum, as `low` is one)
         for (uint32_t from = f.part; from < stages; from += f.part) {
             Float16v part[S::kBM][S::kBN] = {};
-            accumulate<TM, TN, WAVES_M, WAVES_N, PP, QP>(f, at, from, min(from + f.part, stages), buf0, buf1, buf2, buf3, part, wm, wn);
+            accumulate<TM, TN, WAVES_M, WAVES_N>(f, at, from, min(from + f.part, stages), buf0, buf1, buf2, buf3, part, wm, wn);
 #pragma unroll
             for (int b = 0; b < S::kBM * S::kBN; ++b) acc[b / S::kBN][b % S::kBN] += part[b / S::kBN][b % S::kBN];
         }
@@ -452,7 +439,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Fa
     for (int bi = 0; bi < S::kBM; ++bi)
 #pragma unroll
         for (int bj = 0; bj < S::kBN; ++bj)
-            write_block<XP, WHAT, LAST, Out>(f, o, tall, at.batch, at.ti * TM + wm * S::kWM + bi * 32, at.tj * TN + wn * S::kWN + bj * 32, at.ti != at.tj, acc[bi][bj],
+            write_block<WHAT, LAST, Out>(f, o, tall, at.batch, at.ti * TM + wm * S::kWM + bi * 32, at.tj * TN + wn * S::kWN + bj * 32, at.ti != at.tj, acc[bi][bj],
                                              block);
 }
 
@@ -467,12 +454,11 @@ struct Runs {
     uint32_t stages, tiles;   // stages of a tile, tiles of all matrices
     __host__ __device__ uint64_t begin(uint32_t run) const { return static_cast<uint64_t>(run) * stages * tiles / kRuns; }
 };
-using Whole = Tile<256, 256, 2, 4, true, true>;
+using Whole = Tile<256, 256, 2, 4>;
 constexpr int kPartBlocks = 64;             // of 32 x 32
 
-template <bool PP>
 __global__ __launch_bounds__(Whole::kThreads) void ortho_runs(const Factors f, const Runs runs) {
-    using S = Tile<256, 256, 2, 4, PP, PP>;
+    using S = Whole;
     __shared__ __align__(1024) char buf0[S::kBytes], buf1[S::kBytes];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave / 4, wn = wave % 4;
     const uint32_t run = die_run();
@@ -482,7 +468,7 @@ __global__ __launch_bounds__(Whole::kThreads) void ortho_runs(const Factors f, c
         const uint32_t tile = static_cast<uint32_t>(u / runs.stages), from = static_cast<uint32_t>(u - static_cast<uint64_t>(tile) * runs.stages);
         const uint32_t to = static_cast<uint32_t>(min(static_cast<uint64_t>(runs.stages), from + (end - u)));
         Float16v acc[S::kBM][S::kBN] = {};
-        accumulate<256, 256, 2, 4, PP, PP>(f, place_of<true>(tile, f.tiles, f.tiles_n), from, to, buf0, buf1, buf0, buf1, acc, wm, wn);
+        accumulate<256, 256, 2, 4>(f, place_of<true>(tile, f.tiles, f.tiles_n), from, to, buf0, buf1, buf0, buf1, acc, wm, wn);
         Pack<float, 4>* const out = reinterpret_cast<Pack<float, 4>*>(runs.parts + part * kPartFloats) + wave * (S::kBM * S::kBN * 256) + lane;
 #pragma unroll
         for (int b = 0; b < S::kBM * S::kBN; ++b)
@@ -498,7 +484,7 @@ __global__ __launch_bounds__(Whole::kThreads) void ortho_runs(const Factors f, c
 }
 
 constexpr int kGatherThreads = 256;
-template <bool XP, Product WHAT>
+template <Product WHAT>
 __global__ __launch_bounds__(kGatherThreads) void ortho_gather(const Factors f, const Runs runs) {
     using S = Whole;
     __shared__ float blocks[kGatherThreads / 64][32 * 33];
@@ -522,7 +508,7 @@ __global__ __launch_bounds__(kGatherThreads) void ortho_gather(const Factors f, 
         }
     }
     const uint32_t w = b / (S::kBM * S::kBN), in_wave = b % (S::kBM * S::kBN);   // in the order of ortho_runs
-    write_block<XP, WHAT, kNone, float>(f, Outer{}, false, at.batch, at.ti * 256 + w / 4 * S::kWM + in_wave / S::kBN * 32, at.tj * 256 + w % 4 * S::kWN + in_wave % S::kBN * 32,
+    write_block<WHAT, kNone, float>(f, Outer{}, false, at.batch, at.ti * 256 + w / 4 * S::kWM + in_wave / S::kBN * 32, at.tj * 256 + w % 4 * S::kWN + in_wave % S::kBN * 32,
                                         at.ti != at.tj, acc, blocks[wave]);
 }
 
@@ -530,13 +516,12 @@ __global__ __launch_bounds__(kGatherThreads) void ortho_gather(const Factors f, 
 struct Sizes {
     uint32_t m, n, mp, np, tile;
     uint32_t norm_parts;
-    bool pair;
 };
 
 // Tiles of 256 keep the matrix instructions busiest, if there are about as many as compute units (a symmetric product that has fewer is done
 // in runs); tiles of 128 if the symmetric products have half as many.  us, 32-bit, tiles of 64 / 128 / 256: 1024 x 4096 388 / 559 /
 // 702, 1536 x 1536 432 / 443 / 813, 4 of 1024 x 1024 429 / 401 / 739, 2048 x 4096 1253 / 1043 / 1237, 4096 x 4096 5735 / 4306 / 3747.
-Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
+Sizes sizes_of(size_t batch, size_t rows, size_t cols) {
     Sizes z;
     z.m = static_cast<uint32_t>(std::min(rows, cols));
     z.n = static_cast<uint32_t>(std::max(rows, cols));
@@ -545,9 +530,6 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
     z.tile = tiles(256) >= 192 ? 256 : batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
-    // bfloat16 with few rows in pairs too: single factors' errors, 1.3 times the result's own rounding or less above that, reach 2 times at 32
-    // rows, where few numbers make up each, and there the products cost no more than their launches
-    z.pair = dtype != BLINK_BF16 || z.m < 64;
     // parts of 1024 elements at the least, four to a thread, and about 4096 workgroups in all at the most
     const uint64_t parts = std::min<uint64_t>(ceil_div(static_cast<uint64_t>(rows) * cols, 1024), std::max<uint64_t>(16, 4096 / batch));
     z.norm_parts = static_cast<uint32_t>(std::min<uint64_t>(kNormMost, parts));
@@ -557,34 +539,35 @@ Sizes sizes_of(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
 // Whether a symmetric product over k is done in runs: the compute units that its tiles leave idle gain (256 - tiles) / 256 of a tile's
 // stages at about 2 us each, the sums that go through the workspace cost about 0.13 us for each run and tile.
 bool in_runs(const Sizes& z, uint64_t batch, uint64_t k) {
-    const uint64_t side = z.mp / 256, tiles = batch * side * (side + 1) / 2, stages = k / (z.pair ? 32 : 64);
+    const uint64_t side = z.mp / 256, tiles = batch * side * (side + 1) / 2, stages = k / kStage;
     return z.tile == 256 && tiles <= kRuns && (kRuns - tiles) * stages > 17 * (kRuns + tiles);
 }
 
 struct Space {
     float* sums;
     double* parts;
-    Half *x, *xt[2], *a, *b;
+    Half *x, *xt[2], *a, *b;   // a null: shared
     size_t bytes;
 };
-Space space_of(const Sizes& z, size_t batch, void* workspace) {
+// A of 16-bit matrices lies in the copy of X' that the step has yet to write and nobody reads any more: A is not needed once B is there, and
+// mp <= np.  That takes back from their workspace most of what pairs cost it.
+Space space_of(const Sizes& z, size_t batch, bool shared, void* workspace) {
     Space s;
     Carve c(workspace);
-    const size_t mn = batch * z.mp * z.np, mm = batch * z.mp * z.mp, one = z.pair ? 2 : 1;
+    const size_t mn = batch * z.mp * z.np * 2, mm = batch * z.mp * z.mp * 2;
     s.sums = c.take<float>(in_runs(z, batch, z.np) ? kRuns * 2 * kPartFloats : 0);   // (if the square is, which is over fewer, so is A)
     s.parts = c.take<double>(batch * z.norm_parts);
-    s.x = c.take<Half>(mn * one);
-    for (Half*& t : s.xt) t = c.take<Half>(mn * 2);
-    s.a = c.take<Half>(mm * one);
-    s.b = c.take<Half>(mm * one);
+    s.x = c.take<Half>(mn);
+    for (Half*& t : s.xt) t = c.take<Half>(mn);
+    s.a = shared ? nullptr : c.take<Half>(mm);
+    s.b = c.take<Half>(mm);
     s.bytes = c.at;
     return s;
 }
 
-// T: the tile's edge.  XP: the three factors' rows are pairs, else only those of X's transpose are (bfloat16).
-template <int T, bool XP, Product WHAT, Last LAST, typename Out>
+// T: the tile's edge.
+template <int T, Product WHAT, Last LAST, typename Out>
 blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t batch, hipStream_t stream) {
-    constexpr bool kQ = XP || WHAT == kApply || WHAT == kApplyLast;
     constexpr int kM = 2, kN = T >= 128 ? 4 : 2;
     Factors g = f;
     const uint32_t tm = f.mp / T, tn = f.np / T;
@@ -592,42 +575,43 @@ blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t b
     g.tiles = WHAT == kGram || WHAT == kSquare ? tm * (tm + 1) / 2 : tm * tn;
     const uint64_t groups = static_cast<uint64_t>(g.tiles) * batch;
     if (groups > 0x7fffffff) return BLINK_EINVAL;
-    return launch(ortho_product<T, T, kM, kN, XP, kQ, XP, WHAT, LAST, Out>, dim3(static_cast<uint32_t>(groups)), dim3(kM * kN * 64), stream, g, o, tall);
+    return launch(ortho_product<T, T, kM, kN, WHAT, LAST, Out>, dim3(static_cast<uint32_t>(groups)), dim3(kM * kN * 64), stream, g, o, tall);
 }
 
 // A or B, of tiles of T.
-template <int T, bool XP, Product WHAT>
+template <int T, Product WHAT>
 blink_status_t run_symmetric(const Sizes& z, const Space& s, const Factors& f, size_t batch, hipStream_t stream) {
     if constexpr (T == 256)
         if (in_runs(z, batch, f.k)) {
             Factors g = f;
             g.tiles_n = f.mp / 256;
             g.tiles = g.tiles_n * (g.tiles_n + 1) / 2;
-            const Runs runs{s.sums, f.k / (XP ? 32 : 64), static_cast<uint32_t>(g.tiles * batch)};
-            BLINK_TRY(launch(ortho_runs<XP>, dim3(kRuns), dim3(Whole::kThreads), stream, g, runs));
-            return launch(ortho_gather<XP, WHAT>, dim3(runs.tiles * (kPartBlocks / (kGatherThreads / 64))), dim3(kGatherThreads), stream, g, runs);
+            const Runs runs{s.sums, f.k / kStage, static_cast<uint32_t>(g.tiles * batch)};
+            BLINK_TRY(launch(ortho_runs, dim3(kRuns), dim3(Whole::kThreads), stream, g, runs));
+            return launch(ortho_gather<WHAT>, dim3(runs.tiles * (kPartBlocks / (kGatherThreads / 64))), dim3(kGatherThreads), stream, g, runs);
         }
-    return run_product<T, XP, WHAT, kNone, float>(f, Outer{}, false, batch, stream);
+    return run_product<T, WHAT, kNone, float>(f, Outer{}, false, batch, stream);
 }
 
-template <int T, bool XP, Last LAST, typename Out>
+template <int T, Last LAST, typename Out>
 blink_status_t iterate(const Sizes& z, const Space& s, const Outer& o, bool tall, size_t batch, const float* co, int steps, hipStream_t stream) {
     for (int step = 0; step < steps; ++step, co += 3) {
         Factors f{};
+        Half* const a = s.a ? s.a : s.xt[~step & 1];
         f.p = f.q = s.x;
         f.mp = f.np = z.mp;
         f.k = z.np;
-        f.out = s.a;
+        f.out = a;
         f.c2 = kScaleA / (kScaleX * kScaleX);
         f.part = z.m < 64 ? 16 : 64;   // of few rows an element of A weighs more in the result
-        BLINK_TRY((run_symmetric<T, XP, kGram>(z, s, f, batch, stream)));
-        f.p = f.q = f.a = s.a;
+        BLINK_TRY((run_symmetric<T, kGram>(z, s, f, batch, stream)));
+        f.p = f.q = f.a = a;
         f.k = z.mp;
         f.out = s.b;
         f.c0 = co[0] * kScaleB;
         f.c1 = co[1] * (kScaleB / kScaleA);
         f.c2 = co[2] * (kScaleB / (kScaleA * kScaleA));
-        BLINK_TRY((run_symmetric<T, XP, kSquare>(z, s, f, batch, stream)));
+        BLINK_TRY((run_symmetric<T, kSquare>(z, s, f, batch, stream)));
         f.p = s.b;
         f.q = s.xt[step & 1];
         f.np = z.np;
@@ -635,28 +619,28 @@ blink_status_t iterate(const Sizes& z, const Space& s, const Outer& o, bool tall
         f.out_t = s.xt[~step & 1];
         if (step < steps - 1) {
             f.c2 = 1.0f / kScaleB;
-            BLINK_TRY((run_product<T, XP, kApply, kNone, float>(f, o, tall, batch, stream)));
+            BLINK_TRY((run_product<T, kApply, kNone, float>(f, o, tall, batch, stream)));
         } else {
             f.c2 = 1.0f / (kScaleB * kScaleX);
-            BLINK_TRY((run_product<T, XP, kApplyLast, LAST, Out>(f, o, tall, batch, stream)));
+            BLINK_TRY((run_product<T, kApplyLast, LAST, Out>(f, o, tall, batch, stream)));
         }
     }
     return BLINK_OK;
 }
 
-template <typename In, bool XP, Last LAST, typename Out>
+template <typename In, Last LAST, typename Out>
 blink_status_t run_all(const Sizes& z, size_t batch, const Outer& o, const float* co, int steps, float eps, void* workspace, hipStream_t stream) {
-    const Space s = space_of(z, batch, workspace);
+    const Space s = space_of(z, batch, sizeof(Out) == 2, workspace);
     const bool tall = o.rows > o.cols;
     constexpr size_t V = 16 / sizeof(float);
     const bool wide = o.cols % V == 0 && o.in_row % V == 0 && (batch == 1 || o.in_batch % V == 0) && aligned(o.in, V * sizeof(In)) && aligned(o.momentum, 16) &&
                       aligned(o.momentum_out, 16);
     BLINK_TRY(launch(wide ? ortho_norm<In, V> : ortho_norm<In, 1>, dim3(z.norm_parts, static_cast<uint32_t>(batch)), dim3(kNormThreads), stream, o, s.parts));
-    BLINK_TRY(launch(ortho_first<In, XP>, dim3(z.np / 64, z.mp / 64, static_cast<uint32_t>(batch)), dim3(kFirstThreads), stream, o, tall, s.parts, z.norm_parts, eps,
+    BLINK_TRY(launch(ortho_first<In>, dim3(z.np / 64, z.mp / 64, static_cast<uint32_t>(batch)), dim3(kFirstThreads), stream, o, tall, s.parts, z.norm_parts, eps,
                      z.mp, z.np, s.x, s.xt[0]));
-    if (z.tile == 256) return iterate<256, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
-    if (z.tile == 128) return iterate<128, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
-    return iterate<64, XP, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+    if (z.tile == 256) return iterate<256, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+    if (z.tile == 128) return iterate<128, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
+    return iterate<64, LAST, Out>(z, s, o, tall, batch, co, steps, stream);
 }
 
 }  // namespace
@@ -679,7 +663,7 @@ bool coefficients_fit(const float* co, int steps) {
 }
 
 size_t orthogonalize_workspace(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {
-    return space_of(sizes_of(batch, rows, cols, dtype), batch, nullptr).bytes;
+    return space_of(sizes_of(batch, rows, cols), batch, dtype != BLINK_FP32, nullptr).bytes;
 }
 
 blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, size_t rows, size_t cols, size_t in_row, size_t in_batch, const float* co,
@@ -693,12 +677,11 @@ blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, 
     o.out = out;
     o.out_row = out_row;
     o.out_batch = out_batch;
-    const Sizes z = sizes_of(batch, rows, cols, dtype);
-    if (dtype == BLINK_FP32) return run_all<float, true, kMatrix, float>(z, batch, o, co, steps, eps, workspace, stream);
-    if (dtype == BLINK_BF16)
-        return z.pair ? run_all<__bf16, true, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream)
-                      : run_all<__bf16, false, kMatrix, __bf16>(z, batch, o, co, steps, eps, workspace, stream);
-    return run_all<Half, true, kMatrix, Half>(z, batch, o, co, steps, eps, workspace, stream);
+    const Sizes z = sizes_of(batch, rows, cols);
+    return with_float(dtype, [&](auto type) {
+        using T = decltype(type);
+        return run_all<T, kMatrix, T>(z, batch, o, co, steps, eps, workspace, stream);
+    });
 }
 
 blink_status_t orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out, const void* grad,
@@ -718,9 +701,9 @@ blink_status_t orthogonal_step(const float* weights, float* weights_out, const f
     o.weights_out = weights_out;
     o.rate = rate;
     o.keep = 1.0f - decay;
-    const Sizes z = sizes_of(batch, rows, cols, BLINK_FP32);
+    const Sizes z = sizes_of(batch, rows, cols);
     return with_float(grad_type, [&](auto type) {
-        return run_all<decltype(type), true, kWeights, float>(z, batch, o, co, steps, eps, workspace, stream);
+        return run_all<decltype(type), kWeights, float>(z, batch, o, co, steps, eps, workspace, stream);
     });
 }
 

@@ -117,6 +117,37 @@ def test_bfloat16_is_near_its_rounding(shape):
     assert off <= math.sqrt(2.0 / 3.0) * UNIT[torch.bfloat16] * float(torch.linalg.matrix_norm(want))
 
 
+def _plain(m, steps=bl.BLINK_STEPS, eps=1e-7):
+    """The iteration with 32-bit floats throughout."""
+    x = m.float().reshape(-1, *m.shape[-2:])
+    tall = x.shape[1] > x.shape[2]
+    x = x.mT.contiguous() if tall else x
+    x = x / (torch.linalg.matrix_norm(x, keepdim=True) + eps)
+    for a, b, c in steps:
+        gram = x @ x.mT.contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return (x.mT if tall else x).reshape(m.shape)
+
+
+def _as_32_bits(off, m, want):
+    """Whether errors are those of 32-bit floats: half as large again as the plain form's on the same matrix, and what the five roundings of X to 22
+    bits add where few numbers make up a sum and the plain form is nearly exact (2^-23 of X at the most each, about doubled on the way)."""
+    plain = (_plain(m).double() - want).norm()
+    return float(off.norm()) <= 1.5 * float(plain) + 2.0 ** -20 * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", [(64, 64), (128, 512), (65, 70), (333, 200), (3, 129, 257), (2, 22, 4096), (20, 600, 900), (3500, 3600)])
+def test_16_bit_results_are_rounded_once(shape, dtype):
+    """Further from the definition's value than half a unit of the result's last place only by errors of 32-bit floats."""
+    m = _matrix(shape, dtype, 31)
+    want = _want(m)
+    bits = 8 if dtype == torch.bfloat16 else 11
+    least = -126 if dtype == torch.bfloat16 else -14          # below 2^least the last place is that of 2^least
+    half_unit = torch.exp2(torch.frexp(want.abs()).exponent.clamp(min=least + 1).double() - bits - 1)
+    assert _as_32_bits(((_run(m).double() - want).abs() - half_unit).clamp(min=0.0), m, want)
+
+
 def test_singular_values_move_to_one():
     m = _matrix((96, 160), torch.float32, 7)
     s = torch.linalg.svdvals(_run(m).double())
