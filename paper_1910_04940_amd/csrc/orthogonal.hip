@@ -521,13 +521,21 @@ struct Sizes {
 // Tiles of 256 keep the matrix instructions busiest, if there are about as many as compute units (a symmetric product that has fewer is done
 // in runs); tiles of 128 if the symmetric products have half as many.  us, 32-bit, tiles of 64 / 128 / 256: 1024 x 4096 388 / 559 /
 // 702, 1536 x 1536 432 / 443 / 813, 4 of 1024 x 1024 429 / 401 / 739, 2048 x 4096 1253 / 1043 / 1237, 4096 x 4096 5735 / 4306 / 3747.
+// Both only where rounding a side up to them adds no more than a third: what is added is multiplied and stored too.  us, 32-bit,
+// as here / in tiles that do not fill: 16 of 16 x 8192 431 / 877, 16 of 64 x 4096 236 / 527, 32 of 128 x 2048 247 / 562, 200 of 16 x 16
+// 86 / 488, 128 of 64 x 64 81 / 141, 48 of 180 x 1000 284 / 543, 16 of 320 x 4096 690 / 1285, 96 of 250 x 300 445 / 512.  But A of few narrow
+// and very long matrices has hardly a workgroup in small tiles, and runs of large ones share its sums (tiles of 64 / runs in tiles of 256 not
+// filled): 64 x 49152 1556 / 923, 128 x 100000 3205 / 1215, 2 of 128 x 24600 893 / 689, 4 of 16 x 16000 668 / 610, but 3 of 64 x 16600 604 / 607,
+// 4 of 64 x 12288 475 / 554, 8 of 16 x 16000 705 / 903.
 Sizes sizes_of(size_t batch, size_t rows, size_t cols) {
     Sizes z;
     z.m = static_cast<uint32_t>(std::min(rows, cols));
     z.n = static_cast<uint32_t>(std::max(rows, cols));
     const auto tiles = [&](uint64_t t) { return batch * ceil_div(z.m, t) * ceil_div(z.n, t); };
     const uint64_t side = ceil_div(z.m, 128);
-    z.tile = tiles(256) >= 192 ? 256 : batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
+    const auto fills = [&](uint64_t t) { return 3 * ceil_div(z.m, t) * t <= 4 * uint64_t{z.m} && 3 * ceil_div(z.n, t) * t <= 4 * uint64_t{z.n}; };
+    const bool long_sums = batch <= 4 && z.n > 16384;
+    z.tile = (fills(256) || long_sums) && tiles(256) >= 192 ? 256 : fills(128) && batch * side * (side + 1) / 2 >= 128 ? 128 : 64;
     z.mp = static_cast<uint32_t>(ceil_div(z.m, z.tile) * z.tile);
     z.np = static_cast<uint32_t>(ceil_div(z.n, z.tile) * z.tile);
     // parts of 1024 elements at the least, four to a thread, and about 4096 workgroups in all at the most

@@ -103,6 +103,15 @@ def test_workspaces_follow_the_sizes():
     assert bl.blink_orthogonalize_workspace(0, 64, 64, bl.BLINK_FP32) == 0 == bl.blink_orthogonalize_workspace(1, 64, 64, bl.BLINK_INT32)
 
 
+@pytest.mark.parametrize("batch,rows,cols", [(16, 16, 8192), (16, 4096, 22), (8, 32, 8192), (16, 64, 4096), (32, 128, 2048), (200, 16, 16), (128, 64, 64),
+                                             (8, 16_000, 16), (48, 180, 1000), (64, 150, 512), (16, 320, 4096), (96, 250, 300), (96, 400, 520)])
+def test_narrow_matrices_are_not_blown_up(batch, rows, cols):
+    """X, its transposes, A and B with sides rounded up to tiles of 64, or to larger ones that add no more than a third: 16/9 in all at the most,
+    and up to 1024 sums of the norm to a matrix."""
+    m, n = (max(-(-side // 64) * 64, side * 4 / 3) for side in sorted((rows, cols)))
+    assert bl.blink_orthogonalize_workspace(batch, rows, cols, bl.BLINK_FP32) <= batch * (4 * (3 * m * n + 2 * m * m) + 8 * 1024) + 8 * 256
+
+
 def test_collectives_take_none_of_the_new_types():
     import synth_inputs as si
     t = si.complete_graph(4)
