@@ -148,6 +148,26 @@ def test_16_bit_results_are_rounded_once(shape, dtype):
     assert _as_32_bits(((_run(m).double() - want).abs() - half_unit).clamp(min=0.0), m, want)
 
 
+@pytest.mark.parametrize("shape", [(1, 1), (16, 16), (64, 64), (65, 130), (22, 2025), (16, 22, 4096), (8, 4096, 32), (200, 16, 16), (1003, 389), (8, 300, 200),
+                                   (4, 1024, 1024), (20, 600, 900), (20, 900, 600), (3500, 3600), (760, 16_300), (2, 2300, 2500), (64, 49_152), (4, 22, 17_000)])
+def test_32_bit_results_are_those_of_32_bit_floats(shape):
+    """Tiles of every size, and products dealt out in runs."""
+    m = _matrix(shape, torch.float32, 37)
+    want = _want(m)
+    assert _as_32_bits(_run(m).double() - want, m, want)
+
+
+@pytest.mark.parametrize("shape", [(2025, 22), (1003, 389), (3, 22, 4096), (20, 600, 900), (2300, 2500)])
+def test_a_step_is_that_of_32_bit_floats(shape):
+    m, g = _matrix(shape, torch.float32, 41), _matrix(shape, torch.float32, 42)
+    batch = shape[0] if len(shape) == 3 else 1
+    work = torch.full((bl.blink_orthogonalize_workspace(batch, *shape[-2:], bl.BLINK_FP32),), 255, dtype=torch.uint8, device="cuda")
+    w, m1 = torch.zeros_like(m), torch.empty_like(m)
+    bl.blink_orthogonal_step(w, m, g, w, m1, work, rate=1.0, beta=0.5, stream=_stream())
+    want = _want(g.double() + 0.5 * (0.5 * m.double() + g.double()))
+    assert _as_32_bits(-w.double() - want, g + 0.5 * m1, want)
+
+
 def test_singular_values_move_to_one():
     m = _matrix((96, 160), torch.float32, 7)
     s = torch.linalg.svdvals(_run(m).double())
