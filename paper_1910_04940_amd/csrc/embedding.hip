@@ -28,7 +28,8 @@ constexpr int kRowUnits = 2;   // packs of one thread, their loads under way tog
 template <typename In, typename Out, typename Token, typename Unit, int V>
 __global__ __launch_bounds__(kRowThreads) void embedding_rows(const In* table, uint64_t vocab, uint64_t table_stride, const Token* tokens,
                                                               Unit units, uint32_t packs, float scale, Out* out, uint64_t out_stride, bool past) {
-    const Unit first = static_cast<Unit>(blockIdx.x) * (kRowThreads * kRowUnits) + threadIdx.x;   // (a Unit holds the grid's places)
+    const uint32_t block = sizeof(Unit) == 8 ? block_of(blockIdx.y) : blockIdx.x;
+    const Unit first = static_cast<Unit>(block) * (kRowThreads * kRowUnits) + threadIdx.x;   // (a Unit holds the grid's places)
     int64_t token[kRowUnits];
     uint64_t row[kRowUnits];
     uint32_t at[kRowUnits];
@@ -340,7 +341,7 @@ constexpr int kSumAhead = 8;   // rows of a sum whose loads are under way togeth
 template <typename Grad, typename T, int V, bool ADD>
 __global__ __launch_bounds__(kSumThreads) void embedding_sums(const Sums s) {
     constexpr bool ALL = !ADD;
-    const uint32_t place_of = __builtin_amdgcn_readfirstlane(blockIdx.x * (kSumThreads / 64) + (threadIdx.x >> 6));
+    const uint32_t place_of = __builtin_amdgcn_readfirstlane(block_of(blockIdx.y) * (kSumThreads / 64) + (threadIdx.x >> 6));
     const uint32_t w = place_of / s.columns, column = place_of - w * s.columns;
     if (w >= s.stretches) return;
     const uint32_t lane = threadIdx.x & 63, col = (column * 64 + lane) * V;
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join(const Sums s) {
     __shared__ Pack<float, V> part[kJoinWaves][64];
     __shared__ uint32_t row_of[kJoinWaves], from_of[kJoinWaves];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t col = (blockIdx.y * 64 + lane) * V, w0 = blockIdx.x * kJoinWaves;
+    const uint32_t col = (blockIdx.y * 64 + lane) * V, w0 = block_of(blockIdx.z) * kJoinWaves;
     const bool in = col < s.dim;
     const auto add_up = [&](float (&sum)[V], uint32_t a, uint32_t b) {
 #pragma unroll
@@ -543,12 +544,13 @@ template <typename Grad, typename T, int V>
 blink_status_t run_sums(Sums s, bool add, hipStream_t stream) {
     s.columns = static_cast<uint32_t>(ceil_div(s.dim, 64 * V));
     const uint64_t groups = ceil_div(static_cast<uint64_t>(s.stretches) * s.columns, kSumThreads / 64);
-    if (groups > 0x3fffffff) return BLINK_EINVAL;
-    BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, dim3(static_cast<uint32_t>(groups)), dim3(kSumThreads), stream, s));
+    if (groups > 0x3fffff00) return BLINK_EINVAL;   // (the waves' numbers have 32 bits)
+    const Grid grid = grid_of(groups, kSumThreads);
+    BLINK_TRY(launch(add ? embedding_sums<Grad, T, V, true> : embedding_sums<Grad, T, V, false>, dim3(grid.x, grid.y), dim3(kSumThreads), stream, s));
     // no row lies in two stretches: one position alone has one place, but next to that a row's end has one of its own where all rows are written
     if (s.n < (add ? 2u : 1u) || s.stretches < 2) return BLINK_OK;
-    const dim3 grid(static_cast<uint32_t>(ceil_div(s.stretches, kJoinWaves)), s.columns);
-    return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, grid, dim3(kJoinThreads), stream, s);
+    const Grid join = grid_of(ceil_div(s.stretches, kJoinWaves), kJoinThreads);
+    return launch(add ? embedding_join<T, V, true> : embedding_join<T, V, false>, dim3(join.x, s.columns, join.y), dim3(kJoinThreads), stream, s);
 }
 
 }  // namespace
@@ -568,11 +570,12 @@ blink_status_t embedding(const void* table, blink_dtype_t table_type, size_t voc
             };
             const int v = fits(kMost) ? kMost : 1;
             const uint64_t packs = dim / v, units = n * packs, blocks = ceil_div(units, kRowThreads * kRowUnits);
-            if (blocks > 0x7fffffff) return BLINK_EINVAL;
+            if (blocks > 0xfffff000) return BLINK_EINVAL;   // (2^41 elements at the least)
+            const Grid grid = grid_of(blocks, kRowThreads);
             const auto with_token = [&](auto token) {
                 using Token = decltype(token);
                 const auto go = [&](auto kernel) {
-                    return launch(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kRowThreads), stream, static_cast<const In*>(table), vocab, table_stride,
+                    return launch(kernel, dim3(grid.x, grid.y), dim3(kRowThreads), stream, static_cast<const In*>(table), vocab, table_stride,
                                   static_cast<const Token*>(tokens), units, static_cast<uint32_t>(packs), scale, static_cast<Out*>(out), out_stride,
                                   passes_caches(n * dim * sizeof(Out)));
                 };

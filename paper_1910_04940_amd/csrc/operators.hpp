@@ -80,6 +80,17 @@ __device__ inline void wave_sync() {
 
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
+// A launch has fewer than 2^32 threads in x.  More workgroups than that go in rows, y of them; block_of is a workgroup's number, which is past
+// the last one for some of the last row.
+struct Grid {
+    uint32_t x, y;
+};
+inline Grid grid_of(uint64_t groups, uint32_t threads) {
+    const uint64_t y = groups == 0 ? 1 : ceil_div(groups, 0xffffffffu / threads);
+    return {static_cast<uint32_t>(ceil_div(groups, y)), static_cast<uint32_t>(y)};
+}
+__device__ inline uint32_t block_of(uint32_t row) { return row * gridDim.x + blockIdx.x; }
+
 // Parts of a workspace, each on a 256-byte line.
 struct Carve {
     char* base;

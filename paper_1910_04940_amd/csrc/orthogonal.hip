@@ -582,7 +582,7 @@ blink_status_t run_product(const Factors& f, const Outer& o, bool tall, size_t b
     g.tiles_n = tn;
     g.tiles = WHAT == kGram || WHAT == kSquare ? tm * (tm + 1) / 2 : tm * tn;
     const uint64_t groups = static_cast<uint64_t>(g.tiles) * batch;
-    if (groups > 0x7fffffff) return BLINK_EINVAL;
+    if (groups * (kM * kN * 64) > 0xffffffff) return BLINK_EINVAL;   // (threads of a launch; a workspace beyond any memory)
     return launch(ortho_product<T, T, kM, kN, WHAT, LAST, Out>, dim3(static_cast<uint32_t>(groups)), dim3(kM * kN * 64), stream, g, o, tall);
 }
 

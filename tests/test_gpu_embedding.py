@@ -185,6 +185,34 @@ def test_gradient_of_one_row_for_all_tokens_and_of_views():
     assert (whole[:, dim:] == 3.0).all()
 
 
+def test_more_rows_than_a_launch_has_threads_in_one_direction():
+    """More than 2^33 elements that are loaded one by one: their places pass 32 bits, their workgroups 2^24."""
+    n, vocab, dim = 8_600_000, 300, 1001
+    table = torch.randn(vocab, dim, device="cuda").bfloat16()
+    tokens = torch.from_numpy(np.random.default_rng(7).integers(-1, vocab, n)).cuda()
+    out = torch.full((n, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    bl.blink_embedding(table, tokens, out, 1.0, _stream())
+    for lo in range(0, n, 500_000):
+        assert torch.equal(out[lo:lo + 500_000], _want_rows(table, tokens[lo:lo + 500_000], 1.0, torch.bfloat16))
+
+
+def test_a_longer_table_than_a_launch_has_threads_in_one_direction():
+    """The largest vocabulary: more than 2^24 workgroups, and keys of 31 bits."""
+    n, vocab = 3000, (1 << 31) - 2
+    rng = np.random.default_rng(8)
+    tokens = np.concatenate((rng.integers(0, vocab, n - 1000), rng.integers(vocab - 70, vocab, 900), rng.integers(0, 70, 90), np.full(10, vocab)))
+    tokens = torch.from_numpy(rng.permutation(tokens)).cuda()
+    grad = torch.randint(-3, 4, (n, 1), device="cuda").bfloat16()
+    table = torch.full((vocab, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    _gradient(tokens, grad, table, 0.5, False)
+    named = torch.unique(tokens[tokens < vocab])
+    want = torch.zeros(len(named), device="cuda").index_add_(0, torch.searchsorted(named, tokens[tokens < vocab]), 0.5 * grad[tokens < vocab, 0].float())
+    assert torch.equal(table[named, 0].float(), want)     # small halves: exact
+    table[named] = 0.0
+    for lo in range(0, vocab, 1 << 28):
+        assert (table[lo:lo + (1 << 28)] == 0.0).all()
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_a_gradient_past_32_bits(accumulate):
     """A table of more than 2^32 elements: the rows that tokens name, and others beside them."""
