@@ -143,8 +143,9 @@ static int matrix(PyObject* types, PyObject* t, matrix_t* m) {
     if (m->rows <= 1 && m->stride < m->cols) m->stride = m->cols;
     return 1;
 }
-/* A contiguous tensor of `elements` (any number: -1, which is then set) of that type (any of the two for tokens). */
-static int whole(PyObject* types, PyObject* t, long code, long or_code, Py_ssize_t* elements, void** at, long* is) {
+static int is_float(long code) { return code == BLINK_FP32 || code == BLINK_BF16 || code == BLINK_FP16; }
+/* A contiguous tensor of any shape (tokens) of `elements` (any number: -1, which is then set), of one of two types. */
+static int any_shape(PyObject* types, PyObject* t, long code, long or_code, Py_ssize_t* elements, void** at, long* is) {
     long c;
     if (!tensor(types, t, at, &c) || (c != code && c != or_code) || !attribute_is_true(t, contiguous_name, 1)) return 0;
     PyObject* const n = PyObject_CallMethodNoArgs(t, numel_name);
@@ -154,13 +155,23 @@ static int whole(PyObject* types, PyObject* t, long code, long or_code, Py_ssize
     if (many < 0) return unusual();
     if (*elements >= 0 && many != *elements) return 0;
     *elements = many;
-    if (is) *is = c;
+    *is = c;
     return 1;
 }
-/* The same with two dimensions. */
+/* The same of one type and one dimension. */
+static int whole(PyObject* types, PyObject* t, long code, Py_ssize_t* elements, void** at) {
+    long is;
+    PyObject* const shape = PyObject_GetAttr(t, shape_name);
+    if (!shape) return unusual();
+    const int line = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1;
+    Py_DECREF(shape);
+    return line && any_shape(types, t, code, code, elements, at, &is);
+}
+/* Of two dimensions. */
 static int table(PyObject* types, PyObject* t, long code, Py_ssize_t rows, Py_ssize_t cols, void** at) {
     Py_ssize_t r, c, n = rows * cols;
-    return pair_of(PyObject_GetAttr(t, shape_name), &r, &c) && r == rows && c == cols && whole(types, t, code, code, &n, at, NULL);
+    long is;
+    return pair_of(PyObject_GetAttr(t, shape_name), &r, &c) && r == rows && c == cols && any_shape(types, t, code, code, &n, at, &is);
 }
 static int space(PyObject* t, void** at, Py_ssize_t* bytes) {   /* a contiguous tensor of any type, or none */
     unsigned long long p = 0, n = 0;
@@ -208,8 +219,8 @@ static PyObject* embedding(PyObject* self, PyObject* const* args, Py_ssize_t nar
     void* tokens;
     long token;
     float scale;
-    USUAL(matrix(types, args[2], &t) && whole(types, args[3], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[4], &o) &&
-          o.rows == n && o.cols == t.cols && number(args[5], &scale) && t.code > 0 && o.code > 0);
+    USUAL(matrix(types, args[2], &t) && any_shape(types, args[3], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[4], &o) &&
+          o.rows == n && o.cols == t.cols && number(args[5], &scale) && is_float(t.code) && is_float(o.code));
     RUN(((__typeof__(&blink_embedding))fn)(t.at, (blink_dtype_t)t.code, (size_t)t.rows, (size_t)t.cols, (size_t)t.stride, tokens, (blink_dtype_t)token,
                                            (size_t)n, scale, o.at, (blink_dtype_t)o.code, (size_t)o.stride, (void*)stream));
 }
@@ -223,8 +234,8 @@ static PyObject* embedding_gradient(PyObject* self, PyObject* const* args, Py_ss
     long token;
     float scale;
     int accumulate;
-    USUAL(whole(types, args[2], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[3], &g) && matrix(types, args[4], &t) && g.rows == n &&
-          g.cols == t.cols && space(args[5], &work, &size) && number(args[6], &scale) && truth(args[7], &accumulate) && t.code > 0 && g.code > 0);
+    USUAL(any_shape(types, args[2], BLINK_INT64, BLINK_INT32, &n, &tokens, &token) && matrix(types, args[3], &g) && matrix(types, args[4], &t) && g.rows == n &&
+          g.cols == t.cols && space(args[5], &work, &size) && number(args[6], &scale) && truth(args[7], &accumulate) && is_float(t.code) && is_float(g.code));
     RUN(((__typeof__(&blink_embedding_gradient))fn)(tokens, (blink_dtype_t)token, (size_t)n, g.at, (blink_dtype_t)g.code, (size_t)g.stride, scale, accumulate,
                                                     t.at, (blink_dtype_t)t.code, (size_t)t.rows, (size_t)t.cols, (size_t)t.stride, work, (size_t)size,
                                                     (void*)stream));
@@ -237,12 +248,12 @@ static PyObject* route(PyObject* self, PyObject* const* args, Py_ssize_t nargs) 
     Py_ssize_t size, n, e;
     void *chosen, *weights, *counts, *sums, *work, *keep = NULL;
     int k, normalize;
-    USUAL(matrix(types, args[2], &x) && x.code > 0 && x.cols < 0x7fffffff && small(args[3], &k));
+    USUAL(matrix(types, args[2], &x) && is_float(x.code) && x.cols < 0x7fffffff && small(args[3], &k));
     n = x.rows;
     e = x.cols + 1;
     USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && table(types, args[5], BLINK_FP32, n, k, &weights) &&
-          whole(types, args[6], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) && whole(types, args[7], BLINK_FP32, BLINK_FP32, &e, &sums, NULL) &&
-          space(args[8], &work, &size) && (args[9] == Py_None || whole(types, args[9], -1, -1, &n, &keep, NULL)) && truth(args[10], &normalize));
+          whole(types, args[6], BLINK_INT32, &e, &counts) && whole(types, args[7], BLINK_FP32, &e, &sums) &&
+          space(args[8], &work, &size) && (args[9] == Py_None || whole(types, args[9], -1, &n, &keep)) && truth(args[10], &normalize));
     RUN(((__typeof__(&blink_route))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k, normalize, chosen, weights, counts,
                                        sums, work, (size_t)size, (void*)stream));
 }
@@ -254,9 +265,9 @@ static PyObject* route_loss(PyObject* self, PyObject* const* args, Py_ssize_t na
     void *counts, *sums, *loss;
     int k;
     float balance, z;
-    USUAL(whole(types, args[2], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) && e > 0 && e <= 0x7fffffff &&
-          whole(types, args[3], BLINK_FP32, BLINK_FP32, &e, &sums, NULL) && small(args[4], &k) &&
-          whole(types, args[5], BLINK_FP32, BLINK_FP32, &three, &loss, NULL) && number(args[6], &balance) && number(args[7], &z));
+    USUAL(whole(types, args[2], BLINK_INT32, &e, &counts) && e > 0 && e <= 0x7fffffff &&
+          whole(types, args[3], BLINK_FP32, &e, &sums) && small(args[4], &k) &&
+          whole(types, args[5], BLINK_FP32, &three, &loss) && number(args[6], &balance) && number(args[7], &z));
     RUN(((__typeof__(&blink_route_loss))fn)(counts, sums, (int)(e - 1), k, balance, z, loss, (void*)stream));
 }
 
@@ -268,14 +279,14 @@ static PyObject* route_gradient(PyObject* self, PyObject* const* args, Py_ssize_
     void *chosen, *counts, *keep = NULL, *by_weight = NULL, *up = NULL;
     int k, normalize;
     float balance, z;
-    USUAL(matrix(types, args[2], &x) && x.code > 0 && x.cols < 0x7fffffff && small(args[3], &k) && matrix(types, args[6], &g) && g.code == x.code &&
+    USUAL(matrix(types, args[2], &x) && is_float(x.code) && x.cols < 0x7fffffff && small(args[3], &k) && matrix(types, args[6], &g) && g.code == x.code &&
           g.rows == x.rows && g.cols == x.cols);
     n = x.rows;
     e = x.cols + 1;
-    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && whole(types, args[5], BLINK_INT32, BLINK_INT32, &e, &counts, NULL) &&
-          (args[7] == Py_None || whole(types, args[7], -1, -1, &n, &keep, NULL)) && truth(args[8], &normalize) &&
+    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && whole(types, args[5], BLINK_INT32, &e, &counts) &&
+          (args[7] == Py_None || whole(types, args[7], -1, &n, &keep)) && truth(args[8], &normalize) &&
           (args[9] == Py_None || table(types, args[9], BLINK_FP32, n, k, &by_weight)) &&
-          (args[10] == Py_None || whole(types, args[10], BLINK_FP32, BLINK_FP32, &one, &up, NULL)) && number(args[11], &balance) && number(args[12], &z));
+          (args[10] == Py_None || whole(types, args[10], BLINK_FP32, &one, &up)) && number(args[11], &balance) && number(args[12], &z));
     RUN(((__typeof__(&blink_route_gradient))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k, normalize, chosen, by_weight,
                                                 counts, up, balance, z, g.at, (size_t)g.stride, (void*)stream));
 }
