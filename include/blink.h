@@ -501,7 +501,8 @@ void blink_miad_free(blink_miad_t* m);
  *     with any contents; the call's own until it has run.
  *   - Results are the same from call to call: atomics add nothing but whole numbers.
  *   - Outputs may not overlap inputs, except where "in place" is said.
- *   - Floating types are FP32, BF16, FP16; sums are formed in 32 bits or more and rounded once.
+ *   - Floating types are FP32, BF16, FP16; sums are formed in 32 bits or more and results rounded once (the factors of the
+ *     orthogonalised updates' products are held in 22 bits, see there).
  */
 
 /* out[i] = scale * table[tokens[i]], rows of dim elements, for i < n_tokens; a token outside

@@ -411,7 +411,7 @@ __device__ inline void write_block(const Factors& f, const Outer& o, bool tall, 
 }
 
 // A tile of a product to a workgroup.  Tiles of 256 are bound by the matrix instructions at
-// the clock that power allows: B X of 8192 x 4096 pairs 670 us, 1.23 PFLOP/s of products, 71 % busy at 1.73 GHz (16-bit library product
+// the clock that power allows: B X of 8192 x 4096 pairs 706 us, 1.17 PFLOP/s of products, 68 % busy at 1.64 GHz (16-bit library product
 // of 8192 cubed 1.39); small ones by latency, 3 to 10 us.
 template <int TM, int TN, int WAVES_M, int WAVES_N, Product WHAT, Last LAST, typename Out>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void ortho_product(const Factors f, const Outer o, bool tall) {

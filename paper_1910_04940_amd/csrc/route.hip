@@ -408,7 +408,7 @@ __global__ __launch_bounds__(kLossThreads) void route_loss_kernel(const int32_t*
     loss[2] = static_cast<float>(l);
 }
 
-// The logits are read again: their softmax would have to be written and read.  262144 x 256 bfloat16, k = 8, 67 us, 460 vector instructions a
+// The logits are read again: their softmax would have to be written and read.  262144 x 256 bfloat16, k = 8, 67 us, 425 vector instructions a
 // wave for four tokens, 268 MB.
 struct RouteGradient {
     const void* logits;
