@@ -15,7 +15,7 @@
  *                        (paper section 4.2.1)
  *   blink_make_schedule_servers / blink_hybrid_split
  *                        several servers, two classes of links (sections 3.5, 3.4)
- *   blink_embedding* / blink_route* / blink_orthogonal*
+ *   blink_embedding* / blink_route* / blink_orthogonal* / blink_gradient_norm / blink_adamw_step
  *                        what a training step does around its collectives
  *
  * Conventions
@@ -23,7 +23,7 @@
  *     through pointer arguments.  No exception crosses this boundary.
  *   - "host" / "device" in a parameter comment says where the pointed-to memory
  *     must live.
- *   - Handles (blink_trees_t, blink_schedule_t) are owned by the library and
+ *   - Handles (blink_trees_t, blink_schedule_t, blink_update_t) are owned by the library and
  *     released with the matching *_free.  The caller owns every buffer it
  *     passes in; the library never frees or reallocates caller memory.
  *   - A schedule keeps device-side progress counters: it may be used by many
@@ -64,7 +64,7 @@ typedef enum {
 } blink_status_t;
 
 /* The collectives take INT32 and FP32; what each of the operators takes is said there. */
-typedef enum { BLINK_INT32 = 0, BLINK_FP32 = 1, BLINK_BF16 = 2, BLINK_FP16 = 3, BLINK_INT64 = 4 } blink_dtype_t;
+typedef enum { BLINK_INT32 = 0, BLINK_FP32 = 1, BLINK_BF16 = 2, BLINK_FP16 = 3, BLINK_INT64 = 4, BLINK_FP8 = 5 /* e4m3, moments only */ } blink_dtype_t;
 /* Collectives (paper section 4.1).  REDUCE is the reduce phase of AllReduce on
  * its own: afterwards only the root of each tree holds the result (on that
  * tree's share); what the other ranks' buffers hold is unspecified. */
@@ -107,6 +107,7 @@ typedef enum { BLINK_FUSE_EDGE = 0, BLINK_FUSE_NODE = 1, BLINK_FUSE_TREE = 2 } b
 
 typedef struct blink_trees blink_trees_t;
 typedef struct blink_schedule blink_schedule_t;
+typedef struct blink_update blink_update_t;
 
 /* One transfer over one tree edge for one chunk (paper section 4.1).
  * REDUCE: dst[off, off+len) <- dst[off, off+len) + src[off, off+len)
@@ -491,8 +492,9 @@ void blink_miad_free(blink_miad_t* m);
  *
  * What a data-parallel training step does next to its collectives: the rows of an embedding
  * table and the gradient that ranks then sum, a router's choice of experts with the counts
- * and sums that ranks then add up, and the orthogonalised update of a matrix once its
- * gradient is summed.  Each call enqueues gfx950 kernels on the stream and returns; none
+ * and sums that ranks then add up, and the optimiser's step once gradients are summed: the
+ * orthogonalised update of a matrix, or AdamW over many tensors.  Each call but
+ * blink_make_update enqueues gfx950 kernels on the stream and returns; none
  * allocates, copies or synchronises, so each can be recorded into a HIP graph, and calls
  * on different streams are independent if their buffers are.
  *   - All buffers are device memory unless "host" is said; strides count elements.
@@ -567,6 +569,38 @@ blink_status_t blink_orthogonal_step(const float* weights, float* weights_out, c
                                      const void* grad, blink_dtype_t grad_type, size_t batch, size_t rows, size_t cols,
                                      float beta, int nesterov, const float* coefficients, int steps, float eps,
                                      float rate, float decay, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The tensors that an optimiser changes, once for all steps: the list is read, and kept with the addresses in it, in device memory of the
+ * current device (allocated and written synchronously, not while a stream is captured).  The calls below take it on that device (EMISMATCH on
+ * another); it must outlive them, and graphs that hold them. */
+typedef struct {
+    const void* grad;        /* [elements], of grad_type */
+    void* weights;           /* [elements], of weight_type; null: the gradient counts in the norm, and the tensor is left to others */
+    float* master;           /* null, or with 16-bit weights: the copy in 32 bits that is stepped; weights become its rounding */
+    void *moment1, *moment2; /* [elements], FP32: m and v; FP8: m and sqrt(v), each e4m3 number times its scale */
+    float *scale1, *scale2;  /* with FP8 only: one for every 256 elements of a tensor, the last for what is left */
+    size_t elements;
+    blink_dtype_t weight_type, grad_type, moment_type;
+    double rate, decay;      /* lr is multiplied by rate; decay: of the weights, per unit of lr * rate */
+} blink_update_tensor_t;     /* elements lie one after the other and may start anywhere, moments all 0 before the first step */
+blink_status_t blink_make_update(const blink_update_tensor_t* tensors /* host */, int n_tensors, blink_update_t** out);
+void blink_update_free(blink_update_t* u);
+
+/* norm[0] = |factor| * the root of the sum of the squares of all gradients; norm[1] = what a step is to multiply them by: factor, times
+ * max_norm / norm[0] where that is less than 1 (max_norm > 0; infinity: never), or NaN where a gradient is infinite or NaN.  factor: 1 / ranks
+ * makes the mean of a sum over ranks.  step: null, or counted up by one unless norm[1] is NaN. */
+size_t blink_gradient_norm_workspace(const blink_update_t* u);
+blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, double factor, float* norm, int32_t* step,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+/* A step of AdamW on every tensor that has weights, in place, with g = scale[0] * gradient (null: 1) and r = lr * rate of the tensor * rate[0] (null: 1):
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - r decay) - r (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * t = step[0] (read on the device, so that a graph's replays step on); nothing is written where it is below 1 or scale[0] is NaN.  eps > 0.
+ * FP8 moments: a scale is the largest of its 256 / 448 (moments below 2^-100 are 0), and numbers are rounded up or down by random bits of seed, t, the
+ * tensor's place in the list and the element's in it, up with the probability of what down would drop; a root that is not 0 is at least 2^-9
+ * times its scale.  A NaN or an infinity makes its 256 elements' moments NaN.  seed is without meaning for FP32. */
+blink_status_t blink_adamw_step(const blink_update_t* u, const int32_t* step, double lr, double beta1, double beta2, double eps,
+                                const float* scale, const float* rate, uint32_t seed, void* stream);
 
 const char* blink_strerror(blink_status_t st);
 

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libblink.so")
 BLINK_MAX_RANKS = 16
 BLINK_ROOT_ANY = -1
 BLINK_OK, BLINK_EINVAL, BLINK_EDISCONNECTED, BLINK_ENOMEM, BLINK_EMISMATCH, BLINK_EHIP, BLINK_ESTUCK, BLINK_ELIMIT = range(8)
-BLINK_INT32, BLINK_FP32, BLINK_BF16, BLINK_FP16, BLINK_INT64 = 0, 1, 2, 3, 4
+BLINK_INT32, BLINK_FP32, BLINK_BF16, BLINK_FP16, BLINK_INT64, BLINK_FP8 = 0, 1, 2, 3, 4, 5
 BLINK_OP_BROADCAST, BLINK_OP_ALLREDUCE, BLINK_OP_REDUCE, BLINK_OP_ALLGATHER, BLINK_OP_GATHER = 0, 1, 2, 3, 4
 BLINK_SUM, BLINK_PROD, BLINK_MIN, BLINK_MAX = 0, 1, 2, 3
 BLINK_STEP_REDUCE, BLINK_STEP_COPY = 0, 1
@@ -34,6 +34,11 @@ STEP_DTYPE = np.dtype([("kind", "<i4"), ("tree", "<i4"), ("chunk", "<i4"), ("src
 # numpy mirror of blink_progress_t
 PROGRESS_DTYPE = np.dtype([("state", "<i4"), ("stage", "<i4"), ("awaited_stage", "<i4"), ("reserved", "<i4"),
                            ("seen", "<u8"), ("wanted", "<u8"), ("call", "<u8")], align=True)
+
+# numpy mirror of blink_update_tensor_t
+UPDATE_TENSOR_DTYPE = np.dtype([("grad", "<u8"), ("weights", "<u8"), ("master", "<u8"), ("moment1", "<u8"), ("moment2", "<u8"),
+                                ("scale1", "<u8"), ("scale2", "<u8"), ("elements", "<u8"), ("weight_type", "<i4"), ("grad_type", "<i4"),
+                                ("moment_type", "<i4"), ("rate", "<f8"), ("decay", "<f8")], align=True)
 
 # numpy mirror of blink_stage_t
 STAGE_DTYPE = np.dtype([("off", "<u8"), ("len", "<u4"), ("tree", "<i4"), ("chunk", "<i4"), ("flow", "<i4"),
@@ -57,7 +62,8 @@ EXPORTS = [
     "blink_schedule_kernel_bytes", "blink_schedule_set_hand_over", "blink_schedule_handed_over",
     "blink_embedding", "blink_embedding_gradient_workspace", "blink_embedding_gradient", "blink_route_workspace",
     "blink_route", "blink_route_loss", "blink_route_gradient", "blink_orthogonalize_workspace", "blink_orthogonalize",
-    "blink_orthogonal_step",
+    "blink_orthogonal_step", "blink_make_update", "blink_update_free", "blink_gradient_norm_workspace", "blink_gradient_norm",
+    "blink_adamw_step",
 ]
 
 
@@ -173,7 +179,13 @@ def lib() -> C.CDLL:
     L.blink_route_gradient.argtypes = [vp, i, z, i, z, vp, i, i, vp, vp, vp, vp, f, f, vp, z, vp]
     L.blink_orthogonalize.argtypes = [vp, i, z, z, z, z, z, C.POINTER(f), i, f, vp, z, z, vp, z, vp]
     L.blink_orthogonal_step.argtypes = [vp, vp, vp, vp, vp, i, z, z, z, f, i, C.POINTER(f), i, f, f, f, vp, z, vp]
-    for name, sizes in (("embedding_gradient", [z, z, z]), ("route", [z, i]), ("orthogonalize", [z, z, z, i])):
+    L.blink_make_update.argtypes = [vp, i, C.POINTER(vp)]
+    L.blink_update_free.argtypes = [vp]
+    L.blink_update_free.restype = None
+    d = C.c_double
+    L.blink_gradient_norm.argtypes = [vp, d, d, vp, vp, vp, z, vp]
+    L.blink_adamw_step.argtypes = [vp, vp, d, d, d, d, vp, vp, C.c_uint32, vp]
+    for name, sizes in (("gradient_norm", [vp]), ("embedding_gradient", [z, z, z]), ("route", [z, i]), ("orthogonalize", [z, z, z, i])):
         getattr(L, f"blink_{name}_workspace").argtypes = sizes
         getattr(L, f"blink_{name}_workspace").restype = z
     L.blink_strerror.argtypes = [C.c_int]
@@ -186,7 +198,7 @@ def lib() -> C.CDLL:
         for name in _at:
             _at[name] = C.cast(getattr(L, name), vp).value
         _call = _blinkcall.call
-        for name in ("embedding", "embedding_gradient", "route", "route_loss", "route_gradient"):
+        for name in ("embedding", "embedding_gradient", "route", "route_loss", "route_gradient", "gradient_norm", "adamw_step"):
             _operators[name] = getattr(_blinkcall, name), C.cast(getattr(L, f"blink_{name}"), vp).value
     _lib = L
     return L

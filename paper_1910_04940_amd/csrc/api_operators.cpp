@@ -1,12 +1,14 @@
 // extern "C" boundary of the operators around the collectives: argument checks.
 #include <cmath>
+#include <new>
 
 #include "operators_api.hpp"
 
 namespace {
 
 constexpr size_t kMostTokens = 0x7fffffff, kMostDim = size_t{1} << 21, kMostSide = size_t{1} << 20, kMostBatch = 65535;
-constexpr int kMostExperts = 1024, kMostSteps = 64;
+constexpr size_t kMostElements = size_t{1} << 40;
+constexpr int kMostExperts = 1024, kMostSteps = 64, kMostTensors = 1 << 20;
 
 bool is_token(blink_dtype_t t) { return t == BLINK_INT32 || t == BLINK_INT64; }
 // A buffer of elements of `size` bytes; it may be null where it has none.
@@ -16,6 +18,17 @@ bool workspace_ok(const void* p, size_t has, size_t needs) { return needs == 0 |
 // Whether matrices that are written do not overlap: one after the other, or their rows in turn.
 bool apart(size_t batch, size_t rows, size_t cols, size_t row_stride, size_t batch_stride) {
     return batch_stride >= (rows - 1) * row_stride + cols || (batch_stride >= cols && row_stride >= (batch - 1) * batch_stride + cols);
+}
+
+// One tensor of a list: its addresses, types and numbers.
+bool tensor_ok(const blink_update_tensor_t& t) {
+    if (!blink::is_float(t.grad_type) || t.elements > kMostElements || !buffer_ok(t.grad, t.elements, blink::size_of(t.grad_type))) return false;
+    if (!t.weights) return !t.master && !t.moment1 && !t.moment2 && !t.scale1 && !t.scale2;   // (its gradient counts, it is not stepped)
+    const bool eight = t.moment_type == BLINK_FP8;
+    if (!blink::is_float(t.weight_type) || (t.moment_type != BLINK_FP32 && !eight) || (t.master && t.weight_type == BLINK_FP32)) return false;
+    return blink::aligned(t.weights, blink::size_of(t.weight_type)) && blink::aligned(t.master, 4) && buffer_ok(t.moment1, t.elements, eight ? 1 : 4) &&
+           buffer_ok(t.moment2, t.elements, eight ? 1 : 4) && (eight ? buffer_ok(t.scale1, t.elements, 4) && buffer_ok(t.scale2, t.elements, 4) : !t.scale1 && !t.scale2) &&
+           std::isfinite(t.rate) && std::isfinite(t.decay);
 }
 
 }  // namespace
@@ -112,6 +125,39 @@ blink_status_t blink_orthogonal_step(const float* weights, float* weights_out, c
         return BLINK_EINVAL;
     return blink::orthogonal_step(weights, weights_out, momentum, momentum_out, grad, grad_type, batch, rows, cols, beta, nesterov == 1, coefficients, steps, eps,
                                   rate, decay, workspace, static_cast<hipStream_t>(stream));
+}
+
+blink_status_t blink_make_update(const blink_update_tensor_t* tensors, int n, blink_update_t** out) {
+    if (!out) return BLINK_EINVAL;
+    *out = nullptr;
+    if (!tensors || n < 1 || n > kMostTensors) return BLINK_EINVAL;
+    for (int i = 0; i < n; ++i)
+        if (!tensor_ok(tensors[i])) return BLINK_EINVAL;
+    try {
+        return blink::make_update(tensors, n, out);
+    } catch (...) {   // (nothing else throws)
+        return BLINK_ENOMEM;
+    }
+}
+
+void blink_update_free(blink_update_t* u) { blink::free_update(u); }
+
+size_t blink_gradient_norm_workspace(const blink_update_t* u) { return u ? blink::gradient_norm_workspace(*u) : 0; }
+
+blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, double factor, float* norm, int32_t* step, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+    if (!u || !(max_norm > 0) || !std::isfinite(factor) || !buffer_ok(norm, 1, 4) || !blink::aligned(step, 4) ||
+        !workspace_ok(workspace, workspace_bytes, blink::gradient_norm_workspace(*u)))
+        return BLINK_EINVAL;
+    return blink::gradient_norm(*u, max_norm, factor, norm, step, workspace, static_cast<hipStream_t>(stream));
+}
+
+blink_status_t blink_adamw_step(const blink_update_t* u, const int32_t* step, double lr, double beta1, double beta2, double eps, const float* scale,
+                                const float* rate, uint32_t seed, void* stream) {
+    if (!u || !buffer_ok(step, 1, 4) || !std::isfinite(lr) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0 && std::isfinite(eps)) ||
+        !blink::aligned(scale, 4) || !blink::aligned(rate, 4))
+        return BLINK_EINVAL;
+    return blink::adamw_step(*u, step, lr, beta1, beta2, eps, scale, rate, seed, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

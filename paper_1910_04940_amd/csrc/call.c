@@ -182,12 +182,22 @@ static int space(PyObject* t, void** at, Py_ssize_t* bytes) {   /* a contiguous 
     *bytes = (Py_ssize_t)n;
     return 1;
 }
-static int number(PyObject* o, float* out) {
+static int precise(PyObject* o, double* out) {
     if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return 0;
-    const double v = PyFloat_AsDouble(o);
-    if (v == -1.0 && PyErr_Occurred()) return unusual();
+    *out = PyFloat_AsDouble(o);
+    return *out == -1.0 && PyErr_Occurred() ? unusual() : 1;
+}
+static int number(PyObject* o, float* out) {
+    double v;
+    if (!precise(o, &v)) return 0;
     *out = (float)v;
     return 1;
+}
+static int owned(PyObject* o, void** handle) {   /* what a handle's owner holds */
+    unsigned long long w = 0;
+    const int ok = word_of(PyObject_GetAttr(o, address_name), &w);
+    *handle = (void*)w;
+    return ok;
 }
 static int truth(PyObject* o, int* out) {
     *out = o == Py_True;
@@ -291,6 +301,30 @@ static PyObject* route_gradient(PyObject* self, PyObject* const* args, Py_ssize_
                                                 counts, up, balance, z, g.at, (size_t)g.stride, (void*)stream));
 }
 
+/* update, norm, workspace, max_norm, factor, step, stream */
+static PyObject* gradient_norm(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(9);
+    Py_ssize_t one = 1, two = 2, size;
+    void *update, *norm, *work, *step = NULL;
+    double most, factor;
+    USUAL(owned(args[2], &update) && whole(types, args[3], BLINK_FP32, &two, &norm) && space(args[4], &work, &size) && precise(args[5], &most) &&
+          precise(args[6], &factor) && (args[7] == Py_None || whole(types, args[7], BLINK_INT32, &one, &step)));
+    RUN(((__typeof__(&blink_gradient_norm))fn)(update, most, factor, norm, step, work, (size_t)size, (void*)stream));
+}
+
+/* update, step, lr, beta1, beta2, eps, scale, rate, seed, stream */
+static PyObject* adamw_step(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(12);
+    Py_ssize_t one = 1;
+    unsigned long long seed;
+    void *update, *step, *scale = NULL, *rate = NULL;
+    double lr, beta1, beta2, eps;
+    USUAL(owned(args[2], &update) && whole(types, args[3], BLINK_INT32, &one, &step) && precise(args[4], &lr) && precise(args[5], &beta1) &&
+          precise(args[6], &beta2) && precise(args[7], &eps) && (args[8] == Py_None || whole(types, args[8], BLINK_FP32, &one, &scale)) &&
+          (args[9] == Py_None || whole(types, args[9], BLINK_FP32, &one, &rate)) && word(args[10], &seed) && seed <= 0xffffffffu);
+    RUN(((__typeof__(&blink_adamw_step))fn)(update, step, lr, beta1, beta2, eps, scale, rate, (uint32_t)seed, (void*)stream));
+}
+
 static PyMethodDef methods[] = {
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, NULL},
     {"embedding", (PyCFunction)(void (*)(void))embedding, METH_FASTCALL, NULL},
@@ -298,6 +332,8 @@ static PyMethodDef methods[] = {
     {"route", (PyCFunction)(void (*)(void))route, METH_FASTCALL, NULL},
     {"route_loss", (PyCFunction)(void (*)(void))route_loss, METH_FASTCALL, NULL},
     {"route_gradient", (PyCFunction)(void (*)(void))route_gradient, METH_FASTCALL, NULL},
+    {"gradient_norm", (PyCFunction)(void (*)(void))gradient_norm, METH_FASTCALL, NULL},
+    {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blinkcall", NULL, 0, methods, NULL, NULL, NULL, NULL};

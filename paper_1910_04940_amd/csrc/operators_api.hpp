@@ -1,4 +1,4 @@
-// What api_operators.cpp checks the arguments for (embedding.hip, route.hip, orthogonal.hip).
+// What api_operators.cpp checks the arguments for (embedding.hip, route.hip, orthogonal.hip, update.hip).
 #pragma once
 #include "operators.hpp"
 
@@ -27,5 +27,12 @@ blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, 
 blink_status_t orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out, const void* grad,
                                blink_dtype_t grad_type, size_t batch, size_t rows, size_t cols, float beta, bool nesterov, const float* coefficients,
                                int steps, float eps, float rate, float decay, void* workspace, hipStream_t stream);
+
+blink_status_t make_update(const blink_update_tensor_t* tensors, int n, blink_update** out);
+void free_update(blink_update* u);
+size_t gradient_norm_workspace(const blink_update& u);
+blink_status_t gradient_norm(const blink_update& u, double most, double factor, float* norm, int32_t* step, void* workspace, hipStream_t stream);
+blink_status_t adamw_step(const blink_update& u, const int32_t* step, double lr, double beta1, double beta2, double eps, const float* scale, const float* rate,
+                          uint32_t seed, hipStream_t stream);
 
 }  // namespace blink

@@ -13,6 +13,7 @@
 // sums over tokens stay in registers until its end.  Every lane puts its logits in order by a network of exchanges; the k largest are
 // then the k largest of the lanes' first ones in turn, at a cost that hardly depends on N.  Workgroups leave their sums in the workspace, a second kernel adds
 // them up in order.  Both kernels over the logits read them once.
+#include "lanes.hpp"
 #include "operators_api.hpp"
 
 #include <algorithm>
@@ -24,46 +25,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostGroups = 1024;        // workgroups of the first kernel: 16 waves on a CU
 constexpr float kInf = __builtin_inff();
-
-// ---- lanes of a token: L neighbours, L a power of two -----------------------------------------------------------------------
-// op(own value, the other half's), for halves of 1, 2, 4 ... lanes, each of which holds one value by then.
-template <int L, typename X, typename F>
-__device__ inline X over_lanes(X x, F op) {
-    const auto dpp = [](X v, auto control) {
-        return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
-    };
-    if constexpr (L > 1) x = op(x, dpp(x, std::integral_constant<int, 0xB1>()));    // quad_perm 1 0 3 2
-    if constexpr (L > 2) x = op(x, dpp(x, std::integral_constant<int, 0x4E>()));    // quad_perm 2 3 0 1
-    if constexpr (L > 4) x = op(x, dpp(x, std::integral_constant<int, 0x141>()));   // row_half_mirror
-    if constexpr (L > 8) x = op(x, dpp(x, std::integral_constant<int, 0x140>()));   // row_mirror
-    if constexpr (L > 16) {
-        const unsigned v = __builtin_bit_cast(unsigned, x);
-        const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        x = op(__builtin_bit_cast(X, static_cast<unsigned>(both[0])), __builtin_bit_cast(X, static_cast<unsigned>(both[1])));
-    }
-    if constexpr (L > 32) {
-        const unsigned v = __builtin_bit_cast(unsigned, x);
-        const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        x = op(__builtin_bit_cast(X, static_cast<unsigned>(both[0])), __builtin_bit_cast(X, static_cast<unsigned>(both[1])));
-    }
-    return x;
-}
-template <int L>
-__device__ inline float lanes_max(float x) {
-    return over_lanes<L>(x, [](float a, float b) { return __builtin_fmaxf(a, b); });
-}
-template <int L>
-__device__ inline float lanes_sum(float x) {
-    return over_lanes<L>(x, [](float a, float b) { return a + b; });
-}
-template <int L>
-__device__ inline unsigned lanes_max(unsigned x) {
-    return over_lanes<L>(x, [](unsigned a, unsigned b) { return a > b ? a : b; });
-}
-template <int L>
-__device__ inline unsigned lanes_min(unsigned x) {
-    return over_lanes<L>(x, [](unsigned a, unsigned b) { return a < b ? a : b; });
-}
 
 // The expert whose logit is a lane's i-th: 16 bytes of neighbours to a lane, then the next lane's, so that a load of the wave is one
 // piece.  How wide the loads really are changes nothing in it, so that sums do not depend on where a row starts.

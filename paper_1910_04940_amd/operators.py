@@ -6,16 +6,19 @@ another; a result goes into the tensor that is given for it.  stream: hipStream_
 from __future__ import annotations
 
 import ctypes as C
+import math
 from typing import Optional, Sequence, Tuple
 
+import numpy as np
+
 from . import binding
-from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_INT32, BLINK_INT64, _check
+from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_FP8, BLINK_INT32, BLINK_INT64, _check
 
 # Five steps (a, b, c) that move every singular value above 0.003 to between 0.68 and 1.21.
 BLINK_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
 
 _CODES = {"torch.float32": BLINK_FP32, "torch.bfloat16": BLINK_BF16, "torch.float16": BLINK_FP16, "torch.int32": BLINK_INT32,
-          "torch.int64": BLINK_INT64, "torch.bool": -1, "torch.uint8": -1}
+          "torch.int64": BLINK_INT64, "torch.float8_e4m3fn": BLINK_FP8, "torch.bool": -1, "torch.uint8": -1}
 _seen = {}   # a tensor's dtype -> its code, once asked
 _operators = binding._operators
 
@@ -220,3 +223,103 @@ def blink_orthogonal_step(weights, momentum, grad, weights_out, momentum_out, wo
         eps, rate, decay, space, size, stream)
     if status:
         _check(status, "blink_orthogonal_step")
+
+
+class Update:
+    """Owns a blink_update_t handle, and the tensors whose addresses are in it."""
+
+    def __init__(self, handle: int, tensors):
+        self._h = C.c_void_p(handle)
+        self._address = handle
+        self.tensors = tensors
+
+    def __del__(self):
+        if getattr(self, "_h", None) and binding._lib is not None:
+            binding._lib.blink_update_free(self._h)
+            self._h = self._address = None
+
+
+def blink_make_update(grads: Sequence, weights: Optional[Sequence] = None, moments1: Optional[Sequence] = None, moments2: Optional[Sequence] = None,
+                      masters: Optional[Sequence] = None, scales1: Optional[Sequence] = None, scales2: Optional[Sequence] = None,
+                      rates: Optional[Sequence[float]] = None, decays: Optional[Sequence[float]] = None) -> Update:
+    """The tensors that an optimiser changes, a place in every list for each (None: it has none): contiguous, on one device.  Where weights are
+    None the gradient counts in the norm only.  Moments: float32, or float8_e4m3fn with float32 scales, one for every 256 elements."""
+    lists = {"grad": grads, "weights": weights, "master": masters, "moment1": moments1, "moment2": moments2, "scale1": scales1, "scale2": scales2}
+    n = len(grads)
+    if n == 0:
+        raise ValueError("a list of tensors has at least one")
+    for name, values in (*lists.items(), ("rates", rates), ("decays", decays)):
+        if values is not None and len(values) != n:
+            raise ValueError(f"{name}: {n} tensors, {len(values)} places")
+    table = np.zeros(n, binding.UPDATE_TENSOR_DTYPE)
+    device = None if grads[0] is None else grads[0].device
+    for i, row in enumerate(table):
+        got = {name: values[i] for name, values in lists.items() if values is not None and values[i] is not None}
+        if "grad" not in got:
+            raise ValueError("every tensor has a gradient")
+        many = got["grad"].numel()
+        eight = "moment1" in got and _code(got["moment1"], "moment1", (BLINK_FP32, BLINK_FP8)) == BLINK_FP8
+        for name, t in got.items():
+            scale = name.startswith("scale")
+            kind = _code(t, name, _FLOAT if name in ("grad", "weights") else (BLINK_FP8 if eight else BLINK_FP32,) if name.startswith("moment") else _FP32)
+            if not t.is_contiguous() or t.numel() != (-(-many // 256) if scale else many):
+                raise ValueError(f"{name} of tensor {i} must be contiguous, of {-(-many // 256) if scale else many} elements: got {tuple(t.shape)}")
+            if t.device != device:
+                raise ValueError(f"{name} of tensor {i} is on another device")
+            row[name] = t.data_ptr() if t.numel() else 0
+            if name == "grad":
+                row["grad_type"] = kind
+            elif name == "weights":
+                row["weight_type"] = kind
+        if "weights" in got:
+            for name in ("moment1", "moment2", "scale1", "scale2"):
+                if (name in got) != (eight or name.startswith("moment")):
+                    raise ValueError(f"tensor {i}: weights have moments, moments in 8 bits scales")
+            row["moment_type"] = BLINK_FP8 if eight else BLINK_FP32
+            if many == 0:   # (nothing to step; an address is what says that there are weights)
+                for name in got:
+                    row[name] = 0
+        elif len(got) > 1:
+            raise ValueError(f"tensor {i} has no weights that its other tensors go with")
+        row["elements"] = many
+        row["rate"], row["decay"] = 1.0 if rates is None else rates[i], 0.0 if decays is None else decays[i]
+    out = C.c_void_p()
+    import torch
+    with torch.cuda.device(device):
+        _check(binding.lib().blink_make_update(table.ctypes.data, n, C.byref(out)), "blink_make_update")
+    return Update(out.value, [t for values in lists.values() if values is not None for t in values])
+
+
+def blink_gradient_norm_workspace(update: Update) -> int:
+    return binding.lib().blink_gradient_norm_workspace(update._h)
+
+
+def blink_gradient_norm(update: Update, norm, workspace, max_norm: float = math.inf, factor: float = 1.0, step=None, stream: int = 0) -> None:
+    """norm = (length of all gradients times factor, what a step is to multiply them by); step, an int32, is counted up where all are finite."""
+    status = _usual("gradient_norm", update, norm, workspace, max_norm, factor, step, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_gradient_norm")
+    space, size = _space(workspace)
+    status = (binding._lib or binding.lib()).blink_gradient_norm(
+        update._h, max_norm, factor, _whole(norm, "norm", _FP32, (2,)), None if step is None else _whole(step, "step", _INT32, (1,)), space, size, stream)
+    if status:
+        _check(status, "blink_gradient_norm")
+
+
+def blink_adamw_step(update: Update, step, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, scale=None, rate=None, seed: int = 0,
+                     stream: int = 0) -> None:
+    """A step of AdamW on the tensors of `update`, in place; step: which one, from 1 on.  scale, rate: one float32 each that gradients and lr are multiplied by."""
+    status = _usual("adamw_step", update, step, lr, beta1, beta2, eps, scale, rate, seed, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_adamw_step")
+    if not 0 <= seed < 1 << 32:
+        raise ValueError("seed has 32 bits")
+    status = (binding._lib or binding.lib()).blink_adamw_step(
+        update._h, _whole(step, "step", _INT32, (1,)), lr, beta1, beta2, eps, None if scale is None else _whole(scale, "scale", _FP32, (1,)),
+        None if rate is None else _whole(rate, "rate", _FP32, (1,)), seed, stream)
+    if status:
+        _check(status, "blink_adamw_step")
