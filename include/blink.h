@@ -86,6 +86,8 @@ typedef enum {
  * larger under the IEEE total order (-0 below +0), so the result does not
  * depend on the order of the operands. */
 typedef enum { BLINK_SUM = 0, BLINK_PROD = 1, BLINK_MIN = 2, BLINK_MAX = 3 } blink_redop_t;
+/* What a logit's score is: 1 / (1 + e^-x) by itself, or its part of the token's softmax. */
+typedef enum { BLINK_SIGMOID = 0, BLINK_SOFTMAX = 1 } blink_scores_t;
 typedef enum { BLINK_STEP_REDUCE = 0, BLINK_STEP_COPY = 1 } blink_step_kind_t;
 
 /* Which of a tree's transfers are written to the rank buffers.  The result is
@@ -548,6 +550,29 @@ blink_status_t blink_route_gradient(const void* logits, blink_dtype_t dtype, siz
                                     const uint8_t* keep, int k, int normalize, const int32_t* chosen,
                                     const float* grad_weights, const int32_t* counts, const float* grad_loss,
                                     float balance, float z, void* grad_logits, size_t grad_stride, void* stream);
+
+/* A router that is balanced by a bias: p the scores of a token's logits, a = p + bias (null: 0).  The experts lie in `groups` (1 to 64) of the
+ * same size; the kept_groups with the largest scores stay, a group's score being the sum of its two largest a (its one where no
+ * other is left).  The k (<= experts of the groups that stay) largest a in them are chosen, as scores in 64 bits would have it, the lowest
+ * index first among equals (groups too); not a logit of -inf, nor one whose bias is -inf or NaN.
+ *   keep      null, or a byte per token: where it is 0 the token is left out of everything
+ *   chosen    [n_tokens][k], the largest a first; -1 where none is left, and for tokens left out
+ *   weights   [n_tokens][k]: scale * p of the chosen (the bias is not in it), p divided by its sum over them if normalize; 0 next to a -1
+ *   counts    [n_experts + 1]: tokens that chose each expert; last the tokens with a chosen one.  They add up over ranks: blink_allreduce on INT32.
+ * A token that is kept with a NaN among its logits, or with softmax +inf, has no chosen experts and weights that are NaN. */
+size_t blink_route_biased_workspace(size_t n_tokens, int n_experts);
+blink_status_t blink_route_biased(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride,
+                                  const uint8_t* keep, const float* bias, int k, int groups, int kept_groups,
+                                  blink_scores_t scores, int normalize, float scale, int32_t* chosen, float* weights,
+                                  int32_t* counts, void* workspace, size_t workspace_bytes, void* stream);
+/* bias_out[e] = bias[e] + rate where counts[e] (over all ranks) is below the experts' mean, - rate where above.  In place: bias_out may be bias. */
+blink_status_t blink_route_bias(const int32_t* counts, const float* bias, int n_experts, float rate, float* bias_out, void* stream);
+/* Gradient of the logits from that of the weights, grad_weights [n_tokens][k]; the choice, and so the bias, has none.  Zeros for tokens
+ * without chosen experts.  chosen as blink_route_biased left it, the other arguments as they went in. */
+blink_status_t blink_route_biased_gradient(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride,
+                                           const uint8_t* keep, int k, blink_scores_t scores, int normalize, float scale,
+                                           const int32_t* chosen, const float* grad_weights, void* grad_logits,
+                                           size_t grad_stride, void* stream);
 
 /* Each of `batch` matrices (rows x cols) moved towards the nearest matrix with orthonormal rows
  * (columns, if there are fewer): X = M / (|M| + eps), |.| the Frobenius norm, then for each of the `steps` (1 to 64)

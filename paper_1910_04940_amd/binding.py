@@ -23,6 +23,7 @@ BLINK_OK, BLINK_EINVAL, BLINK_EDISCONNECTED, BLINK_ENOMEM, BLINK_EMISMATCH, BLIN
 BLINK_INT32, BLINK_FP32, BLINK_BF16, BLINK_FP16, BLINK_INT64, BLINK_FP8 = 0, 1, 2, 3, 4, 5
 BLINK_OP_BROADCAST, BLINK_OP_ALLREDUCE, BLINK_OP_REDUCE, BLINK_OP_ALLGATHER, BLINK_OP_GATHER = 0, 1, 2, 3, 4
 BLINK_SUM, BLINK_PROD, BLINK_MIN, BLINK_MAX = 0, 1, 2, 3
+BLINK_SIGMOID, BLINK_SOFTMAX = 0, 1
 BLINK_STEP_REDUCE, BLINK_STEP_COPY = 0, 1
 BLINK_FUSE_EDGE, BLINK_FUSE_NODE, BLINK_FUSE_TREE = 0, 1, 2
 
@@ -63,7 +64,7 @@ EXPORTS = [
     "blink_embedding", "blink_embedding_gradient_workspace", "blink_embedding_gradient", "blink_route_workspace",
     "blink_route", "blink_route_loss", "blink_route_gradient", "blink_orthogonalize_workspace", "blink_orthogonalize",
     "blink_orthogonal_step", "blink_make_update", "blink_update_free", "blink_gradient_norm_workspace", "blink_gradient_norm",
-    "blink_adamw_step",
+    "blink_adamw_step", "blink_route_biased_workspace", "blink_route_biased", "blink_route_bias", "blink_route_biased_gradient",
 ]
 
 
@@ -179,13 +180,16 @@ def lib() -> C.CDLL:
     L.blink_route_gradient.argtypes = [vp, i, z, i, z, vp, i, i, vp, vp, vp, vp, f, f, vp, z, vp]
     L.blink_orthogonalize.argtypes = [vp, i, z, z, z, z, z, C.POINTER(f), i, f, vp, z, z, vp, z, vp]
     L.blink_orthogonal_step.argtypes = [vp, vp, vp, vp, vp, i, z, z, z, f, i, C.POINTER(f), i, f, f, f, vp, z, vp]
+    L.blink_route_biased.argtypes = [vp, i, z, i, z, vp, vp, i, i, i, i, i, f, vp, vp, vp, vp, z, vp]
+    L.blink_route_bias.argtypes = [vp, vp, i, f, vp, vp]
+    L.blink_route_biased_gradient.argtypes = [vp, i, z, i, z, vp, i, i, i, f, vp, vp, vp, z, vp]
     L.blink_make_update.argtypes = [vp, i, C.POINTER(vp)]
     L.blink_update_free.argtypes = [vp]
     L.blink_update_free.restype = None
     d = C.c_double
     L.blink_gradient_norm.argtypes = [vp, d, d, vp, vp, vp, z, vp]
     L.blink_adamw_step.argtypes = [vp, vp, d, d, d, d, vp, vp, C.c_uint32, vp]
-    for name, sizes in (("gradient_norm", [vp]), ("embedding_gradient", [z, z, z]), ("route", [z, i]), ("orthogonalize", [z, z, z, i])):
+    for name, sizes in (("gradient_norm", [vp]), ("embedding_gradient", [z, z, z]), ("route", [z, i]), ("route_biased", [z, i]), ("orthogonalize", [z, z, z, i])):
         getattr(L, f"blink_{name}_workspace").argtypes = sizes
         getattr(L, f"blink_{name}_workspace").restype = z
     L.blink_strerror.argtypes = [C.c_int]
@@ -198,7 +202,8 @@ def lib() -> C.CDLL:
         for name in _at:
             _at[name] = C.cast(getattr(L, name), vp).value
         _call = _blinkcall.call
-        for name in ("embedding", "embedding_gradient", "route", "route_loss", "route_gradient", "gradient_norm", "adamw_step"):
+        for name in ("embedding", "embedding_gradient", "route", "route_loss", "route_gradient", "gradient_norm", "adamw_step",
+                     "route_biased", "route_bias", "route_biased_gradient"):
             _operators[name] = getattr(_blinkcall, name), C.cast(getattr(L, f"blink_{name}"), vp).value
     _lib = L
     return L

@@ -22,7 +22,7 @@ SOURCES = ["kernel_f32.hip", "kernel_i32.hip",
            "fold_once_f32_sum.hip", "fold_once_i32_sum.hip", "fold_once_f32_other.hip", "fold_once_i32_other.hip",
            "fold_once_f32_mid.hip", "fold_once_i32_mid.hip", "fold_once_copy.hip",
            "fold_f32_mid.hip", "fold_i32_mid.hip", "fold_copy.hip", "exec.hip",
-           "embedding.hip", "route.hip", "orthogonal.hip", "update.hip", "api_operators.cpp", "api.cpp", "pack.cpp", "schedule.cpp", "miad.cpp"]
+           "embedding.hip", "route.hip", "route_biased.hip", "orthogonal.hip", "update.hip", "api_operators.cpp", "api.cpp", "pack.cpp", "schedule.cpp", "miad.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-c",
     "-fno-gpu-flush-denormals-to-zero",      # fp32 subnormals are ordinary addends

@@ -8,7 +8,7 @@ namespace {
 
 constexpr size_t kMostTokens = 0x7fffffff, kMostDim = size_t{1} << 21, kMostSide = size_t{1} << 20, kMostBatch = 65535;
 constexpr size_t kMostElements = size_t{1} << 40;
-constexpr int kMostExperts = 1024, kMostSteps = 64, kMostTensors = 1 << 20;
+constexpr int kMostExperts = 1024, kMostGroups = 64, kMostSteps = 64, kMostTensors = 1 << 20;
 
 bool is_token(blink_dtype_t t) { return t == BLINK_INT32 || t == BLINK_INT64; }
 // A buffer of elements of `size` bytes; it may be null where it has none.
@@ -95,6 +95,43 @@ blink_status_t blink_route_gradient(const void* logits, blink_dtype_t dtype, siz
         return BLINK_EINVAL;
     return blink::route_gradient(logits, dtype, n_tokens, n_experts, stride, keep, k, normalize == 1, chosen, grad_weights, counts, grad_loss, balance, z,
                                  grad_logits, grad_stride, static_cast<hipStream_t>(stream));
+}
+
+size_t blink_route_biased_workspace(size_t n_tokens, int n_experts) {
+    if (n_tokens > kMostTokens || n_experts < 1 || n_experts > kMostExperts) return 0;
+    return blink::route_biased_workspace(n_tokens, n_experts);
+}
+
+blink_status_t blink_route_biased(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride, const uint8_t* keep, const float* bias,
+                                  int k, int groups, int kept_groups, blink_scores_t scores, int normalize, float scale, int32_t* chosen, float* weights,
+                                  int32_t* counts, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!blink::is_float(dtype) || n_tokens > kMostTokens || n_experts < 1 || n_experts > kMostExperts || groups < 1 || groups > kMostGroups ||
+        n_experts % groups != 0 || kept_groups < 1 || kept_groups > groups || k < 1 || k > n_experts / groups * kept_groups ||
+        stride < static_cast<size_t>(n_experts) || (scores != BLINK_SIGMOID && scores != BLINK_SOFTMAX) || (normalize != 0 && normalize != 1) ||
+        !std::isfinite(scale) || !buffer_ok(logits, n_tokens, blink::size_of(dtype)) || !blink::aligned(bias, 4) || !buffer_ok(chosen, n_tokens, 4) ||
+        !buffer_ok(weights, n_tokens, 4) || !buffer_ok(counts, 1, 4) ||
+        !workspace_ok(workspace, workspace_bytes, blink::route_biased_workspace(n_tokens, n_experts)))
+        return BLINK_EINVAL;
+    return blink::route_biased(logits, dtype, n_tokens, n_experts, stride, keep, bias, k, groups, kept_groups, scores == BLINK_SOFTMAX, normalize == 1, scale,
+                               chosen, weights, counts, workspace, static_cast<hipStream_t>(stream));
+}
+
+blink_status_t blink_route_bias(const int32_t* counts, const float* bias, int n_experts, float rate, float* bias_out, void* stream) {
+    if (n_experts < 1 || n_experts > kMostExperts || !std::isfinite(rate) || !buffer_ok(counts, 1, 4) || !buffer_ok(bias, 1, 4) || !buffer_ok(bias_out, 1, 4))
+        return BLINK_EINVAL;
+    return blink::route_bias(counts, bias, bias_out, n_experts, rate, static_cast<hipStream_t>(stream));
+}
+
+blink_status_t blink_route_biased_gradient(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride, const uint8_t* keep, int k,
+                                           blink_scores_t scores, int normalize, float scale, const int32_t* chosen, const float* grad_weights,
+                                           void* grad_logits, size_t grad_stride, void* stream) {
+    if (!blink::is_float(dtype) || n_tokens > kMostTokens || n_experts < 1 || n_experts > kMostExperts || k < 1 || k > n_experts ||
+        stride < static_cast<size_t>(n_experts) || grad_stride < static_cast<size_t>(n_experts) || (scores != BLINK_SIGMOID && scores != BLINK_SOFTMAX) ||
+        (normalize != 0 && normalize != 1) || !std::isfinite(scale) || !buffer_ok(logits, n_tokens, blink::size_of(dtype)) || !buffer_ok(chosen, n_tokens, 4) ||
+        !buffer_ok(grad_weights, n_tokens, 4) || !buffer_ok(grad_logits, n_tokens, blink::size_of(dtype)))
+        return BLINK_EINVAL;
+    return blink::route_biased_gradient(logits, dtype, n_tokens, n_experts, stride, keep, k, scores == BLINK_SOFTMAX, normalize == 1, scale, chosen,
+                                        grad_weights, grad_logits, grad_stride, static_cast<hipStream_t>(stream));
 }
 
 size_t blink_orthogonalize_workspace(size_t batch, size_t rows, size_t cols, blink_dtype_t dtype) {

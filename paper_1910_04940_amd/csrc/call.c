@@ -301,6 +301,54 @@ static PyObject* route_gradient(PyObject* self, PyObject* const* args, Py_ssize_
                                                 counts, up, balance, z, g.at, (size_t)g.stride, (void*)stream));
 }
 
+/* logits, k, chosen, weights, counts, workspace, bias, keep, groups, kept_groups, scores, normalize, scale, stream */
+static PyObject* route_biased(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(16);
+    matrix_t x;
+    Py_ssize_t size, n, e, counted;
+    void *chosen, *weights, *counts, *work, *bias = NULL, *keep = NULL;
+    int k, groups, kept, scores, normalize;
+    float scale;
+    USUAL(matrix(types, args[2], &x) && is_float(x.code) && x.cols < 0x7fffffff && small(args[3], &k));
+    n = x.rows;
+    e = x.cols;
+    counted = e + 1;
+    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && table(types, args[5], BLINK_FP32, n, k, &weights) &&
+          whole(types, args[6], BLINK_INT32, &counted, &counts) && space(args[7], &work, &size) &&
+          (args[8] == Py_None || whole(types, args[8], BLINK_FP32, &e, &bias)) && (args[9] == Py_None || whole(types, args[9], -1, &n, &keep)) &&
+          small(args[10], &groups) && small(args[11], &kept) && small(args[12], &scores) && truth(args[13], &normalize) && number(args[14], &scale));
+    RUN(((__typeof__(&blink_route_biased))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, bias, k, groups, kept,
+                                              (blink_scores_t)scores, normalize, scale, chosen, weights, counts, work, (size_t)size, (void*)stream));
+}
+
+/* counts, bias, bias_out, rate, stream */
+static PyObject* route_bias(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(7);
+    Py_ssize_t e = -1, counted;
+    void *counts, *bias, *out;
+    float rate;
+    USUAL(whole(types, args[3], BLINK_FP32, &e, &bias) && e < 0x7fffffff && (counted = e + 1) && whole(types, args[2], BLINK_INT32, &counted, &counts) &&
+          whole(types, args[4], BLINK_FP32, &e, &out) && number(args[5], &rate));
+    RUN(((__typeof__(&blink_route_bias))fn)(counts, bias, (int)e, rate, out, (void*)stream));
+}
+
+/* logits, k, chosen, grad_weights, grad_logits, keep, scores, normalize, scale, stream */
+static PyObject* route_biased_gradient(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    TAKES(12);
+    matrix_t x, g;
+    Py_ssize_t n;
+    void *chosen, *by_weight, *keep = NULL;
+    int k, scores, normalize;
+    float scale;
+    USUAL(matrix(types, args[2], &x) && is_float(x.code) && x.cols < 0x7fffffff && small(args[3], &k) && matrix(types, args[6], &g) && g.code == x.code &&
+          g.rows == x.rows && g.cols == x.cols);
+    n = x.rows;
+    USUAL(table(types, args[4], BLINK_INT32, n, k, &chosen) && table(types, args[5], BLINK_FP32, n, k, &by_weight) &&
+          (args[7] == Py_None || whole(types, args[7], -1, &n, &keep)) && small(args[8], &scores) && truth(args[9], &normalize) && number(args[10], &scale));
+    RUN(((__typeof__(&blink_route_biased_gradient))fn)(x.at, (blink_dtype_t)x.code, (size_t)x.rows, (int)x.cols, (size_t)x.stride, keep, k,
+                                                       (blink_scores_t)scores, normalize, scale, chosen, by_weight, g.at, (size_t)g.stride, (void*)stream));
+}
+
 /* update, norm, workspace, max_norm, factor, step, stream */
 static PyObject* gradient_norm(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
     TAKES(9);
@@ -332,6 +380,9 @@ static PyMethodDef methods[] = {
     {"route", (PyCFunction)(void (*)(void))route, METH_FASTCALL, NULL},
     {"route_loss", (PyCFunction)(void (*)(void))route_loss, METH_FASTCALL, NULL},
     {"route_gradient", (PyCFunction)(void (*)(void))route_gradient, METH_FASTCALL, NULL},
+    {"route_biased", (PyCFunction)(void (*)(void))route_biased, METH_FASTCALL, NULL},
+    {"route_bias", (PyCFunction)(void (*)(void))route_bias, METH_FASTCALL, NULL},
+    {"route_biased_gradient", (PyCFunction)(void (*)(void))route_biased_gradient, METH_FASTCALL, NULL},
     {"gradient_norm", (PyCFunction)(void (*)(void))gradient_norm, METH_FASTCALL, NULL},
     {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},

@@ -45,5 +45,15 @@ template <int L>
 __device__ inline unsigned lanes_min(unsigned x) {
     return over_lanes<L>(x, [](unsigned a, unsigned b) { return a < b ? a : b; });
 }
+template <int L>
+__device__ inline unsigned lanes_or(unsigned x) {
+    return over_lanes<L>(x, [](unsigned a, unsigned b) { return a | b; });
+}
+template <int L>
+__device__ inline double lanes_sum(double x) {
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
+    return x;
+}
 
 }  // namespace blink

@@ -1,4 +1,4 @@
-// What the operators around the collectives share (embedding.hip, route.hip, orthogonal.hip, update.hip): element types, wide
+// What the operators around the collectives share (embedding.hip, route.hip, route_biased.hip, orthogonal.hip, update.hip): element types, wide
 // loads, the launch.
 #pragma once
 #include <hip/hip_runtime.h>

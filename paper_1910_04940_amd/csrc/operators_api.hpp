@@ -1,4 +1,4 @@
-// What api_operators.cpp checks the arguments for (embedding.hip, route.hip, orthogonal.hip, update.hip).
+// What api_operators.cpp checks the arguments for (embedding.hip, route.hip, route_biased.hip, orthogonal.hip, update.hip).
 #pragma once
 #include "operators.hpp"
 
@@ -27,6 +27,15 @@ blink_status_t orthogonalize(const void* in, blink_dtype_t dtype, size_t batch, 
 blink_status_t orthogonal_step(const float* weights, float* weights_out, const float* momentum, float* momentum_out, const void* grad,
                                blink_dtype_t grad_type, size_t batch, size_t rows, size_t cols, float beta, bool nesterov, const float* coefficients,
                                int steps, float eps, float rate, float decay, void* workspace, hipStream_t stream);
+
+size_t route_biased_workspace(size_t tokens, int experts);
+blink_status_t route_biased(const void* logits, blink_dtype_t dtype, size_t tokens, int experts, size_t stride, const uint8_t* keep, const float* bias, int k,
+                            int expert_groups, int kept_groups, bool soft, bool normalize, float scale, int32_t* chosen, float* weights, int32_t* counts,
+                            void* workspace, hipStream_t stream);
+blink_status_t route_bias(const int32_t* counts, const float* bias, float* out, int experts, float rate, hipStream_t stream);
+blink_status_t route_biased_gradient(const void* logits, blink_dtype_t dtype, size_t tokens, int experts, size_t stride, const uint8_t* keep, int k, bool soft,
+                                     bool normalize, float scale, const int32_t* chosen, const float* grad_weights, void* out, size_t out_stride,
+                                     hipStream_t stream);
 
 blink_status_t make_update(const blink_update_tensor_t* tensors, int n, blink_update** out);
 void free_update(blink_update* u);

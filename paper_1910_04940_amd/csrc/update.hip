@@ -149,7 +149,9 @@ __device__ inline uint32_t to_eight(uint32_t z, uint32_t up) {
     constexpr uint32_t kNormal = 0x3c800000u;   // 2^-6
     const float y = __builtin_bit_cast(float, z);
     const uint32_t large = ((z + (up << 4 | 8)) >> 20) - 960;             // (exponents differ by 120, 3 bits of 23 stay)
-    const uint32_t small = static_cast<uint32_t>(y * 512.0f + (static_cast<float>(up) + 0.5f) * 0x1p-16f);
+    const float units = y * 512.0f;                                       // exact, as is what is left of it
+    const uint32_t down = static_cast<uint32_t>(units);
+    const uint32_t small = down + (units - static_cast<float>(down) >= 1.0f - (static_cast<float>(up) + 0.5f) * 0x1p-16f);
     const uint32_t code = z >= kNormal ? large : small;
     return code > 0x7e ? 0x7e : code;
 }
@@ -175,7 +177,7 @@ __device__ inline uint32_t encode(const float (&y)[4], const uint32_t (&up)[4], 
         return 0;
     }
     *scale = largest * (1.0f / 448.0f);
-    const float by = 448.0f / largest;
+    const float by = 1.0f / largest * 448.0f;
     uint32_t codes = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -12,7 +12,7 @@ from typing import Optional, Sequence, Tuple
 import numpy as np
 
 from . import binding
-from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_FP8, BLINK_INT32, BLINK_INT64, _check
+from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_FP8, BLINK_INT32, BLINK_INT64, BLINK_SIGMOID, BLINK_SOFTMAX, _check
 
 # Five steps (a, b, c) that move every singular value above 0.003 to between 0.68 and 1.21.
 BLINK_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
@@ -170,6 +170,73 @@ def blink_route_gradient(logits, k: int, chosen, counts, grad_logits, keep=None,
         stream)
     if status:
         _check(status, "blink_route_gradient")
+
+
+_SCORES = {"sigmoid": BLINK_SIGMOID, "softmax": BLINK_SOFTMAX}
+
+
+def _scores(name: str) -> int:
+    code = _SCORES.get(name)
+    if code is None:
+        raise ValueError(f"scores are {' or '.join(_SCORES)}: got {name!r}")
+    return code
+
+
+def blink_route_biased_workspace(n_tokens: int, n_experts: int) -> int:
+    return binding.lib().blink_route_biased_workspace(n_tokens, n_experts)
+
+
+def blink_route_biased(logits, k: int, chosen, weights, counts, workspace, bias=None, keep=None, groups: int = 1, kept_groups: int = 1, scores: str = "sigmoid",
+                       normalize: bool = False, scale: float = 1.0, stream: int = 0) -> None:
+    """The k experts with the largest scores + bias of every token, in the kept_groups best of its groups; weights from the scores alone; per-expert counts."""
+    code = _scores(scores)
+    status = _usual("route_biased", logits, k, chosen, weights, counts, workspace, bias, keep, groups, kept_groups, code, normalize, scale, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route_biased")
+    at, kind, n, experts, stride = _rows(logits, "logits", _FLOAT)
+    space, size = _space(workspace)
+    status = (binding._lib or binding.lib()).blink_route_biased(
+        at, kind, n, experts, stride, None if keep is None else _whole(keep, "keep", _BYTE, (n,)), None if bias is None else _whole(bias, "bias", _FP32, (experts,)),
+        k, groups, kept_groups, code, 1 if normalize else 0, scale, _whole(chosen, "chosen", _INT32, (n, k)), _whole(weights, "weights", _FP32, (n, k)),
+        _whole(counts, "counts", _INT32, (experts + 1,)), space, size, stream)
+    if status:
+        _check(status, "blink_route_biased")
+
+
+def blink_route_bias(counts, bias, bias_out, rate: float, stream: int = 0) -> None:
+    """The bias a step up where an expert has fewer than the mean of the counts (over all ranks), down where more.  bias_out may be bias."""
+    status = _usual("route_bias", counts, bias, bias_out, rate, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route_bias")
+    experts = bias.numel()
+    status = (binding._lib or binding.lib()).blink_route_bias(_whole(counts, "counts", _INT32, (experts + 1,)), _whole(bias, "bias", _FP32, (experts,)), experts,
+                                                              rate, _whole(bias_out, "bias_out", _FP32, (experts,)), stream)
+    if status:
+        _check(status, "blink_route_bias")
+
+
+def blink_route_biased_gradient(logits, k: int, chosen, grad_weights, grad_logits, keep=None, scores: str = "sigmoid", normalize: bool = False,
+                                scale: float = 1.0, stream: int = 0) -> None:
+    """Gradient of the logits through the weights of blink_route_biased."""
+    code = _scores(scores)
+    status = _usual("route_biased_gradient", logits, k, chosen, grad_weights, grad_logits, keep, code, normalize, scale, stream)
+    if status == 0:
+        return
+    if status is not None:
+        _check(status, "blink_route_biased_gradient")
+    at, kind, n, experts, stride = _rows(logits, "logits", _FLOAT)
+    to, out_kind, _, _, out_stride = _rows(grad_logits, "grad_logits", _FLOAT, n, experts)
+    if out_kind != kind:
+        raise ValueError("grad_logits must have the type of logits")
+    status = (binding._lib or binding.lib()).blink_route_biased_gradient(
+        at, kind, n, experts, stride, None if keep is None else _whole(keep, "keep", _BYTE, (n,)), k, code, 1 if normalize else 0, scale,
+        _whole(chosen, "chosen", _INT32, (n, k)), _whole(grad_weights, "grad_weights", _FP32, (n, k)), to, out_stride, stream)
+    if status:
+        _check(status, "blink_route_biased_gradient")
 
 
 def _coefficients(steps: Sequence[Sequence[float]]):
