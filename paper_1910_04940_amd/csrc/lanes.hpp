@@ -59,5 +59,37 @@ __device__ inline double lanes_sum(double x) {
     for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
     return x;
 }
+// The same over a wave for values of more than 32 bits, whole words of them.
+template <typename X, typename F>
+__device__ inline X over_wave(X x, F op) {
+    constexpr int kWords = sizeof(X) / 4;
+    struct Words {
+        unsigned w[kWords];
+    };
+    const auto moved = [&](auto control) {
+        Words y = __builtin_bit_cast(Words, x);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) y.w[i] = __builtin_amdgcn_update_dpp(0, static_cast<int>(y.w[i]), decltype(control)::value, 0xf, 0xf, true);
+        return __builtin_bit_cast(X, y);
+    };
+    x = op(x, moved(std::integral_constant<int, 0xB1>()));
+    x = op(x, moved(std::integral_constant<int, 0x4E>()));
+    x = op(x, moved(std::integral_constant<int, 0x141>()));
+    x = op(x, moved(std::integral_constant<int, 0x140>()));
+    const auto halves = [&](auto swap) {
+        const Words y = __builtin_bit_cast(Words, x);
+        Words a, b;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const auto both = swap(y.w[i]);
+            a.w[i] = both[0];
+            b.w[i] = both[1];
+        }
+        x = op(__builtin_bit_cast(X, a), __builtin_bit_cast(X, b));
+    };
+    halves([](unsigned v) { return __builtin_amdgcn_permlane16_swap(v, v, false, false); });
+    halves([](unsigned v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); });
+    return x;
+}
 
 }  // namespace blink

@@ -12,6 +12,7 @@
 //
 // The choice is that of scores in 64 bits.  L lanes hold a token, N logits each (see route.hpp).
 #include <algorithm>
+#include <array>
 #include <type_traits>
 
 #include "operators_api.hpp"
@@ -38,14 +39,14 @@ struct Biased {
     int32_t* counts;       // of the result, or [workgroup][experts + 1]
     uint32_t* later;       // [workgroup][room]: tokens whose choice in 32 bits is not sure; null: none
     uint32_t* left;        // [workgroup]: how many those are
-    uint32_t room;
+    uint32_t room, lists;
 };
 
 // What the weights of a token's chosen are made of: p times a factor that is the same for all of them and keeps them in range.
 //   sigmoid: e^(x - c) / (1 + e^x), c the largest chosen x if that is below 0;  softmax: e^(x - c), c the largest
 __device__ inline float part_of(bool soft, float x, float c) {
-    if (soft) return expf(x - c);
-    return x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - c) / (1.0f + expf(x));
+    const float up = power((x > 0.0f && !soft ? 0.0f : x) - c);
+    return soft ? up : up * __builtin_amdgcn_rcpf(1.0f + power(-__builtin_fabsf(x)));
 }
 
 // Weights of a token's chosen, and what they add to the counts; chosen(j): the j-th, for the j of this lane.  most, sum: of the whole softmax.
@@ -53,19 +54,28 @@ __device__ inline float part_of(bool soft, float x, float c) {
 template <typename T, int L, typename F>
 __device__ inline void weigh(const Biased& a, uint64_t token, const T* row, int lane, float most, float sum, int32_t* count, F chosen) {
     float* const weights = a.weights + token * a.k;
-    float c = 0.0f, all = 1.0f;
+    const bool one = a.k <= L;   // to a lane
+    int e = -1;
+    float x = -kInf, part = 0.0f, c = 0.0f, all = 1.0f;
+    const auto take = [&](int j) {
+        e = j < a.k ? chosen(j) : -1;
+        x = e >= 0 ? static_cast<float>(row[e]) : -kInf;
+    };
+    take(lane);
     if (a.normalize) {
-        c = -kInf;
-        for (int j = lane; j < a.k; j += L) {
-            const int e = chosen(j);
-            if (e >= 0) c = __builtin_fmaxf(c, static_cast<float>(row[e]));
+        c = x;
+        for (int j = lane + L; j < a.k; j += L) {
+            take(j);
+            c = __builtin_fmaxf(c, x);
         }
         c = lanes_max<L>(c);
         if (!a.soft) c = __builtin_fminf(c, 0.0f);
-        all = 0.0f;
-        for (int j = lane; j < a.k; j += L) {
-            const int e = chosen(j);
-            if (e >= 0) all += part_of(a.soft, static_cast<float>(row[e]), c);
+        if (!one) take(lane);
+        part = e >= 0 ? part_of(a.soft, x, c) : 0.0f;
+        all = part;
+        for (int j = lane + L; j < a.k; j += L) {
+            take(j);
+            if (e >= 0) all += part_of(a.soft, x, c);
         }
         all = lanes_sum<L>(all);
     } else if (a.soft) {
@@ -73,27 +83,14 @@ __device__ inline void weigh(const Biased& a, uint64_t token, const T* row, int 
         all = sum;
     }
     for (int j = lane; j < a.k; j += L) {
-        const int e = chosen(j);
-        weights[j] = e < 0 ? 0.0f : a.scale * (part_of(a.soft, static_cast<float>(row[e]), c) / all);
+        if (!one) take(j);
+        if (!one || !a.normalize) part = part_of(a.soft, x, c);
+        weights[j] = e < 0 ? 0.0f : a.scale * (part / all);
         if (e >= 0) atomicAdd(&count[e], 1);
         if (e >= 0 && j == 0) atomicAdd(&count[a.experts], 1);
     }
 }
 
-template <int L, int N>
-__device__ inline bool any_nan(const float (&x)[N]) {
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < N; i += 2) nan |= __builtin_isunordered(x[i], x[i + 1]);
-    return lanes_or<L>(static_cast<unsigned>(nan));
-}
-template <int L, int N>
-__device__ inline float largest(const float (&x)[N]) {
-    float m = -kInf;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = __builtin_fmaxf(m, x[i]);
-    return lanes_max<L>(m);
-}
 template <int L>
 __device__ inline void choose_none(const Biased& a, uint64_t token, int lane) {
     for (int j = lane; j < a.k; j += L) {
@@ -103,28 +100,40 @@ __device__ inline void choose_none(const Biased& a, uint64_t token, int lane) {
 }
 
 // ---- the choice in 64 bits ----------------------------------------------------------------------------------------------------
-constexpr int kMostExact = 8;   // tokens of a call that are all chosen this way
+// A wave for each of the few tokens that two workgroups leave: so all of the kernel's workgroups are there at once (262144 x 256, 0.8 % of the tokens: 19 us,
+// 28 with a workgroup of four or eight waves to a list).
+constexpr int kExactThreads = 512;
+constexpr uint32_t kLists = 2;
+constexpr int kMostExact = 8;        // tokens of a call that are all chosen this way
 
+// The largest of a wave's lanes; the two largest of all that its lanes hold (pairs that stand for different numbers).
 __device__ inline double wave_max(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = __builtin_fmax(x, __shfl_xor(x, d));
-    return x;
+    return over_wave(x, [](double a, double b) { return __builtin_fmax(a, b); });
+}
+struct Two64 {
+    double first = -kInf64, second = -kInf64;
+};
+__device__ inline Two64 joined(Two64 a, Two64 b) {
+    return {__builtin_fmax(a.first, b.first), __builtin_fmax(__builtin_fmin(a.first, b.first), __builtin_fmax(a.second, b.second))};
 }
 
 // A wave to a token, N experts to a lane, expert 64 i + lane the i-th: for the tokens that a workgroup of route_biased_choose left in its list, for calls of a
 // few tokens and for k above kMostFast.
 template <typename T, int N>
-__global__ __launch_bounds__(kThreads) void route_biased_exact(const Biased a) {
+__global__ __launch_bounds__(kExactThreads) void route_biased_exact(const Biased a) {
     __shared__ int32_t count[64 * N + 1];
+    __shared__ double sums[kExactThreads / 64][64 * N];
     const int t = threadIdx.x, lane = t & 63;
-    const uint32_t* const list = a.later ? a.later + static_cast<uint64_t>(blockIdx.x) * a.room : nullptr;
-    const uint64_t n = list ? a.left[blockIdx.x] : a.tokens;
+    const uint32_t first = blockIdx.x * kLists;   // of its lists, whose tokens come one list after the other
+    const uint32_t* const list = a.later ? a.later + static_cast<uint64_t>(first) * a.room : nullptr;
+    const uint32_t mine = list ? a.left[first] : 0;
+    const uint64_t n = list ? mine + (first + 1 < a.lists ? a.left[first + 1] : 0) : a.tokens;
     if (list && n == 0) return;
-    for (int i = t; i <= a.experts; i += kThreads) count[i] = 0;
+    for (int i = t; i <= a.experts; i += kExactThreads) count[i] = 0;
     __syncthreads();
-    const uint64_t wave = (list ? 0 : blockIdx.x) * (kThreads / 64) + t / 64, step = (list ? 1 : gridDim.x) * (kThreads / 64);
+    const uint64_t wave = (list ? 0 : blockIdx.x) * (kExactThreads / 64) + t / 64, step = (list ? 1 : gridDim.x) * (kExactThreads / 64);
     for (uint64_t at = wave; at < n; at += step) {
-        const uint64_t token = list ? list[at] : at;
+        const uint64_t token = list ? list[at < mine ? at : a.room + (at - mine)] : at;
         const bool keep = !a.keep || a.keep[token];
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         int32_t* const chosen = a.chosen + token * a.k;
@@ -146,59 +155,49 @@ __global__ __launch_bounds__(kThreads) void route_biased_exact(const Biased a) {
             choose_none<64>(a, token, lane);
             continue;
         }
-        if (a.soft) {
-            most = lanes_max<64>(most);
-            const double from = most == -kInf ? 0.0 : most;
-            double s = 0.0;
+        if (a.soft) most = lanes_max<64>(most);
+        const double from = !a.soft || most == -kInf ? 0.0 : most;
+        double all = 0.0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[i] = exp(x[i] - from);
-                s += v[i];
-            }
-            s = lanes_sum<64>(s);
-            sum = static_cast<float>(s);
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] /= s;
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = 1.0 / (1.0 + exp(-static_cast<double>(x[i])));
+        for (int i = 0; i < N; ++i) {   // (one exponential for both: its code is what takes long to come)
+            v[i] = exp(a.soft ? x[i] - from : -static_cast<double>(x[i]));
+            all += v[i];
         }
+        all = a.soft ? lanes_sum<64>(all) : 1.0;
+        sum = static_cast<float>(all);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int e = 64 * i + lane;
-            const double y = v[i] + (a.bias && e < a.experts ? static_cast<double>(a.bias[e]) : 0.0);
+            const double p = (a.soft ? v[i] : 1.0) / (a.soft ? all : 1.0 + v[i]);
+            const double y = p + (a.bias && e < a.experts ? static_cast<double>(a.bias[e]) : 0.0);
             v[i] = x[i] > -kInf && y > -kInf64 ? y : -kInf64;   // (a bias of -inf or NaN: never)
         }
         if (a.groups > 1) {
             const int size = a.experts / a.groups;
-            double score = -kInf64;   // of group `lane`
-            for (int g = 0; g < a.groups; ++g) {
-                double first = -kInf64, second = -kInf64;
+            // Q lanes to a group, which look at its sums in turn
+            int Q = 1;
+            while (2 * Q * a.groups <= 64) Q *= 2;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int e = 64 * i + lane - g * size;
-                    const double y = e >= 0 && e < size ? v[i] : -kInf64;
-                    second = __builtin_fmax(second, __builtin_fmin(first, y));
-                    first = __builtin_fmax(first, y);
-                }
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const double f = __shfl_xor(first, d), s = __shfl_xor(second, d);
-                    second = __builtin_fmax(__builtin_fmin(first, f), __builtin_fmax(second, s));
-                    first = __builtin_fmax(first, f);
-                }
-                score = lane == g ? (second > -kInf64 ? first + second : first) : score;
-            }
+            for (int i = 0; i < N; ++i) sums[t / 64][64 * i + lane] = v[i];
+            wave_sync();
+            Two64 two;
+            if (lane / Q < a.groups)
+                for (int i = lane % Q; i < size; i += Q) two = joined(two, {sums[t / 64][lane / Q * size + i], -kInf64});
+            for (int d = 1; d < Q; d *= 2) two = joined(two, {__shfl_xor(two.first, d), __shfl_xor(two.second, d)});
+            double score = two.second > -kInf64 ? two.first + two.second : two.first;   // of group lane / Q, then of group `lane`
+            score = __shfl(score, lane * Q & 63);
+            wave_sync();
             int before = 0;
             for (int h = 0; h < a.groups; ++h) {
                 const double other = __shfl(score, h);
-                before += other > score || (other == score && h < lane);
+                before += other > score || (other == score && h < lane);   // (the same for lanes past the last group, which nobody asks)
             }
             const uint64_t stay = __ballot(lane < a.groups && before < a.kept);
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (!(stay >> ((64 * i + lane) / size & 63) & 1)) v[i] = -kInf64;
         }
+        int own = -1;   // the lane-th
         for (int j = 0; j < a.k; ++j) {
             double best = v[0];
 #pragma unroll
@@ -213,13 +212,14 @@ __global__ __launch_bounds__(kThreads) void route_biased_exact(const Biased a) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (64 * i + lane == at) v[i] = -kInf64;
+            own = j == lane ? at : own;
             if (j % 64 == lane) chosen[j] = at;
         }
-        weigh<T, 64>(a, token, row, lane, most, sum, count, [&](int j) { return chosen[j]; });   // (each lane its own)
+        weigh<T, 64>(a, token, row, lane, most, sum, count, [&](int j) { return j == lane ? own : chosen[j]; });   // (each lane its own)
     }
     __syncthreads();
-    int32_t* const counts = a.counts + static_cast<uint64_t>(blockIdx.x) * (a.experts + 1);
-    for (int i = t; i <= a.experts; i += kThreads) counts[i] = (list ? counts[i] : 0) + count[i];
+    int32_t* const counts = a.counts + static_cast<uint64_t>(list ? first : blockIdx.x) * (a.experts + 1);
+    for (int i = t; i <= a.experts; i += kExactThreads) counts[i] = (list ? counts[i] : 0) + count[i];
 }
 
 // ---- the choice in 32 bits, where it is sure --------------------------------------------------------------------------------
@@ -227,58 +227,68 @@ __global__ __launch_bounds__(kThreads) void route_biased_exact(const Biased a) {
 // 1.5 * 2^-23 s for the sum and the reciprocal; s (1 - s) |x| < 0.224 and s < 1 make 1.92 * 2^-23.
 // Of a softmax by kSoftmaxOff times the largest p: 2.5 |x - m| 2^-24 of p for its power, whose p |x - m| is below 0.37 of the largest, and 47 * 2^-24 for
 // the sum (1024 numbers, their mean |x - m| at most ln 1024; 22 additions on the way), its reciprocal and product.
-// Keys: sums with the bias whose lowest four bits are the place in the lane, and of groups whose lowest six are the group: a key is off by 2^-19, or
-// 2^-17, of itself, and no two of a lane, or of a token's groups, are the same.  A token is sure if no two neighbours in the order of its first k + 1, nor the last group
-// that stays and the first that does not, are nearer than the sum of all that.
-constexpr float kSigmoidOff = 0x1p-21f, kSoftmaxOff = 0x1p-18f;
-constexpr float kNone = -1e38f;          // below every key; its sums are numbers still
-constexpr float kLargeBias = 1e30f;      // larger ones (but -inf) leave everything to the 64 bits
+// The largest |bias|, w, is added to all, so that sums are not negative and compare as whole numbers do; they are off by (1 + 4 w) 2^-24 for that.  Their
+// lowest four bits give way to the place in the lane (a key is off by 2^-19 of itself), those of groups, sums of two, their lowest six to the group (2^-17).
+// A token is sure if no two neighbours in the order of its first k + 1, nor the last group that stays and the first that does not, are nearer than the
+// sum of all that.
+constexpr float kSigmoidOff = 0x1p-22f, kSoftmaxOff = 0x1p-18f;
+constexpr float kLargeBias = 1e37f;      // larger ones (but -inf) leave everything to the 64 bits
 constexpr int kMostFast = 16;            // k
+// No sum: below 0, and of no two lanes the same, so that one lane has the largest even then.
+__device__ inline int32_t none_of(int lane) { return static_cast<int32_t>(0xbf800000u) | lane << 4; }
+// A bias that makes it so: what is added to it is lost.
+__device__ inline float no_bias(int lane) { return __builtin_bit_cast(float, 0xf0000000u | static_cast<uint32_t>(lane) << 4); }
 
-__device__ inline float key_of(float v, uint32_t bits, uint32_t place) {
-    return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) & ~bits) | place);
-}
-__device__ inline uint32_t place_of(float key, uint32_t bits) { return __builtin_bit_cast(uint32_t, key) & bits; }
-__device__ inline float pick(bool first, float a, float b) { return first ? a : b; }   // (of values: of places would keep them in memory)
-__device__ inline void order(float& a, float& b) {   // a the larger
-    const float x = a, y = b;
-    a = __builtin_fmaxf(x, y);
-    b = __builtin_fminf(x, y);
+__device__ inline int32_t bits_of(float x) { return __builtin_bit_cast(int32_t, x); }
+__device__ inline float float_of(int32_t x) { return __builtin_bit_cast(float, x); }
+__device__ inline int32_t max_of(int32_t a, int32_t b) { return a > b ? a : b; }
+__device__ inline int32_t min_of(int32_t a, int32_t b) { return a < b ? a : b; }
+__device__ inline int32_t pick(bool first, int32_t a, int32_t b) { return first ? a : b; }   // (of values: of places would keep them in memory)
+__device__ inline void order(int32_t& a, int32_t& b) {   // a the larger
+    const int32_t x = a, y = b;
+    a = max_of(x, y);
+    b = min_of(x, y);
 }
 // Eight, the largest first (Batcher's odd-even merge sort); the same of eight that rise and then fall, or the other way round.
-__device__ inline void sort8(float (&k)[8]) {
+__device__ inline void sort8(int32_t (&k)[8]) {
     constexpr int pair[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
                                  {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
 #pragma unroll
     for (int e = 0; e < 19; ++e) order(k[pair[e][0]], k[pair[e][1]]);
 }
-__device__ inline void merge8(float (&k)[8]) {
+__device__ inline void merge8(int32_t (&k)[8]) {
 #pragma unroll
     for (int d = 4; d > 0; d >>= 1)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (!(i & d)) order(k[i], k[i + d]);
 }
+template <int L>
+__device__ inline int32_t lanes_most(int32_t x) {
+    return over_lanes<L>(x, [](int32_t a, int32_t b) { return max_of(a, b); });
+}
 
 // The two largest of all that a pair stands for, of this and of other lanes.
 struct Two {
-    float first = kNone, second = kNone;
-    __device__ void add(float y) {
-        second = __builtin_amdgcn_fmed3f(first, second, y);
-        first = __builtin_fmaxf(first, y);
+    int32_t first = none_of(0), second = none_of(0);
+    __device__ void add(int32_t y) {
+        second = bits_of(__builtin_amdgcn_fmed3f(float_of(first), float_of(second), float_of(y)));
+        first = max_of(first, y);
     }
-    __device__ void join(float f, float s) {
-        second = __builtin_fmaxf(__builtin_fminf(first, f), __builtin_fmaxf(second, s));
-        first = __builtin_fmaxf(first, f);
+    __device__ void join(int32_t f, int32_t s) {
+        second = max_of(min_of(first, f), max_of(second, s));
+        first = max_of(first, f);
     }
     template <int CONTROL>
     __device__ void join_lane() {
-        const auto dpp = [](float v) {
-            return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
-        };
-        join(dpp(first), dpp(second));
+        const int32_t f = __builtin_amdgcn_update_dpp(0, first, CONTROL, 0xf, 0xf, true), s = __builtin_amdgcn_update_dpp(0, second, CONTROL, 0xf, 0xf, true);
+        join(f, s);
     }
-    __device__ float sum() const { return second > kNone ? first + second : first; }
+    // The group's key; `alone`: what stands for the second of a group that has none, all sums being that much too large.
+    __device__ int32_t key(float alone, int32_t g) const {
+        const float sum = float_of(first) + (second >= 0 ? float_of(second) : alone);
+        return first >= 0 ? (bits_of(sum) & ~63) | g : static_cast<int32_t>(0x80000000u) | g;
+    }
 };
 
 template <int L, int N>
@@ -288,11 +298,11 @@ struct Shared {   // of a workgroup
     uint32_t left;
     union Token {      // one after the other
         struct {
-            float group[kGroups];      // keys of groups
-            float edge[2];             // of the last that stays, and the first that does not
-            float sums[L * N];         // where groups are no runs of a lane's neighbours
+            alignas(16) int32_t group[kGroups];   // keys of groups
+            int32_t edge[2];                      // of the last that stays, and the first that does not
+            int32_t sums[L * N];                  // where groups are no runs of a lane's neighbours
         };
-        int32_t won[kMostFast];        // places of the chosen
+        alignas(8) int32_t won[kMostFast][2];     // keys of the chosen, and their lanes
     } token[kThreads / L];
 };
 
@@ -302,9 +312,9 @@ template <typename T, int L, int N, int M, int V>
 __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased a) {
     using S = Shared<L, N>;
     __shared__ S s;
-    if (threadIdx.x == 0) s.left = 0;
     constexpr int NB = kNeighbours<T>, R = N / NB;   // runs of neighbours of a lane
     const int t = threadIdx.x, lane = t & (L - 1);
+    if (t == 0) s.left = 0;
     for (int i = t; i <= a.experts; i += kThreads) s.count[i] = 0;
     __syncthreads();
     float bias[N], widest = 0.0f;
@@ -315,47 +325,96 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
         if (bias[i] > -kInf) widest = __builtin_fmaxf(widest, __builtin_fabsf(bias[i]));
     }
     widest = lanes_max<L>(widest);
+    const bool fits = widest <= kLargeBias;
+    if (!fits) widest = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bias[i] = bias[i] > -kInf ? bias[i] + widest : no_bias(lane);
+    const int32_t none = none_of(lane);
+    const float rounded = (1.0f + 4.0f * widest) * 0x1p-23f;
     // groups that are runs of P lanes, or not
     const int size = a.experts / a.groups, P = size / NB;
     const bool runs = size % NB == 0 && (P & (P - 1)) == 0 && P <= L && P <= 16;
     const int shift = 31 - __builtin_clz(P | 1);
-    typename S::Token& own_slot = s.token[t / L];
+    typename S::Token& mine = s.token[t / L];
     const uint32_t step = gridDim.x * (kThreads / L);
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
-        const bool keep = !a.keep || a.keep[token];
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
-        float x[N], v[N];
+        const bool keep = !a.keep || a.keep[token];
+        float x[N];
         load_logits<T, L, N, V>(x, row, lane, a.experts);
         if (a.keep)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = keep ? x[i] : -kInf;
+        // infinities and NaN: largest as whole numbers, with and without a sign
+        int32_t above = bits_of(x[0]);
+        uint32_t below = above;
+#pragma unroll
+        for (int i = 1; i < N; ++i) {
+            above = max_of(above, bits_of(x[i]));
+            below = below > static_cast<uint32_t>(bits_of(x[i])) ? below : bits_of(x[i]);
+        }
+        const bool special = above >= 0x7f800000 || below >= 0xff800000u;
+        bool bad = false;
         float most = 0.0f, sum = 0.0f, off = kSigmoidOff;
-        if (a.soft) {
-            most = largest<L, N>(x);
-            const float from = most == -kInf ? 0.0f : most;
+        int32_t v[N];   // sums with the bias
+        {
+            float p[N];
+            if (a.soft) {
+                most = -kInf;
+#pragma unroll
+                for (int i = 0; i < N; ++i) most = __builtin_fmaxf(most, x[i]);
+                most = lanes_max<L>(most);
+                const float from = most == -kInf ? 0.0f : most;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    p[i] = power(x[i] - from);
+                    sum += p[i];
+                }
+                sum = lanes_sum<L>(sum);
+                const float by = 1.0f / sum;
+#pragma unroll
+                for (int i = 0; i < N; ++i) p[i] *= by;
+                off = by * kSoftmaxOff;
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) p[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * -1.44269504088896341f));
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = bits_of(p[i] + bias[i]);
+        }
+        if (special) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                v[i] = power(x[i] - from);
-                sum += v[i];
+                if (!(x[i] > -kInf)) v[i] = none;
+                bad |= x[i] != x[i] || (a.soft && x[i] == kInf);
             }
-            sum = lanes_sum<L>(sum);
-            const float by = 1.0f / sum;
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] *= by;
-            off = by * kSoftmaxOff;
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * -1.44269504088896341f));
         }
-        const bool bad = any_nan<L, N>(x) || (a.soft && most == kInf);
-        bool sure = widest <= kLargeBias;
-        // sums with the bias, kNone where the logit or the bias is -inf
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = x[i] > -kInf ? __builtin_fmaxf(v[i] + bias[i], kNone) : kNone;
+        bad = lanes_or<L>(static_cast<unsigned>(bad));
+        bool sure = fits;
         if (a.groups > 1) {
-            float mine[R];        // keys of the groups of a lane's runs
-            bool stays[R];
+            const auto before = [&](auto keys) {   // how many keys of groups are larger than each of these
+                std::array<int, keys.size()> n{};
+                const auto look = [&](int32_t other) {
+#pragma unroll
+                    for (size_t r = 0; r < keys.size(); ++r) n[r] += other > keys[r];
+                };
+                int h = 0;
+                for (; h + 4 <= a.groups; h += 4) {
+                    const int4 four = *reinterpret_cast<const int4*>(mine.group + h);
+                    look(four.x);
+                    look(four.y);
+                    look(four.z);
+                    look(four.w);
+                }
+                for (; h < a.groups; ++h) look(mine.group[h]);
+                return n;
+            };
+            const auto edges = [&](int n, int32_t key) {
+                if (n == a.kept - 1) mine.edge[0] = key;
+                if (n == a.kept) mine.edge[1] = key;
+            };
             if (runs) {
+                std::array<int32_t, R> key;   // of the groups of the lane's runs
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     Two two;
@@ -366,45 +425,33 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
                     if (P > 4) two.template join_lane<0x141>();
                     if (P > 8) two.template join_lane<0x140>();
                     const int g = (r * L + lane) >> shift;
-                    mine[r] = key_of(two.sum(), 63, g & 63);
-                    if (g < a.groups) own_slot.group[g] = mine[r];
+                    key[r] = two.key(widest, g & 63);
+                    if (g < a.groups) mine.group[g] = key[r];
                 }
+                wave_sync();
+                const auto n = before(key);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if ((r * L + lane) >> shift < a.groups) edges(n[r], key[r]);
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) v[r * NB + i] = pick(n[r] < a.kept, v[r * NB + i], none);
+                }
+                wave_sync();
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) own_slot.sums[expert_of<T, L>(lane, i)] = v[i];
+                for (int i = 0; i < N; ++i) mine.sums[expert_of<T, L>(lane, i)] = v[i];
                 wave_sync();
                 for (int g = lane; g < a.groups; g += L) {
                     Two two;
-                    for (int i = 0; i < size; ++i) two.add(own_slot.sums[g * size + i]);
-                    own_slot.group[g] = key_of(two.sum(), 63, g);
-                }
-            }
-            wave_sync();
-            const auto before = [&](float key) {
-                int n = 0;
-                for (int h = 0; h < a.groups; ++h) n += own_slot.group[h] > key;
-                return n;
-            };
-            const auto edges = [&](int n, float key) {
-                if (n == a.kept - 1) own_slot.edge[0] = key;
-                if (n == a.kept) own_slot.edge[1] = key;
-            };
-            if (runs) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int n = before(mine[r]);
-                    stays[r] = n < a.kept;
-                    if ((r * L + lane) >> shift < a.groups) edges(n, mine[r]);
-#pragma unroll
-                    for (int i = 0; i < NB; ++i) v[r * NB + i] = stays[r] ? v[r * NB + i] : kNone;
+                    for (int i = 0; i < size; ++i) two.add(mine.sums[g * size + i]);
+                    mine.group[g] = two.key(widest, g);
                 }
                 wave_sync();
-            } else {
                 uint32_t low = 0, high = 0;   // the groups that stay
                 for (int g = lane; g < a.groups; g += L) {
-                    const float key = own_slot.group[g];
-                    const int n = before(key);
-                    edges(n, key);
+                    const std::array<int32_t, 1> key{mine.group[g]};
+                    const int n = before(key)[0];
+                    edges(n, key[0]);
                     const uint32_t bit = n < a.kept ? 1u << (g & 31) : 0;
                     low |= g < 32 ? bit : 0;
                     high |= g < 32 ? 0 : bit;
@@ -415,80 +462,82 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int g = expert_of<T, L>(lane, i) / size;
-                    v[i] = (g < 32 ? low >> (g & 31) : high >> (g & 31)) & 1 ? v[i] : kNone;
+                    v[i] = pick((g < 32 ? low >> (g & 31) : high >> (g & 31)) & 1, v[i], none);
                 }
             }
-            const float last = own_slot.edge[0], next = own_slot.edge[1];
-            sure &= last < 0.5f * kNone || last - next > __builtin_fabsf(last) * 0x1p-16f + 4.0f * off + (1.0f + widest) * 0x1p-21f;
+            const int32_t last = mine.edge[0], next = mine.edge[1];
+            sure &= next < 0 || float_of(last) - float_of(next) > float_of(last) * 0x1.2p-16f + 4.0f * (off + rounded);
         }
         // the lane's own in order
-        float own[8], more[8], ninth = kNone;   // `more` after `own`; of the lane's ninth at the least how large it is
+        int32_t own[8], more[8], ninth = none;   // `more` after `own`
+        constexpr bool kNinth = N == 16 && M == 8 && L <= 2;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) own[i] = key_of(v[i], 15, i);
+        for (int i = 0; i < 8; ++i) own[i] = (v[i] & ~15) | i;
         sort8(own);
         if constexpr (N == 16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) more[i] = key_of(v[8 + i], 15, 8 + i);
+            for (int i = 0; i < 8; ++i) more[i] = (v[8 + i] & ~15) | (8 + i);
             sort8(more);
 #pragma unroll
             for (int i = 0; i < 8; ++i) order(own[i], more[7 - i]);
             merge8(own);
             if constexpr (M == 16) merge8(more);
-            else
+            if constexpr (kNinth)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ninth = __builtin_fmaxf(ninth, more[i]);
+                for (int i = 0; i < 8; ++i) ninth = max_of(ninth, more[i]);
         }
-        // k + 1 times the largest of the lanes' first; two lanes may have the same, and then neither is sure
-        float last = kInf;
-        int found = 0, claimed = 0;
-        const auto largest_left = [&](float mine) {
-            const float best = lanes_max<L>(mine);
-            sure &= best < 0.5f * kNone || last - best > __builtin_fabsf(best) * 0x1.8p-18f + 2.0f * off;
-            last = best;
-        };
-        const auto take = [&](int j, float first) {   // false: not the lane's
-            const bool mine = first == last, some = last > 0.5f * kNone;
-            found += some;
-            claimed += mine && some;
-            if (mine) own_slot.won[j] = some ? static_cast<int32_t>(lane << 4 | place_of(last, 15)) : -1;
-            return mine;
-        };
+        // k + 1 times the largest of the lanes' first, which leaves its key and its lane.  Two lanes may have the same, and then the choice is not sure: more
+        // lanes of the wave take one than there are to take
         wave_sync();
+        int wins = 0, taken = 0;
+        const auto take = [&](int j, int32_t first) {
+            const int32_t best = lanes_most<L>(first);
+            const bool won = first == best;
+            wins += __popcll(__ballot(won));
+            taken += won;
+            if (won) *reinterpret_cast<int2*>(mine.won[j]) = int2{best, lane};
+            return won;
+        };
         if constexpr (M == 8) {   // (what the j-th leaves behind of a lane's keys gets shorter)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (j >= a.k) break;
-                largest_left(own[0]);
-                const bool mine = take(j, own[0]);
+                const bool won = take(j, own[0]);
 #pragma unroll
-                for (int i = 0; i < 7 && i < 8 - j; ++i) own[i] = pick(mine, own[i + 1], own[i]);
-                if (j == 0) own[7] = pick(mine, ninth, own[7]);
+                for (int i = 0; i < 7 && i < 8 - j; ++i) own[i] = pick(won, own[i + 1], own[i]);
+                // a lane that takes all eight has its eighth once more after it, which is not sure, unless its ninth is there
+                if (j == 0 && (kNinth || N == 8)) own[7] = pick(won, ninth, own[7]);
             }
         } else {
 #pragma unroll 1
             for (int j = 0; j < a.k; ++j) {
-                largest_left(own[0]);
-                const bool mine = take(j, own[0]);
+                const bool won = take(j, own[0]);
 #pragma unroll
-                for (int i = 0; i < 7; ++i) own[i] = pick(mine, own[i + 1], own[i]);
-                own[7] = pick(mine, more[0], own[7]);
+                for (int i = 0; i < 7; ++i) own[i] = pick(won, own[i + 1], own[i]);
+                own[7] = pick(won, more[0], own[7]);
 #pragma unroll
-                for (int i = 0; i < 7; ++i) more[i] = pick(mine, more[i + 1], more[i]);
-                more[7] = pick(mine, kNone, more[7]);
+                for (int i = 0; i < 7; ++i) more[i] = pick(won, more[i + 1], more[i]);
+                more[7] = pick(won, none, more[7]);
             }
         }
-        largest_left(own[0]);
+        const int32_t next = lanes_most<L>(own[0]);
         wave_sync();
-        sure &= lanes_sum<L>(claimed) == found;
+        const float near = float_of(max_of(mine.won[0][0], 0)) * 0x1.2p-18f + 2.0f * off + rounded;
+        for (int j = lane; j < a.k; j += L) {
+            const int32_t key = mine.won[j][0], after = j + 1 < a.k ? mine.won[j + 1][0] : next;
+            sure &= after < 0 || float_of(key) - float_of(after) > near;
+        }
+        if (wins != a.k * __popcll(__ballot(lane == 0))) sure &= lanes_sum<L>(taken) == a.k;
+        sure = !lanes_or<L>(static_cast<unsigned>(!sure));
         if (bad) {
             choose_none<L>(a, token, lane);
         } else if (!sure) {
             if (lane == 0) a.later[static_cast<uint64_t>(blockIdx.x) * a.room + atomicAdd(&s.left, 1u)] = static_cast<uint32_t>(token);
         } else {
             const auto chosen = [&](int j) {
-                const int32_t w = own_slot.won[j];
-                const int l = w >> 4, i = w & 15;
-                return w < 0 ? -1 : (i / NB * L + l) * NB + i % NB;
+                const int2 w = *reinterpret_cast<const int2*>(mine.won[j]);
+                const int i = w.x & 15;
+                return w.x < 0 ? -1 : (i / NB * L + w.y) * NB + i % NB;
             };
             for (int j = lane; j < a.k; j += L) a.chosen[token * a.k + j] = chosen(j);
             weigh<T, L>(a, token, row, lane, most, sum, s.count, chosen);
@@ -573,12 +622,24 @@ __global__ __launch_bounds__(kThreads) void route_biased_gradient_kernel(const B
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const bool keep = !a.keep || a.keep[token];
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
-        // f(expert, gradient of its weight, its logit) for each of the lane's chosen
+        // the lane's first chosen: its expert (-1: none), the gradient of its weight, its logit
+        int e0 = -1;
+        float g0 = 0.0f, x0 = -kInf;
+        const auto chosen = [&](int j, int* e, float* g, float* x) {
+            *e = j < a.k && keep ? a.chosen[token * a.k + j] : -1;
+            *g = j < a.k ? a.grad_weights[token * a.k + j] : 0.0f;
+            if (*e >= a.experts) *e = -1;
+            *x = *e >= 0 ? static_cast<float>(row[*e]) : -kInf;
+        };
+        chosen(lane, &e0, &g0, &x0);
+        // f(expert, gradient, logit) for each of the lane's chosen
         const auto each = [&](auto f) {
-            if (!keep) return;
-            for (int j = lane; j < a.k; j += L) {
-                const int e = a.chosen[token * a.k + j];
-                if (e >= 0 && e < a.experts) f(e, a.grad_weights[token * a.k + j], static_cast<float>(row[e]));
+            if (e0 >= 0) f(e0, g0, x0);
+            for (int j = lane + L; j < a.k; j += L) {
+                int e;
+                float g, x;
+                chosen(j, &e, &g, &x);
+                if (e >= 0) f(e, g, x);
             }
         };
         float most = -kInf;
@@ -593,12 +654,12 @@ __global__ __launch_bounds__(kThreads) void route_biased_gradient_kernel(const B
                 sum += p;
                 dot += p * g;
             });
-            sum = lanes_sum<L>(sum);
-            dot = lanes_sum<L>(dot) / sum;
+            sum = 1.0 / lanes_sum<L>(sum);
+            dot = lanes_sum<L>(dot) * sum;
         }
         each([&](int e, float g, float x) {
             float d = a.scale * g;
-            if (a.normalize) d = static_cast<float>(a.scale * (g - dot) * (part_of(a.soft, x, most) / sum));
+            if (a.normalize) d = a.k == 1 ? 0.0f : static_cast<float>(a.scale * (g - dot) * (part_of(a.soft, x, most) * sum));
             else if (!a.soft) d *= part_of(false, x, 0.0f);
             if (!a.soft) d *= 1.0f / (1.0f + expf(x));
             add[place(e)] = d;
@@ -609,7 +670,11 @@ __global__ __launch_bounds__(kThreads) void route_biased_gradient_kernel(const B
 #pragma unroll
         for (int i = 0; i < N; ++i) d[i] = add[place_at(lane, i)];
         wave_sync();
-        each([&](int e, float, float) { add[place(e)] = 0.0f; });
+        if (e0 >= 0) add[place(e0)] = 0.0f;
+        for (int j = lane + L; j < a.k; j += L) {
+            const int e = a.chosen[token * a.k + j];
+            if (e >= 0 && e < a.experts) add[place(e)] = 0.0f;
+        }
         wave_sync();
         if (whole && lanes_or<L>(any)) {
             float x[N], from, scale, lse;
@@ -648,7 +713,7 @@ struct Plan {
     size_t bytes;
     Plan(size_t tokens, int experts, int k, void* workspace) : exact(tokens <= kMostExact || k > kMostFast) {
         Carve c(workspace);
-        groups = exact ? static_cast<uint32_t>(tokens <= kMostExact ? 1 : std::min<uint64_t>(kMostGroups, ceil_div(tokens, kThreads / 64))) : groups_of(tokens, experts);
+        groups = exact ? static_cast<uint32_t>(tokens <= kMostExact ? 1 : std::min<uint64_t>(kMostGroups, ceil_div(tokens, kExactThreads / 64))) : groups_of(tokens, experts);
         if (groups > 1) counts = c.take<int32_t>(static_cast<size_t>(groups) * (experts + 1));
         if (!exact) {
             const uint32_t at_once = kThreads / lanes_of(experts);
@@ -671,7 +736,7 @@ blink_status_t route_biased(const void* logits, blink_dtype_t dtype, size_t toke
                             void* workspace, hipStream_t stream) {
     const Plan plan(tokens, experts, k, workspace);
     const Biased a{logits, stride, keep, bias, static_cast<uint32_t>(tokens), experts, k, kept_groups < expert_groups ? expert_groups : 1, kept_groups, soft,
-                   normalize, scale, chosen, weights, plan.groups > 1 ? plan.counts : counts, plan.later, plan.left, plan.room};
+                   normalize, scale, chosen, weights, plan.groups > 1 ? plan.counts : counts, plan.later, plan.left, plan.room, plan.groups};
     BLINK_TRY(with_float(dtype, [&](auto type) {
         using T = decltype(type);
         const auto run = [&](void (*kernel)(Biased)) { return launch(kernel, dim3(plan.groups), dim3(kThreads), stream, a); };
@@ -684,9 +749,12 @@ blink_status_t route_biased(const void* logits, blink_dtype_t dtype, size_t toke
                     return run(route_biased_choose<T, L, N, 8, V>);
                 });
             }));
-        if (experts <= 64) return run(route_biased_exact<T, 1>);
-        if (experts <= 256) return run(route_biased_exact<T, 4>);
-        return run(route_biased_exact<T, 16>);
+        const auto exact = [&](void (*kernel)(Biased)) {
+            return launch(kernel, dim3(plan.exact ? plan.groups : static_cast<uint32_t>(ceil_div(plan.groups, kLists))), dim3(kExactThreads), stream, a);
+        };
+        if (experts <= 64) return exact(route_biased_exact<T, 1>);
+        if (experts <= 256) return exact(route_biased_exact<T, 4>);
+        return exact(route_biased_exact<T, 16>);
     }));
     if (plan.groups == 1) return BLINK_OK;
     return launch(route_biased_add, dim3(static_cast<uint32_t>(ceil_div(experts + 1, kAddColumns))), dim3(kAddThreads), stream, a.counts, plan.groups, experts + 1,

@@ -96,6 +96,8 @@ def _want(logits, k, bias=None, keep=None, groups=1, kept=1, scores="sigmoid", n
         spread = d.abs()
     if scores == "sigmoid":
         d, spread = d * not_p, spread * not_p
+        if not normalize:      # a p below the normal numbers of 32 bits may be 0, and p times (scale g) is then all off
+            spread = spread + torch.where(s < 2.0 ** -126, 2.0 ** -126 * SCALE * g.abs() / (3 * rel), 0.0)
     dx.scatter_add_(1, at, torch.where(found, d, 0.0))
     size_of.scatter_add_(1, at, torch.where(found, spread, 0.0))
     if whole:
