@@ -50,8 +50,8 @@ __device__ inline unsigned lanes_or(unsigned x) {
     return over_lanes<L>(x, [](unsigned a, unsigned b) { return a | b; });
 }
 template <int L>
-__device__ inline int lanes_sum(int x) {
-    return over_lanes<L>(x, [](int a, int b) { return a + b; });
+__device__ inline int lanes_least(int x) {
+    return over_lanes<L>(x, [](int a, int b) { return a < b ? a : b; });
 }
 template <int L>
 __device__ inline double lanes_sum(double x) {

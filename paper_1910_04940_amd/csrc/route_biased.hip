@@ -228,9 +228,11 @@ __global__ __launch_bounds__(kExactThreads) void route_biased_exact(const Biased
 // Of a softmax by kSoftmaxOff times the largest p: 2.5 |x - m| 2^-24 of p for its power, whose p |x - m| is below 0.37 of the largest, and 47 * 2^-24 for
 // the sum (1024 numbers, their mean |x - m| at most ln 1024; 22 additions on the way), its reciprocal and product.
 // The largest |bias|, w, is added to all, so that sums are not negative and compare as whole numbers do; they are off by (1 + 4 w) 2^-24 for that.  Their
-// lowest four bits give way to the place in the lane (a key is off by 2^-19 of itself), those of groups, sums of two, their lowest six to the group (2^-17).
+// lowest four bits give way to the place in the lane, first places largest (a key is off by 2^-19 of itself), those of groups, sums of two, their lowest six to
+// the group (2^-17).
 // A token is sure if no two neighbours in the order of its first k + 1, nor the last group that stays and the first that does not, are nearer than the
-// sum of all that.
+// sum of all that; two of its first k may be nearer if their logits and biases are the same (16-bit logits often are): among lanes whose keys differ in
+// the place only, and so in one run of neighbours, the first one is taken first, and a lane's places are in order.
 constexpr float kSigmoidOff = 0x1p-22f, kSoftmaxOff = 0x1p-18f;
 constexpr float kLargeBias = 1e37f;      // larger ones (but -inf) leave everything to the 64 bits
 constexpr int kMostFast = 16;            // k
@@ -472,11 +474,11 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
         int32_t own[8], more[8], ninth = none;   // `more` after `own`
         constexpr bool kNinth = N == 16 && M == 8 && L <= 2;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) own[i] = (v[i] & ~15) | i;
+        for (int i = 0; i < 8; ++i) own[i] = (v[i] & ~15) | (15 - i);
         sort8(own);
         if constexpr (N == 16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) more[i] = (v[8 + i] & ~15) | (8 + i);
+            for (int i = 0; i < 8; ++i) more[i] = (v[8 + i] & ~15) | (7 - i);
             sort8(more);
 #pragma unroll
             for (int i = 0; i < 8; ++i) order(own[i], more[7 - i]);
@@ -486,16 +488,17 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ninth = max_of(ninth, more[i]);
         }
-        // k + 1 times the largest of the lanes' first, which leaves its key and its lane.  Two lanes may have the same, and then the choice is not sure: more
-        // lanes of the wave take one than there are to take
+        // k + 1 times the largest of the lanes' first, which leaves its key and its lane
         wave_sync();
-        int wins = 0, taken = 0;
+        const int there = __popcll(__ballot(lane == 0));
         const auto take = [&](int j, int32_t first) {
-            const int32_t best = lanes_most<L>(first);
-            const bool won = first == best;
-            wins += __popcll(__ballot(won));
-            taken += won;
-            if (won) *reinterpret_cast<int2*>(mine.won[j]) = int2{best, lane};
+            const int32_t key = first & -NB, best = lanes_most<L>(key);
+            bool won = key == best;
+            if (__popcll(__ballot(won)) != there) {   // some lanes have the same: the first one's
+                const int least = lanes_least<L>(won ? lane : L);   // (asked of all lanes)
+                won = won && lane == least;
+            }
+            if (won) *reinterpret_cast<int2*>(mine.won[j]) = int2{first, lane};
             return won;
         };
         if constexpr (M == 8) {   // (what the j-th leaves behind of a lane's keys gets shorter)
@@ -523,22 +526,25 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
         const int32_t next = lanes_most<L>(own[0]);
         wave_sync();
         const float near = float_of(max_of(mine.won[0][0], 0)) * 0x1.2p-18f + 2.0f * off + rounded;
+        const auto expert_at = [&](int2 w) {
+            const int i = 15 - (w.x & 15);
+            return w.x < 0 ? -1 : (i / NB * L + w.y) * NB + i % NB;
+        };
+        const auto at = [&](int j) { return *reinterpret_cast<const int2*>(mine.won[j]); };
         for (int j = lane; j < a.k; j += L) {
-            const int32_t key = mine.won[j][0], after = j + 1 < a.k ? mine.won[j + 1][0] : next;
-            sure &= after < 0 || float_of(key) - float_of(after) > near;
+            const int2 w = at(j), then = j + 1 < a.k ? at(j + 1) : int2{next, 0};
+            if (!bad && then.x >= 0 && !(float_of(w.x) - float_of(then.x) > near)) {   // (a NaN's keys may stand for no expert)
+                const int e = expert_at(w), f = expert_at(then);
+                sure &= j + 1 < a.k && row[e] == row[f] && (!a.bias || a.bias[e] == a.bias[f]);
+            }
         }
-        if (wins != a.k * __popcll(__ballot(lane == 0))) sure &= lanes_sum<L>(taken) == a.k;
         sure = !lanes_or<L>(static_cast<unsigned>(!sure));
         if (bad) {
             choose_none<L>(a, token, lane);
         } else if (!sure) {
             if (lane == 0) a.later[static_cast<uint64_t>(blockIdx.x) * a.room + atomicAdd(&s.left, 1u)] = static_cast<uint32_t>(token);
         } else {
-            const auto chosen = [&](int j) {
-                const int2 w = *reinterpret_cast<const int2*>(mine.won[j]);
-                const int i = w.x & 15;
-                return w.x < 0 ? -1 : (i / NB * L + w.y) * NB + i % NB;
-            };
+            const auto chosen = [&](int j) { return expert_at(at(j)); };
             for (int j = lane; j < a.k; j += L) a.chosen[token * a.k + j] = chosen(j);
             weigh<T, L>(a, token, row, lane, most, sum, s.count, chosen);
         }
