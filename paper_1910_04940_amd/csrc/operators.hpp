@@ -65,7 +65,6 @@ blink_status_t launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s
     std::tuple<P...> args(static_cast<P>(a)...);
     return launch_with(kernel, grid, block, stream, args, std::index_sequence_for<P...>());
 }
-
 // Orders a wave's accesses to LDS for the compiler; the wave itself makes them in order.
 __device__ inline void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -337,6 +337,9 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
     const int size = a.experts / a.groups, P = size / NB;
     const bool runs = size % NB == 0 && (P & (P - 1)) == 0 && P <= L && P <= 16;
     const int shift = 31 - __builtin_clz(P | 1);
+    // e / size for e and size below 2^10: e * (2^20 / size, rounded up) is off by less than 2^20
+    const uint32_t by_size = ((1u << 20) + size - 1) / size;
+    const auto group_of = [&](int e) { return static_cast<int>(e * by_size >> 20); };
     typename S::Token& mine = s.token[t / L];
     const uint32_t step = gridDim.x * (kThreads / L);
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
@@ -445,7 +448,14 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
                 wave_sync();
                 for (int g = lane; g < a.groups; g += L) {
                     Two two;
-                    for (int i = 0; i < size; ++i) two.add(mine.sums[g * size + i]);
+                    const int32_t* const of = mine.sums + g * size;
+                    int i = 0;
+                    for (; i + 4 <= size; i += 4) {   // (reads under way together)
+                        const int32_t y[4] = {of[i], of[i + 1], of[i + 2], of[i + 3]};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) two.add(y[j]);
+                    }
+                    for (; i < size; ++i) two.add(of[i]);
                     mine.group[g] = two.key(widest, g);
                 }
                 wave_sync();
@@ -463,7 +473,7 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
                 wave_sync();
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int g = expert_of<T, L>(lane, i) / size;
+                    const int g = group_of(expert_of<T, L>(lane, i));
                     v[i] = pick((g < 32 ? low >> (g & 31) : high >> (g & 31)) & 1, v[i], none);
                 }
             }

@@ -31,6 +31,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kBlock = 256;                  // elements of a wave at a time, and of a scale
 constexpr uint32_t kPieceBlocks = 8, kPiece = kPieceBlocks * kBlock;
 constexpr uint32_t kMostGroups = 2048;            // workgroups of the norm, which leave a sum each
+constexpr uint64_t kCache = uint64_t{256} << 20;  // the memory-side cache
+constexpr uint32_t kHeld = 52 << 10;              // bytes of LDS that let three workgroups onto a compute unit
 
 struct Record {
     void* weights;
@@ -46,24 +48,38 @@ struct Piece {
     uint32_t tensor, number;   // its `number`-th 2048 elements
 };
 
-// Four elements, wherever they start.
+// Four elements, wherever they start.  PAST: they come from memory and go there, past the caches.
 template <typename T>
 struct alignas(sizeof(T)) Four {
     T v[4];
 };
 template <typename T>
-__device__ inline Four<T> load4(const T* p, uint32_t left) {   // zeros past the end
-    if (left >= 4) return *reinterpret_cast<const Four<T>*>(p);
+struct Words {   // their bits, as the loads and stores past the caches take them
+    typedef uint32_t type __attribute__((ext_vector_type(sizeof(T)), aligned(sizeof(T))));
+};
+template <>
+struct Words<uint8_t> {
+    typedef uint32_t type __attribute__((aligned(1)));
+};
+template <bool PAST, typename T>
+__device__ inline Four<T> load4(const T* p) {
+    if constexpr (PAST) return __builtin_bit_cast(Four<T>, __builtin_nontemporal_load(reinterpret_cast<const typename Words<T>::type*>(p)));
+    else return *reinterpret_cast<const Four<T>*>(p);
+}
+template <bool PAST, typename T>
+__device__ inline void store4(T* p, const Four<T>& y) {
+    if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(typename Words<T>::type, y), reinterpret_cast<typename Words<T>::type*>(p));
+    else *reinterpret_cast<Four<T>*>(p) = y;
+}
+// The same of the last elements of a tensor, `left` of them: zeros past the end.
+template <typename T>
+__device__ inline Four<T> load_some(const T* p, uint32_t left) {
     Four<T> y;
     for (uint32_t i = 0; i < 4; ++i) y.v[i] = i < left ? p[i] : static_cast<T>(0);
     return y;
 }
 template <typename T>
-__device__ inline void store4(T* p, uint32_t left, const Four<T>& y) {
-    if (left >= 4) {
-        *reinterpret_cast<Four<T>*>(p) = y;
-        return;
-    }
+__device__ inline void store_some(T* p, const Four<T>& y, uint32_t left) {
     for (uint32_t i = 0; i < 4; ++i)
         if (i < left) p[i] = y.v[i];
 }
@@ -78,52 +94,85 @@ struct Norm {
     double* sums;          // one to a workgroup
 };
 
-__device__ inline double add_up(double s, double (&part)[kWaves]) {   // for thread 0
+template <int WAVES>
+__device__ inline double add_up(double s, double (&part)[WAVES]) {   // for thread 0
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
     s = 0.0;
-    for (int w = 0; w < kWaves; ++w) s += part[w];
+    for (int w = 0; w < WAVES; ++w) s += part[w];
     return s;
 }
 
-// Squares and their sums in 64 bits: no gradient's square overflows or is lost.
-template <typename G>
+// What a sum of squares makes.
+struct Clip {
+    double most, factor;
+    float* norm;
+    int32_t* step;
+    __device__ void finish(double s) const {
+        const bool fine = s < __builtin_inf();   // (not with an infinite gradient, nor with a NaN)
+        const double length = sqrt(s) * fabs(factor);
+        norm[0] = static_cast<float>(length);
+        norm[1] = fine ? static_cast<float>(length > most ? factor * (most / length) : factor) : __builtin_nanf("");
+        if (step && fine) *step += 1;
+    }
+};
+
+// Squares and their sums in 64 bits: no gradient's square overflows or is lost.  THREADS threads take a piece.
+template <typename G, bool PAST, uint32_t THREADS>
+__device__ inline double squares_of(const Norm& a, uint32_t piece, uint32_t thread) {
+    double s = 0.0;
+    const auto add = [&](const Four<G>& g) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double x = static_cast<float>(g.v[j]);
+            s = __builtin_fma(x, x, s);
+        }
+    };
+    constexpr uint32_t kLoads = kPiece / (4 * THREADS);
+    const Piece p = a.pieces[piece];
+    const Record& r = a.tensors[p.tensor];
+    const uint64_t from = static_cast<uint64_t>(p.number) * kPiece;
+    const G* const grad = static_cast<const G*>(r.grad) + from;
+    if (from + kPiece <= r.elements) {
+        Four<G> g[kLoads];
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) g[u] = load4<PAST>(grad + (u * THREADS + thread) * 4);
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) add(g[u]);
+    } else {
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            const uint32_t at = (u * THREADS + thread) * 4;
+            add(load_some(grad + at, left_of(r.elements, from + at)));
+        }
+    }
+    return s;
+}
+template <typename G, bool PAST>
 __global__ __launch_bounds__(kThreads) void update_squares(const Norm a) {
     __shared__ double part[kWaves];
     double s = 0.0;
-    for (uint32_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-        const Piece p = a.pieces[i];
-        const Record& r = a.tensors[p.tensor];
-        const uint64_t from = static_cast<uint64_t>(p.number) * kPiece;
-        const G* const grad = static_cast<const G*>(r.grad);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint64_t at = from + (u * kThreads + threadIdx.x) * 4;
-            const uint32_t left = left_of(r.elements, at);
-            const Four<G> g = load4(grad + at, left);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const double x = static_cast<float>(g.v[j]);
-                s = __builtin_fma(x, x, s);
-            }
-        }
-    }
+    for (uint32_t i = blockIdx.x; i < a.n; i += gridDim.x) s += squares_of<G, PAST, kThreads>(a, i, threadIdx.x);
     s = add_up(s, part);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
-
-__global__ __launch_bounds__(kThreads) void update_norm(const double* sums, uint32_t n, double most, double factor, float* norm, int32_t* step) {
+__global__ __launch_bounds__(kThreads) void update_norm(const double* sums, uint32_t n, const Clip clip) {
     __shared__ double part[kWaves];
     double s = 0.0;
     for (uint32_t i = threadIdx.x; i < n; i += kThreads) s += sums[i];
     s = add_up(s, part);
-    if (threadIdx.x != 0) return;
-    const bool fine = s < __builtin_inf();   // (not with an infinite gradient, nor with a NaN)
-    const double length = sqrt(s) * fabs(factor);
-    norm[0] = static_cast<float>(length);
-    norm[1] = fine ? static_cast<float>(length > most ? factor * (most / length) : factor) : __builtin_nanf("");
-    if (step && fine) *step += 1;
+    if (threadIdx.x == 0) clip.finish(s);
+}
+// Few pieces of one type in one workgroup, a wave to a piece: nine tensors of 5365 elements in all 4.7 us a call, 7.1 as two kernels.
+constexpr int kFewThreads = 1024;
+constexpr uint32_t kFew = 2 * kFewThreads / 64;
+template <typename G>
+__global__ __launch_bounds__(kFewThreads) void update_few(const Norm a, const Clip clip) {
+    __shared__ double part[kFewThreads / 64];
+    double s = 0.0;
+    for (uint32_t i = threadIdx.x / 64; i < a.n; i += kFewThreads / 64) s += squares_of<G, false, 64>(a, i, threadIdx.x & 63);
+    s = add_up(s, part);
+    if (threadIdx.x == 0) clip.finish(s);
 }
 
 // ---- step -------------------------------------------------------------------------------------------------------------------
@@ -144,26 +193,17 @@ __device__ inline uint32_t mixed(uint32_t h) {   // the finalizer of MurmurHash3
     return h ^ h >> 16;
 }
 
-// |z| <= 448, given by its bits, as an e4m3 number; `up`: 16 random bits.
-__device__ inline uint32_t to_eight(uint32_t z, uint32_t up) {
-    constexpr uint32_t kNormal = 0x3c800000u;   // 2^-6
-    const float y = __builtin_bit_cast(float, z);
-    const uint32_t large = ((z + (up << 4 | 8)) >> 20) - 960;             // (exponents differ by 120, 3 bits of 23 stay)
-    const float units = y * 512.0f;                                       // exact, as is what is left of it
-    const uint32_t down = static_cast<uint32_t>(units);
-    const uint32_t small = down + (units - static_cast<float>(down) >= 1.0f - (static_cast<float>(up) + 0.5f) * 0x1p-16f);
-    const uint32_t code = z >= kNormal ? large : small;
-    return code > 0x7e ? 0x7e : code;
-}
-
-// The four numbers of a lane as codes, and the scale of the wave's 256.  ROOT: y >= 0, and what is not zero is not stored as zero.
+// The four numbers of a lane as codes, and the scale of the wave's 256; up: 16 random bits each, in the upper half of a word.  ROOT: y >= 0, and what is not
+// zero is not stored as zero.
+// The instruction adds the upper 20 of the word's bits to the 20 of a number's 23 that have no place (numbers below 2^-6: to what is left of a
+// multiple of 2^-9) and cuts them off; the lower half of the word stands for half of a sixteenth bit, so that all are used alike.  Made of ordinary
+// instructions, twenty a number, the 8-bit step of 168 M elements took 590 us, 516 like this.
 template <bool ROOT>
 __device__ inline uint32_t encode(const float (&y)[4], const uint32_t (&up)[4], float* scale) {
-    uint32_t bits[4], most = 0;
+    uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        bits[j] = __builtin_bit_cast(uint32_t, y[j]);
-        const uint32_t size = bits[j] & 0x7fffffffu;
+        const uint32_t size = __builtin_bit_cast(uint32_t, y[j]) & 0x7fffffffu;
         most = size > most ? size : most;
     }
     most = lanes_max<64>(most);
@@ -178,14 +218,16 @@ __device__ inline uint32_t encode(const float (&y)[4], const uint32_t (&up)[4], 
     }
     *scale = largest * (1.0f / 448.0f);
     const float by = 1.0f / largest * 448.0f;
+    const auto cut = [&](int j) { return static_cast<float>(__builtin_amdgcn_fmed3f(y[j] * by, -448.0f, 448.0f)); };
     uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(cut(0), up[0] | 0x8000u, codes, 0);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(cut(1), up[1] | 0x8000u, codes, 1);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(cut(2), up[2] | 0x8000u, codes, 2);
+    codes = __builtin_amdgcn_cvt_sr_fp8_f32(cut(3), up[3] | 0x8000u, codes, 3);
+    if (ROOT && ((codes - 0x01010101u) & ~codes & 0x80808080u)) {   // some are zero
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float z = __builtin_fminf(__builtin_fabsf(y[j]) * by, 448.0f);
-        uint32_t c = to_eight(__builtin_bit_cast(uint32_t, z), up[j]);
-        if (ROOT) c = c == 0 && z != 0.0f ? 1 : c;
-        else c |= bits[j] >> 24 & 0x80u;
-        codes |= c << (8 * j);
+        for (int j = 0; j < 4; ++j)
+            if (!(codes >> (8 * j) & 0xffu) && y[j] * by != 0.0f) codes |= 1u << (8 * j);
     }
     return codes;
 }
@@ -198,87 +240,151 @@ __device__ inline void decode(uint32_t codes, float scale, float (&y)[4]) {
     y[3] = high[1] * scale;
 }
 
-// W, G: types of the weights and the gradient; MASTER: weights are the rounding of a copy in 32 bits; EIGHT: moments in 8 bits.
+// What a step is for all elements of a tensor.
+struct Factors {
+    float scale, by_m, by_v, kept, b1, b2, g1, g2, eps;
+};
+// A lane's four elements of one block of a tensor, as they are in memory.
 template <typename W, typename G, bool MASTER, bool EIGHT>
-__global__ __launch_bounds__(kThreads) void update_adamw(const Step a) {
-    const uint32_t number = block_of(blockIdx.y);
-    if (number >= a.n) return;
-    const Piece p = a.pieces[number];
-    const Record r = a.tensors[p.tensor];
-    const int32_t t = *a.step;
-    const float scale = a.scale ? *a.scale : 1.0f;
-    const double rate = a.lr * r.rate * (a.rate ? static_cast<double>(*a.rate) : 1.0);
-    if (t < 1 || scale != scale) return;
-    const float by_m = static_cast<float>(rate / (1.0 - exp(t * a.ln1))), by_v = static_cast<float>(1.0 / sqrt(1.0 - exp(t * a.ln2)));
-    const float kept = static_cast<float>(1.0 - rate * r.decay);
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t key = mixed(mixed(a.seed + 0x9e3779b9u * static_cast<uint32_t>(t)) ^ static_cast<uint32_t>(r.number));
-    for (uint32_t u = wave; u < kPieceBlocks; u += kWaves) {
-        const uint64_t block = static_cast<uint64_t>(p.number) * kPieceBlocks + u, from = block * kBlock;
-        if (from >= r.elements) return;
-        const uint64_t at = from + lane * 4;
-        const uint32_t left = left_of(r.elements, at);
-        const Four<G> g4 = load4(static_cast<const G*>(r.grad) + at, left);
-        float w[4], m[4], v[4];
-        if constexpr (MASTER) {
-            const Four<float> y = load4(r.master + at, left);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = y.v[j];
-        } else {
-            const Four<W> y = load4(static_cast<const W*>(r.weights) + at, left);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = static_cast<float>(y.v[j]);
-        }
+struct Held {
+    using M = typename std::conditional<EIGHT, uint8_t, float>::type;
+    using C = typename std::conditional<MASTER, float, W>::type;   // of the weights that are stepped
+    Four<G> g;
+    Four<C> w;
+    Four<M> m, v;
+    float scale1, scale2;
+
+    template <bool PAST>
+    __device__ void load(const Record& r, uint64_t block, uint32_t lane) {
+        const uint64_t at = block * kBlock + lane * 4;
+        g = load4<PAST>(static_cast<const G*>(r.grad) + at);
+        w = load4<PAST>(stepped(r) + at);
+        m = load4<PAST>(static_cast<const M*>(r.moment1) + at);
+        v = load4<PAST>(static_cast<const M*>(r.moment2) + at);
+        scales(r, block);
+    }
+    __device__ void load(const Record& r, uint64_t block, uint32_t lane, uint32_t left) {
+        const uint64_t at = block * kBlock + lane * 4;
+        g = load_some(static_cast<const G*>(r.grad) + at, left);
+        w = load_some(stepped(r) + at, left);
+        m = load_some(static_cast<const M*>(r.moment1) + at, left);
+        v = load_some(static_cast<const M*>(r.moment2) + at, left);
+        scales(r, block);
+    }
+    __device__ static C* stepped(const Record& r) {
+        if constexpr (MASTER) return r.master;
+        else return static_cast<W*>(r.weights);
+    }
+    __device__ void scales(const Record& r, uint64_t block) {
         if constexpr (EIGHT) {
-            const Four<uint8_t> c1 = load4(static_cast<const uint8_t*>(r.moment1) + at, left), c2 = load4(static_cast<const uint8_t*>(r.moment2) + at, left);
-            decode(__builtin_bit_cast(uint32_t, c1), r.scale1[block], m);
-            decode(__builtin_bit_cast(uint32_t, c2), r.scale2[block], v);
+            scale1 = r.scale1[block];
+            scale2 = r.scale2[block];
+        }
+    }
+    // The step, and what it leaves by `store`(place, four elements).
+    template <typename F>
+    __device__ void step(const Record& r, const Factors& f, uint64_t block, uint32_t lane, uint32_t left, uint32_t key, F store) const {
+        float y[4], a[4], b[4], root[4];
+        if constexpr (EIGHT) {
+            decode(__builtin_bit_cast(uint32_t, m), scale1, a);
+            decode(__builtin_bit_cast(uint32_t, v), scale2, b);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] *= v[j];
+            for (int j = 0; j < 4; ++j) b[j] *= b[j];
         } else {
-            const Four<float> y1 = load4(static_cast<const float*>(r.moment1) + at, left), y2 = load4(static_cast<const float*>(r.moment2) + at, left);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                m[j] = y1.v[j];
-                v[j] = y2.v[j];
+                a[j] = m.v[j];
+                b[j] = v.v[j];
             }
         }
-        float root[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float g = static_cast<float>(g4.v[j]) * scale;
-            m[j] = a.b1 * m[j] + a.g1 * g;
-            v[j] = a.b2 * v[j] + a.g2 * (g * g);
-            root[j] = sqrtf(v[j]);
-            w[j] = w[j] * kept - by_m * (m[j] / (root[j] * by_v + a.eps));
+            const float grad = static_cast<float>(g.v[j]) * f.scale;
+            a[j] = f.b1 * a[j] + f.g1 * grad;
+            b[j] = f.b2 * b[j] + f.g2 * (grad * grad);
+            root[j] = sqrtf(b[j]);
+            y[j] = static_cast<float>(w.v[j]) * f.kept - f.by_m * (a[j] / (root[j] * f.by_v + f.eps));
         }
-        Four<W> w4;
+        const uint64_t at = block * kBlock + lane * 4;
+        Four<W> to;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w4.v[j] = static_cast<W>(w[j]);
-        store4(static_cast<W*>(r.weights) + at, left, w4);
-        if constexpr (MASTER) store4(r.master + at, left, Four<float>{{w[0], w[1], w[2], w[3]}});
+        for (int j = 0; j < 4; ++j) to.v[j] = static_cast<W>(y[j]);
+        store(static_cast<W*>(r.weights) + at, to);
+        if constexpr (MASTER) store(r.master + at, Four<float>{{y[0], y[1], y[2], y[3]}});
         if constexpr (EIGHT) {
             const uint32_t mine = mixed(key ^ static_cast<uint32_t>(block));
             uint32_t up1[4], up2[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t h = mixed(mine ^ (lane * 4 + j));
-                up1[j] = h & 0xffffu;
-                up2[j] = h >> 16;
-                if (static_cast<uint32_t>(j) >= left) m[j] = root[j] = 0.0f;
+                up1[j] = h << 16;
+                up2[j] = h & 0xffff0000u;
+                if (static_cast<uint32_t>(j) >= left) a[j] = root[j] = 0.0f;
             }
             float s1, s2;
-            const uint32_t c1 = encode<false>(m, up1, &s1), c2 = encode<true>(root, up2, &s2);
-            store4(static_cast<uint8_t*>(r.moment1) + at, left, __builtin_bit_cast(Four<uint8_t>, c1));
-            store4(static_cast<uint8_t*>(r.moment2) + at, left, __builtin_bit_cast(Four<uint8_t>, c2));
+            const uint32_t c1 = encode<false>(a, up1, &s1), c2 = encode<true>(root, up2, &s2);
+            store(static_cast<uint8_t*>(r.moment1) + at, __builtin_bit_cast(Four<uint8_t>, c1));
+            store(static_cast<uint8_t*>(r.moment2) + at, __builtin_bit_cast(Four<uint8_t>, c2));
             if (lane == 0) {
                 r.scale1[block] = s1;
                 r.scale2[block] = s2;
             }
         } else {
-            store4(static_cast<float*>(r.moment1) + at, left, Four<float>{{m[0], m[1], m[2], m[3]}});
-            store4(static_cast<float*>(r.moment2) + at, left, Four<float>{{v[0], v[1], v[2], v[3]}});
+            store(static_cast<float*>(r.moment1) + at, Four<float>{{a[0], a[1], a[2], a[3]}});
+            store(static_cast<float*>(r.moment2) + at, Four<float>{{b[0], b[1], b[2], b[3]}});
         }
+    }
+};
+
+// W, G: types of the weights and the gradient; MASTER: weights are the rounding of a copy in 32 bits; EIGHT: moments in 8 bits.
+template <typename W, typename G, bool MASTER, bool EIGHT, bool PAST>
+__global__ __launch_bounds__(kThreads) void update_adamw(const Step a) {
+    if constexpr (PAST && !EIGHT) {   // LDS that nobody uses, so that three workgroups are on a compute unit
+        __shared__ volatile uint8_t held[kHeld];
+        if (a.n == 0) held[threadIdx.x] = 0;
+    }
+    // a piece to a workgroup, or where caches serve half a piece: more of them
+    constexpr uint32_t kShares = PAST ? 1 : 2, kBlocks = kPieceBlocks / kShares;
+    const uint32_t number = block_of(blockIdx.y);
+    if (number >= a.n * kShares) return;
+    const Piece p = a.pieces[number / kShares];
+    const Record r = a.tensors[p.tensor];
+    const int32_t t = *a.step;
+    const float scale = a.scale ? *a.scale : 1.0f;
+    const double rate = a.lr * r.rate * (a.rate ? static_cast<double>(*a.rate) : 1.0);
+    if (t < 1 || scale != scale) return;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t first = static_cast<uint64_t>(p.number) * kPieceBlocks + number % kShares * kBlocks;
+    using H = Held<W, G, MASTER, EIGHT>;
+    const auto factors = [&]() {
+        return Factors{scale, static_cast<float>(rate / (1.0 - exp(t * a.ln1))), static_cast<float>(1.0 / sqrt(1.0 - exp(t * a.ln2))),
+                       static_cast<float>(1.0 - rate * r.decay), a.b1, a.b2, a.g1, a.g2, a.eps};
+    };
+    const uint32_t key = mixed(mixed(a.seed + 0x9e3779b9u * static_cast<uint32_t>(t)) ^ static_cast<uint32_t>(r.number));
+    if ((first + kBlocks) * kBlock <= r.elements) {
+        constexpr uint32_t kTogether = EIGHT && PAST ? 2 : 1;   // blocks of a wave that are under way together
+        H h[kTogether];
+        const auto load = [&](uint32_t u) {
+#pragma unroll
+            for (uint32_t i = 0; i < kTogether; ++i) h[i].template load<PAST>(r, first + (u + i) * kWaves + wave, lane);
+        };
+        load(0);
+        const Factors f = factors();
+#pragma unroll 1
+        for (uint32_t u = 0; u < kBlocks / kWaves; u += kTogether) {
+            if (u > 0) load(u);
+#pragma unroll
+            for (uint32_t i = 0; i < kTogether; ++i)
+                h[i].step(r, f, first + (u + i) * kWaves + wave, lane, 4, key, [](auto* to, const auto& y) { store4<PAST>(to, y); });
+        }
+        return;
+    }
+    const Factors f = factors();
+    for (uint64_t block = first + wave; block < first + kBlocks && block * kBlock < r.elements; block += kWaves) {
+        const uint32_t left = left_of(r.elements, block * kBlock + lane * 4);
+        H h;
+        h.load(r, block, lane, left);
+        h.step(r, f, block, lane, left, key, [&](auto* to, const auto& y) { store_some(to, y, left); });
     }
 }
 
@@ -287,6 +393,7 @@ struct Kind {   // tensors of the same types, pieces first .. first + n
     blink_dtype_t weights, grad, moments;
     bool master, stepped;
     uint32_t first, n;
+    uint64_t bytes;   // that a step reads
 };
 bool same(const Kind& k, const blink_update_tensor_t& t) {
     const bool stepped = t.weights != nullptr;
@@ -302,7 +409,7 @@ struct blink_update {
     void* block = nullptr;                 // records, then pieces
     const blink::Record* tensors = nullptr;
     const blink::Piece* pieces = nullptr;
-    uint32_t n_pieces = 0;
+    uint64_t bytes = 0;                    // that a step reads
     std::vector<blink::Kind> kinds;        // those of one gradient type next to one another
 };
 
@@ -348,7 +455,7 @@ blink_status_t make_update(const blink_update_tensor_t* tensors, int n, blink_up
         while (k < kinds.size() && !same(kinds[k], tensors[i])) ++k;
         if (k == kinds.size()) {
             const blink_update_tensor_t& t = tensors[i];
-            kinds.push_back({t.weight_type, t.grad_type, t.moment_type, t.master != nullptr, t.weights != nullptr, 0, 0});
+            kinds.push_back({t.weight_type, t.grad_type, t.moment_type, t.master != nullptr, t.weights != nullptr, 0, 0, 0});
             members.emplace_back();
         }
         members[k].push_back(i);
@@ -377,13 +484,14 @@ blink_status_t make_update(const blink_update_tensor_t* tensors, int n, blink_up
         for (const int i : members[k]) {
             const blink_update_tensor_t& t = tensors[i];
             record[i] = {t.weights, t.master, t.grad, t.moment1, t.moment2, t.scale1, t.scale2, t.elements, t.rate, t.decay, static_cast<uint64_t>(i)};
+            kind.bytes += t.elements * (size_of(t.grad_type) + (t.master ? 4 : size_of(t.weight_type)) + (t.moment_type == BLINK_FP8 ? 2 : 8));
             const uint32_t pieces = static_cast<uint32_t>(ceil_div(t.elements, kPiece));
             for (uint32_t j = 0; j < pieces; ++j) piece[at++] = {static_cast<uint32_t>(i), j};
         }
         kind.n = at - kind.first;
         u->kinds.push_back(kind);
     }
-    u->n_pieces = at;
+    for (const Kind& k : u->kinds) u->bytes += k.stepped ? k.bytes : 0;
     BLINK_HIP(hipGetDevice(&u->device));
     BLINK_HIP(hipMalloc(&u->block, bytes));
     BLINK_HIP(hipMemcpy(u->block, host.data(), bytes, hipMemcpyHostToDevice));
@@ -408,17 +516,30 @@ size_t gradient_norm_workspace(const blink_update& u) {
 
 blink_status_t gradient_norm(const blink_update& u, double most, double factor, float* norm, int32_t* step, void* workspace, hipStream_t stream) {
     BLINK_TRY(on_its_device(u));
+    const Clip clip{most, factor, norm, step};
     double* const sums = static_cast<double*>(workspace);
-    uint32_t at = 0;
+    uint32_t at = 0, types = 0;
     blink_status_t st = BLINK_OK;
+    each_gradient(u, [&](uint32_t, uint32_t, blink_dtype_t) { ++types; });
+    bool done = false;
     each_gradient(u, [&](uint32_t first, uint32_t n, blink_dtype_t grad) {
+        if (types == 1 && n <= kFew) {
+            done = true;
+            st = with_float(grad, [&](auto g) {
+                return launch(update_few<decltype(g)>, dim3(1), dim3(kFewThreads), stream, Norm{u.tensors, u.pieces + first, n, nullptr}, clip);
+            });
+            return;
+        }
         const uint32_t groups = groups_of(n);
         const Norm a{u.tensors, u.pieces + first, n, sums + at};
         at += groups;
-        if (st == BLINK_OK) st = with_float(grad, [&](auto g) { return launch(update_squares<decltype(g)>, dim3(groups), dim3(kThreads), stream, a); });
+        const bool past = static_cast<uint64_t>(n) * kPiece * size_of(grad) > kCache;
+        if (st == BLINK_OK) st = with_float(grad, [&](auto g) {
+            return launch(past ? update_squares<decltype(g), true> : update_squares<decltype(g), false>, dim3(groups), dim3(kThreads), stream, a);
+        });
     });
-    BLINK_TRY(st);
-    return launch(update_norm, dim3(1), dim3(kThreads), stream, sums, at, most, factor, norm, step);
+    if (done || st != BLINK_OK) return st;
+    return launch(update_norm, dim3(1), dim3(kThreads), stream, sums, at, clip);
 }
 
 blink_status_t adamw_step(const blink_update& u, const int32_t* step, double lr, double beta1, double beta2, double eps, const float* scale, const float* rate,
@@ -432,11 +553,17 @@ blink_status_t adamw_step(const blink_update& u, const int32_t* step, double lr,
             return with_float(k.grad, [&](auto g) {
                 using W = decltype(w);
                 using G = decltype(g);
-                const Grid grid = grid_of(k.n, kThreads);
-                const auto run = [&](void (*kernel)(Step)) { return launch(kernel, dim3(grid.x, grid.y), dim3(kThreads), stream, a); };
+                const bool beyond = u.bytes > kCache;
+                const Grid grid = grid_of(beyond ? k.n : 2 * static_cast<uint64_t>(k.n), kThreads);
+                const auto run = [&](void (*here)(Step), void (*past)(Step)) {
+                    return launch(beyond ? past : here, dim3(grid.x, grid.y), dim3(kThreads), stream, a);
+                };
                 if constexpr (!std::is_same<W, float>::value)
-                    if (k.master) return k.moments == BLINK_FP32 ? run(update_adamw<W, G, true, false>) : run(update_adamw<W, G, true, true>);
-                return k.moments == BLINK_FP32 ? run(update_adamw<W, G, false, false>) : run(update_adamw<W, G, false, true>);
+                    if (k.master)
+                        return k.moments == BLINK_FP32 ? run(update_adamw<W, G, true, false, false>, update_adamw<W, G, true, false, true>)
+                                                       : run(update_adamw<W, G, true, true, false>, update_adamw<W, G, true, true, true>);
+                return k.moments == BLINK_FP32 ? run(update_adamw<W, G, false, false, false>, update_adamw<W, G, false, false, true>)
+                                               : run(update_adamw<W, G, false, true, false>, update_adamw<W, G, false, true, true>);
             });
         }));
     }
