@@ -8,9 +8,17 @@ Every rank holds the same parameters (an embedding table and a router's matrix) 
   AllReduce of the gradient buffers along packed trees
   the table moves against its gradient, the router's matrix by an orthogonalised update with momentum
 
-All ranks end with the same parameters, bit for bit: the trees fix the order of every sum, and no operator adds by atomics.
+With --balance bias experts are kept evenly used by a bias instead of a loss, and the table moves by AdamW:
 
-  python examples/data_parallel_step.py [--steps 20] [--ranks 4]
+  router's logits -> the k experts with the largest sigmoid + bias in the best groups, their counts
+  AllReduce of counts -> every rank's bias a step up or down
+  AllReduce of the gradient buffers -> the norm of the whole gradient, from which both updates are clipped alike
+  the table moves by AdamW with its moments in 8 bits, the router's matrix by the orthogonalised update
+
+All ranks end with the same parameters, bit for bit: the trees fix the order of every sum, no operator adds by atomics, and the random bits that
+round moments are those of a seed.
+
+  python examples/data_parallel_step.py [--steps 20] [--ranks 4] [--balance loss|bias]
 """
 import argparse
 import os
@@ -85,13 +93,72 @@ class Trainer:
         return torch.stack((task, self.loss[1], self.loss[2]))
 
 
+class BiasTrainer(Trainer):
+    """The same with experts balanced by a bias, gradients clipped by their norm and AdamW for the table."""
+
+    def __init__(self, ranks=4, tokens=512, vocab=1000, dim=64, experts=16, k=2, seed=0, groups=4, kept=2, max_norm=1.0):
+        super().__init__(ranks, tokens, vocab, dim, experts, k, seed)
+        self.groups, self.kept, self.max_norm = groups, kept, max_norm
+        split, blocks = vocab * dim, -(-vocab * dim // 256)
+        self.bias = [torch.zeros(experts, device="cuda") for _ in range(ranks)]
+        self.moments = [[torch.zeros(split, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)] for _ in range(ranks)]
+        self.scales = [[torch.zeros(blocks, device="cuda") for _ in range(2)] for _ in range(ranks)]
+        self.norm = [torch.empty(2, device="cuda") for _ in range(ranks)]      # the gradient's norm, and what it is to be multiplied by
+        self.count = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(ranks)]
+        # the router's matrix has no weights in the list: its gradient counts in the norm, its update is the orthogonalised one
+        self.update = [bl.blink_make_update([self.grad[r][:split], self.grad[r][split:]], [self.table[r].view(-1), None], [self.moments[r][0], None],
+                                            [self.moments[r][1], None], scales1=[self.scales[r][0], None], scales2=[self.scales[r][1], None])
+                       for r in range(ranks)]
+        size = max(self.work.numel(), bl.blink_route_biased_workspace(tokens, experts), *(bl.blink_gradient_norm_workspace(u) for u in self.update))
+        self.work = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def step(self, rate=0.02):
+        """One step; the weight that tokens give to their own experts, a mean over all ranks, and how unevenly experts are used (the largest count over the mean)."""
+        stream = torch.cuda.current_stream().cuda_stream
+        n, e, k = self.tokens, self.experts, self.k
+        held = []
+        for r in range(self.ranks):
+            rows = torch.empty(n, self.dim, device="cuda")
+            bl.blink_embedding(self.table[r], self.batch[r], rows, 1.0, stream)
+            logits = rows @ self.router[r]
+            keep = self.batch[r] >= 0
+            chosen, weights = torch.empty(n, k, dtype=torch.int32, device="cuda"), torch.empty(n, k, device="cuda")
+            bl.blink_route_biased(logits, k, chosen, weights, self.counts[r], self.work, self.bias[r], keep, self.groups, self.kept, "sigmoid", True, 1.0, stream)
+            held.append((rows, logits, keep, chosen, weights))
+        bl.blink_allreduce(self.counts, e + 1, bl.BLINK_INT32, self.sum_of[e + 1], stream)
+        task = torch.zeros((), device="cuda")
+        split = self.vocab * self.dim
+        for r, (rows, logits, keep, chosen, weights) in enumerate(held):
+            bl.blink_route_bias(self.counts[r], self.bias[r], self.bias[r], 0.01 * rate, stream)
+            own = (chosen == self.label[self.batch[r].clamp(min=0)][:, None]) & keep[:, None]
+            grad_weights = -own.float() / self.counts[r][e]
+            task -= (own * weights).sum() / self.counts[r][e]
+            grad_logits = torch.empty_like(logits)
+            bl.blink_route_biased_gradient(logits, k, chosen, grad_weights, grad_logits, keep, "sigmoid", True, 1.0, stream)
+            torch.mm(rows.t(), grad_logits, out=self.grad[r][split:].view(self.dim, e))
+            grad_rows = grad_logits @ self.router[r].t()
+            bl.blink_embedding_gradient(self.batch[r], grad_rows, self.grad[r][:split].view(self.vocab, self.dim), self.work, 1.0, False, stream)
+        bl.blink_allreduce(self.grad, self.n, bl.BLINK_FP32, self.sum_of[self.n], stream)
+        for r in range(self.ranks):
+            bl.blink_gradient_norm(self.update[r], self.norm[r], self.work, self.max_norm, 1.0, self.count[r], stream)
+            bl.blink_adamw_step(self.update[r], self.count[r], rate, 0.9, 0.99, 1e-8, self.norm[r][1:], None, 1234, stream)
+            router = (self.grad[r][split:] * self.norm[r][1]).view(self.dim, e)
+            bl.blink_orthogonal_step(self.router[r], self.momentum[r], router, self.router[r], self.momentum[r], self.work, rate, 0.9, True, stream=stream)
+        return torch.stack((task, self.counts[0][:e].max() * e / self.counts[0][:e].sum()))
+
+
 def main():
     parser = argparse.ArgumentParser()
     parser.add_argument("--steps", type=int, default=20)
     parser.add_argument("--ranks", type=int, default=4)
+    parser.add_argument("--balance", choices=("loss", "bias"), default="loss")
     a = parser.parse_args()
-    trainer = Trainer(ranks=a.ranks)
+    trainer = (BiasTrainer if a.balance == "bias" else Trainer)(ranks=a.ranks)
     for i in range(a.steps):
+        if a.balance == "bias":
+            task, uneven = trainer.step().tolist()
+            print(f"step {i + 1}: weight on a token's own expert {-task:.4f}, busiest expert {uneven:.2f} times the mean", flush=True)
+            continue
         task, balance, z = trainer.step().tolist()
         print(f"step {i + 1}: weight on a token's own expert {-task:.4f}, balance loss {balance:.4f}, z loss {z:.5f}", flush=True)
     same = all(torch.equal(t, trainer.table[0]) for t in trainer.table) and all(torch.equal(t, trainer.router[0]) for t in trainer.router)

@@ -178,6 +178,17 @@ def test_equal_scores_go_to_the_lowest_index(scores, dtype):
     assert run.chosen[0].tolist() == [0, 1, 2, 3, 4] and run.chosen[1].tolist()[0] == 50
 
 
+@pytest.mark.parametrize("groups,kept", [(1, 1), (8, 4), (5, 2)])
+def test_logits_that_are_often_equal(groups, kept):
+    """Multiples of 1/8 without a bias: most tokens have equal experts among their first, in one lane's neighbours, in several lanes, at the end of the choice."""
+    for e, dtype in ((80, F32), (80, B16), (240, B16), (1000, H16)):
+        logits = (8 * _logits(5000, e, F32, e)).round().div(8).to(dtype)
+        e_groups = groups if e % groups == 0 else 1
+        for bias in (None, torch.zeros(e, device="cuda"), torch.full((e,), -0.5, device="cuda")):
+            arguments = (logits, 8, bias, None, e_groups, min(kept, e_groups), "sigmoid", True)
+            _check(Run(*arguments), _want(*arguments), dtype)
+
+
 @pytest.mark.parametrize("groups,kept", [(1, 1), (8, 4)])
 @pytest.mark.parametrize("e", [64, 256])
 def test_scores_that_all_but_tie(e, groups, kept):

@@ -165,6 +165,28 @@ def test_step(weights, grads, master, eight):
         assert int(step) == t
 
 
+@pytest.mark.parametrize("weights,grads,master,eight", [(F32, F32, False, False), (F32, B16, False, True), (B16, F32, True, True), (H16, B16, True, False),
+                                                        (B16, F32, False, False)])
+def test_lists_larger_than_the_caches(weights, grads, master, eight):
+    """More than 256 MiB are read by another variant; here at odd places."""
+    T = Tensors([1, 30_000_001, 257, 18_000_003], weights, grads, master, eight, seed=3)
+    step, norm = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.empty(2, device="cuda")
+    bl.blink_gradient_norm(T.update, norm, _work(T.update), 0.5, 2.0, step, _stream())
+    want = 2 * math.sqrt(sum(float(v.double().square().sum()) for v in T.lists["grads"]))
+    assert abs(float(norm[0]) - want) <= 1.01 * 2.0 ** -24 * want
+    bl.blink_adamw_step(T.update, step, LR, B1, B2, EPS, norm[1:], None, 78, _stream())
+    _check(T, 1, float(norm[1]), 1.0, 78)
+
+
+def test_norm_larger_than_the_caches():
+    grads = [torch.randn(n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)) for n in (80_000_001, 5)]
+    update = bl.blink_make_update(grads)
+    norm = torch.empty(2, device="cuda")
+    bl.blink_gradient_norm(update, norm, _work(update), stream=_stream())
+    want = math.sqrt(sum(float(v.double().square().sum()) for v in grads))
+    assert abs(float(norm[0]) - want) <= 1.01 * 2.0 ** -24 * want
+
+
 @pytest.mark.parametrize("eight", [False, True])
 def test_first_step_from_zeros(eight):
     T = Tensors([1, 300, 4097], eight=eight)
