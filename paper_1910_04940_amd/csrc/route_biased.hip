@@ -22,7 +22,7 @@ namespace blink {
 namespace {
 
 constexpr int kThreads = kRouteThreads;
-constexpr int kMostGroups = 1024;        // workgroups: 16 waves on a CU
+constexpr int kMostGroups = 1280;        // workgroups: 20 waves on a CU
 constexpr double kInf64 = __builtin_inf();
 
 struct Biased {
@@ -311,7 +311,7 @@ struct Shared {   // of a workgroup
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
 // route_biased_exact.
 template <typename T, int L, int N, int M, int V>
-__global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased a) {
+__global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased a) {
     using S = Shared<L, N>;
     __shared__ S s;
     constexpr int NB = kNeighbours<T>, R = N / NB;   // runs of neighbours of a lane
@@ -345,8 +345,10 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
     for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         const bool keep = !a.keep || a.keep[token];
+        int here = lane;   // (or what only some calls need of all places, masks and groups, would be kept in registers for all tokens)
+        asm volatile("" : "+v"(here));
         float x[N];
-        load_logits<T, L, N, V>(x, row, lane, a.experts);
+        load_logits<T, L, N, V>(x, row, here, a.experts);
         if (a.keep)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = keep ? x[i] : -kInf;
@@ -444,7 +446,7 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
                 wave_sync();
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) mine.sums[expert_of<T, L>(lane, i)] = v[i];
+                for (int i = 0; i < N; ++i) mine.sums[expert_of<T, L>(here, i)] = v[i];
                 wave_sync();
                 for (int g = lane; g < a.groups; g += L) {
                     Two two;
@@ -471,10 +473,11 @@ __global__ __launch_bounds__(kThreads, 4) void route_biased_choose(const Biased 
                 low = lanes_or<L>(low);
                 high = lanes_or<L>(high);
                 wave_sync();
+                const uint64_t stay = static_cast<uint64_t>(high) << 32 | low;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int g = group_of(expert_of<T, L>(lane, i));
-                    v[i] = pick((g < 32 ? low >> (g & 31) : high >> (g & 31)) & 1, v[i], none);
+                    const int g = group_of(expert_of<T, L>(here, i));
+                    v[i] = pick(stay >> (g & 63) & 1, v[i], none);
                 }
             }
             const int32_t last = mine.edge[0], next = mine.edge[1];

@@ -156,10 +156,12 @@ __global__ __launch_bounds__(kThreads) void update_squares(const Norm a) {
     s = add_up(s, part);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
-__global__ __launch_bounds__(kThreads) void update_norm(const double* sums, uint32_t n, const Clip clip) {
-    __shared__ double part[kWaves];
+constexpr int kNormThreads = 1024;   // two sums to each at the most: 3.0 us of 2048, 4.4 with 256 threads
+__global__ __launch_bounds__(kNormThreads) void update_norm(const double* sums, uint32_t n, const Clip clip) {
+    __shared__ double part[kNormThreads / 64];
     double s = 0.0;
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) s += sums[i];
+#pragma unroll 2
+    for (uint32_t i = threadIdx.x; i < n; i += kNormThreads) s += sums[i];
     s = add_up(s, part);
     if (threadIdx.x == 0) clip.finish(s);
 }
@@ -539,7 +541,7 @@ blink_status_t gradient_norm(const blink_update& u, double most, double factor, 
         });
     });
     if (done || st != BLINK_OK) return st;
-    return launch(update_norm, dim3(1), dim3(kThreads), stream, sums, at, clip);
+    return launch(update_norm, dim3(1), dim3(kNormThreads), stream, sums, at, clip);
 }
 
 blink_status_t adamw_step(const blink_update& u, const int32_t* step, double lr, double beta1, double beta2, double eps, const float* scale, const float* rate,
