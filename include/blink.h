@@ -57,7 +57,7 @@ typedef enum {
     BLINK_EINVAL = 1,        /* bad argument (null pointer, k < 2, bad vertex id, capacity <= 0, chunk 0, misaligned buffer ...) */
     BLINK_EDISCONNECTED = 2, /* some vertex cannot be reached from the root: rate 0 */
     BLINK_ENOMEM = 3,        /* host or device allocation failed */
-    BLINK_EMISMATCH = 4,     /* schedule does not fit the call (k, n, collective) */
+    BLINK_EMISMATCH = 4,     /* schedule does not fit the call (k, n, collective), or a list's tensors are on another device */
     BLINK_EHIP = 5,          /* a HIP runtime call failed (no device, launch error) */
     BLINK_ESTUCK = 6,        /* a stage gave up waiting for another one, or calls overlapped (see blink_schedule_status) */
     BLINK_ELIMIT = 7         /* the schedule does not fit the fixed device block of blink_allreduce_noalloc */

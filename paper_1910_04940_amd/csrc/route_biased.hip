@@ -310,6 +310,9 @@ struct Shared {   // of a workgroup
 
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
 // route_biased_exact.
+// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 105 us, 698 a wave for four tokens (32 of them powers and reciprocals at a quarter of
+// the rate), issued three quarters of the time; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than four.  Without groups
+// 90 us.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their sums go through LDS (20011 x 60 in six groups 10.6 us, the latency of one pass).
 template <typename T, int L, int N, int M, int V>
 __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased a) {
     using S = Shared<L, N>;
@@ -625,6 +628,7 @@ struct BiasedGradient {
     bool past;
 };
 
+// A chosen logit lies in a line of its own, so that nearly all of the logits are read again: 262144 x 256 bfloat16, k = 8, 123 MB read and 134 written, 44 us.
 template <typename T, int L, int N, int V>
 __global__ __launch_bounds__(kThreads) void route_biased_gradient_kernel(const BiasedGradient a) {
     // what the token's chosen get (with a whole softmax: d), 0 wherever no token's are; four neighbours of each lane side by side

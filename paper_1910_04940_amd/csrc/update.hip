@@ -148,6 +148,8 @@ __device__ inline double squares_of(const Norm& a, uint32_t piece, uint32_t thre
     }
     return s;
 }
+// Bound by memory: 151 M fp32 gradients 91 us, 6.6 TB/s; loads past the caches 102, others 109 (168 M).  Gradients that fit the memory-side cache are left
+// there for the step.
 template <typename G, bool PAST>
 __global__ __launch_bounds__(kThreads) void update_squares(const Norm a) {
     __shared__ double part[kWaves];
@@ -338,7 +340,13 @@ struct Held {
     }
 };
 
-// W, G: types of the weights and the gradient; MASTER: weights are the rounding of a copy in 32 bits; EIGHT: moments in 8 bits.
+// W, G: types of the weights and the gradient; MASTER: weights are the rounding of a copy in 32 bits; EIGHT: moments in 8 bits.  Bound by memory.
+// Lists that read more than the memory-side cache holds go past the caches (PAST): 168 M fp32 elements, 4.7 GB, 860 us otherwise, 830 so, and 752 (6.2 TB/s)
+// with three workgroups on a unit, which follow one another closely through memory (four 790, two 835).  In 8 bits (16-bit weights with a copy,
+// 3.0 GB) there is more to compute, 97 vector instructions an element: as many workgroups as fit, both blocks of a wave loaded
+// before either is computed, 506 to 555 us (six TB/s at the best); with LDS for three workgroups 650, one block after the other 600.
+// Smaller lists are served by that cache when they were written a step ago: half a piece to a workgroup, 4.9 M elements 19.9 us, a whole one 21.3, past
+// the caches 27.
 template <typename W, typename G, bool MASTER, bool EIGHT, bool PAST>
 __global__ __launch_bounds__(kThreads) void update_adamw(const Step a) {
     if constexpr (PAST && !EIGHT) {   // LDS that nobody uses, so that three workgroups are on a compute unit

@@ -301,7 +301,7 @@ class Update:
         self.tensors = tensors
 
     def __del__(self):
-        if getattr(self, "_h", None) and binding._lib is not None:
+        if getattr(self, "_h", None) and binding is not None and binding._lib is not None:
             binding._lib.blink_update_free(self._h)
             self._h = self._address = None
 
