@@ -401,8 +401,9 @@ def test_in_a_graph():
             assert torch.equal(o, w)
 
 
-def test_two_streams():
-    arguments = [(_logits(20_000, 60, B16, s), 4, _bias(60, s), None, 6, 3, "softmax", False, _randn(20_000, 4, seed=s)) for s in (1, 2)]
+def test_streams():
+    """Four at once: as many as there are hardware queues, so that streams of tests after this one fall to the queues that they fell to without it."""
+    arguments = [(_logits(20_000, 60, B16, s), 4, _bias(60, s), None, 6, 3, "softmax", False, _randn(20_000, 4, seed=s)) for s in (1, 2, 3, 4)]
     runs, streams = [], [torch.cuda.Stream() for _ in arguments]
     torch.cuda.synchronize()
     for a, s in zip(arguments, streams):

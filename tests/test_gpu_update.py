@@ -230,6 +230,19 @@ def test_norm_of_all_types_together():
     assert abs(float(norm[0]) - want) <= 1.01 * 2.0 ** -24 * want and norm[1] == 1
 
 
+def test_nothing_to_do():
+    """Tensors without elements, a list without weights."""
+    empty = torch.zeros(0, device="cuda")
+    update = bl.blink_make_update([empty, empty], [empty, None], [empty, None], [empty, None])
+    norm, step = torch.full((2,), 9.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bl.blink_gradient_norm(update, norm, None, 1.0, 0.5, step, _stream())
+    assert norm.tolist() == [0.0, 0.5] and int(step) == 1
+    bl.blink_adamw_step(update, step, LR, stream=_stream())
+    grad = torch.ones(5, device="cuda")
+    bl.blink_adamw_step(bl.blink_make_update([grad]), step, LR, stream=_stream())
+    assert (grad == 1).all()
+
+
 def test_sizes_of_gradients():
     """Squares beyond and below what 32 bits hold; nothing but zeros."""
     for value, most, scale in ((3e38, 1.0, None), (1e-38, 1e-40, None), (0.0, 1.0, 2.0)):
@@ -341,9 +354,9 @@ def test_in_a_graph():
                 assert torch.equal(T.flat[name].view(torch.uint8), U.flat[name].view(torch.uint8)), name
 
 
-def test_two_streams():
-    """Two lists on streams of their own."""
-    both = [Tensors([200_001, 7], B16, F32, True, True, s) for s in (1, 2)]
+def test_streams():
+    """Four lists on streams of their own: as many as there are hardware queues, so that streams of later tests fall to the queues that they fell to without it."""
+    both = [Tensors([200_001, 7], B16, F32, True, True, s) for s in (1, 2, 3, 4)]
     streams = [torch.cuda.Stream() for _ in both]
     state = []
     torch.cuda.synchronize()
@@ -351,9 +364,8 @@ def test_two_streams():
         with torch.cuda.stream(s):
             norm, step = torch.empty(2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
             work = _work(T.update)
-            for _ in range(1):
-                bl.blink_gradient_norm(T.update, norm, work, math.inf, 1.0, step, s.cuda_stream)
-                bl.blink_adamw_step(T.update, step, LR, B1, B2, EPS, norm[1:], None, 6, s.cuda_stream)
+            bl.blink_gradient_norm(T.update, norm, work, math.inf, 1.0, step, s.cuda_stream)
+            bl.blink_adamw_step(T.update, step, LR, B1, B2, EPS, norm[1:], None, 6, s.cuda_stream)
             state.append((norm, step, work))
     torch.cuda.synchronize()
     for T in both:
