@@ -91,6 +91,42 @@ __device__ inline void weigh(const Biased& a, uint64_t token, const T* row, int 
     }
 }
 
+// The same of at most S chosen to a lane, in registers: e[i] the (lane + L i)-th, -1 past the last.
+template <typename T, int L, int S>
+__device__ inline void weigh_few(const Biased& a, uint64_t token, const T* row, int lane, float most, float sum, int32_t* count,
+                                 const int (&e)[S]) {
+    float x[S], part[S], c = 0.0f, all = 1.0f;
+#pragma unroll
+    for (int i = 0; i < S; ++i) x[i] = e[i] >= 0 ? static_cast<float>(row[e[i]]) : -kInf;
+    if (a.normalize) {
+        c = x[0];
+#pragma unroll
+        for (int i = 1; i < S; ++i) c = __builtin_fmaxf(c, x[i]);
+        c = lanes_max<L>(c);
+        if (!a.soft) c = __builtin_fminf(c, 0.0f);
+    } else if (a.soft) {
+        c = most;
+        all = sum;
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) part[i] = e[i] >= 0 ? part_of(a.soft, x[i], c) : 0.0f;
+    if (a.normalize) {
+        all = part[0];
+#pragma unroll
+        for (int i = 1; i < S; ++i) all += part[i];
+        all = lanes_sum<L>(all);
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const int j = lane + i * L;
+        if (j >= a.k) break;
+        a.chosen[token * a.k + j] = e[i];
+        a.weights[token * a.k + j] = e[i] < 0 ? 0.0f : a.scale * (part[i] / all);
+        if (e[i] >= 0) atomicAdd(&count[e[i]], 1);
+        if (e[i] >= 0 && j == 0) atomicAdd(&count[a.experts], 1);
+    }
+}
+
 template <int L>
 __device__ inline void choose_none(const Biased& a, uint64_t token, int lane) {
     for (int j = lane; j < a.k; j += L) {
@@ -119,8 +155,10 @@ __device__ inline Two64 joined(Two64 a, Two64 b) {
 
 // A wave to a token, N experts to a lane, expert 64 i + lane the i-th: for the tokens that a workgroup of route_biased_choose left in its list, for calls of a
 // few tokens and for k above kMostFast.
+// Bound by one token's chain of 64-bit instructions: 2100 tokens of 256 experts, eight groups, 15 us.  Six waves on a SIMD hold all 640 workgroups at once; with the
+// registers for five, which hold 512, it was 21, with a workgroup of four waves for each list 25.
 template <typename T, int N>
-__global__ __launch_bounds__(kExactThreads) void route_biased_exact(const Biased a) {
+__global__ __launch_bounds__(kExactThreads, N <= 4 ? 6 : 2) void route_biased_exact(const Biased a) {
     __shared__ int32_t count[64 * N + 1];
     __shared__ double sums[kExactThreads / 64][64 * N];
     const int t = threadIdx.x, lane = t & 63;
@@ -129,7 +167,8 @@ __global__ __launch_bounds__(kExactThreads) void route_biased_exact(const Biased
     const uint32_t mine = list ? a.left[first] : 0;
     const uint64_t n = list ? mine + (first + 1 < a.lists ? a.left[first + 1] : 0) : a.tokens;
     if (list && n == 0) return;
-    for (int i = t; i <= a.experts; i += kExactThreads) count[i] = 0;
+    int32_t* const counts = a.counts + static_cast<uint64_t>(list ? first : blockIdx.x) * (a.experts + 1);
+    for (int i = t; i <= a.experts; i += kExactThreads) count[i] = list ? counts[i] : 0;
     __syncthreads();
     const uint64_t wave = (list ? 0 : blockIdx.x) * (kExactThreads / 64) + t / 64, step = (list ? 1 : gridDim.x) * (kExactThreads / 64);
     for (uint64_t at = wave; at < n; at += step) {
@@ -218,8 +257,7 @@ __global__ __launch_bounds__(kExactThreads) void route_biased_exact(const Biased
         weigh<T, 64>(a, token, row, lane, most, sum, count, [&](int j) { return j == lane ? own : chosen[j]; });   // (each lane its own)
     }
     __syncthreads();
-    int32_t* const counts = a.counts + static_cast<uint64_t>(list ? first : blockIdx.x) * (a.experts + 1);
-    for (int i = t; i <= a.experts; i += kExactThreads) counts[i] = (list ? counts[i] : 0) + count[i];
+    for (int i = t; i <= a.experts; i += kExactThreads) counts[i] = count[i];
 }
 
 // ---- the choice in 32 bits, where it is sure --------------------------------------------------------------------------------
@@ -310,14 +348,16 @@ struct Shared {   // of a workgroup
 
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
 // route_biased_exact.
-// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 105 us, 698 a wave for four tokens (32 of them powers and reciprocals at a quarter of
-// the rate), issued three quarters of the time; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than four.  Without groups
-// 90 us.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their sums go through LDS (20011 x 60 in six groups 10.6 us, the latency of one pass).
+// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 104 us, 662 a wave for four tokens (32 of them powers and reciprocals at a quarter of
+// the rate), issued three quarters of the time; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than four, a lane's chosen in registers
+// rather than read from LDS for each of their uses 2.5 % (698 instructions).  Without groups 89 us.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes
+// their sums go through LDS (20011 x 60 in six groups 10.4 us, the latency of one pass).
 template <typename T, int L, int N, int M, int V>
 __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased a) {
     using S = Shared<L, N>;
     __shared__ S s;
     constexpr int NB = kNeighbours<T>, R = N / NB;   // runs of neighbours of a lane
+    constexpr int kSlots = (M + L - 1) / L;          // of a lane's chosen
     const int t = threadIdx.x, lane = t & (L - 1);
     if (t == 0) s.left = 0;
     for (int i = t; i <= a.experts; i += kThreads) s.count[i] = 0;
@@ -547,11 +587,18 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
             return w.x < 0 ? -1 : (i / NB * L + w.y) * NB + i % NB;
         };
         const auto at = [&](int j) { return *reinterpret_cast<const int2*>(mine.won[j]); };
-        for (int j = lane; j < a.k; j += L) {
-            const int2 w = at(j), then = j + 1 < a.k ? at(j + 1) : int2{next, 0};
-            if (!bad && then.x >= 0 && !(float_of(w.x) - float_of(then.x) > near)) {   // (a NaN's keys may stand for no expert)
-                const int e = expert_at(w), f = expert_at(then);
-                sure &= j + 1 < a.k && row[e] == row[f] && (!a.bias || a.bias[e] == a.bias[f]);
+        int chosen[kSlots];
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            const int j = lane + i * L;
+            chosen[i] = -1;
+            if (j < a.k) {
+                const int2 w = at(j), then = j + 1 < a.k ? at(j + 1) : int2{next, 0};
+                chosen[i] = expert_at(w);
+                if (!bad && then.x >= 0 && !(float_of(w.x) - float_of(then.x) > near)) {   // (a NaN's keys may stand for no expert)
+                    const int e = chosen[i], f = expert_at(then);
+                    sure &= j + 1 < a.k && row[e] == row[f] && (!a.bias || a.bias[e] == a.bias[f]);
+                }
             }
         }
         sure = !lanes_or<L>(static_cast<unsigned>(!sure));
@@ -560,9 +607,7 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
         } else if (!sure) {
             if (lane == 0) a.later[static_cast<uint64_t>(blockIdx.x) * a.room + atomicAdd(&s.left, 1u)] = static_cast<uint32_t>(token);
         } else {
-            const auto chosen = [&](int j) { return expert_at(at(j)); };
-            for (int j = lane; j < a.k; j += L) a.chosen[token * a.k + j] = chosen(j);
-            weigh<T, L>(a, token, row, lane, most, sum, s.count, chosen);
+            weigh_few<T, L, kSlots>(a, token, row, lane, most, sum, s.count, chosen);
         }
     }
     __syncthreads();
