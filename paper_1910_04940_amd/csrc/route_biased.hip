@@ -32,7 +32,7 @@ struct Biased {
     const float* bias;     // null: 0
     uint32_t tokens;
     int experts, k, groups, kept;
-    bool soft, normalize;
+    int soft, normalize;   // or not
     float scale;
     int32_t* chosen;
     float* weights;
@@ -336,6 +336,7 @@ struct Shared {   // of a workgroup
     static constexpr int kGroups = L * N < 64 ? L * N : 64;
     int32_t count[L * N + 1];
     uint32_t left;
+    alignas(8) int32_t lost[kMostFast][2];        // what lanes write that did not win, and nobody reads
     union Token {      // one after the other
         struct {
             alignas(16) int32_t group[kGroups];   // keys of groups
@@ -348,25 +349,26 @@ struct Shared {   // of a workgroup
 
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
 // route_biased_exact.
-// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 104 us, 662 a wave for four tokens (32 of them powers and reciprocals at a quarter of
-// the rate), issued three quarters of the time; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than four, a lane's chosen in registers
-// rather than read from LDS for each of their uses 2.5 % (698 instructions).  Without groups 89 us.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes
-// their sums go through LDS (20011 x 60 in six groups 10.4 us, the latency of one pass).
+// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 95 us; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than
+// four, a lane's chosen in registers rather than read from LDS for each of their uses 2.5 %.  The call's numbers are asked of for each token: kept as masks of lanes
+// they fill the scalar registers and move to vector registers and back, which with a branch around each write of a winner, whose two
+// sides both move the lane's keys, took 104 us.  Without groups 89 us (before that).  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their
+// sums go through LDS (20011 x 60 in six groups 9.9 us, the latency of one pass).
 template <typename T, int L, int N, int M, int V>
-__global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased a) {
+__global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased args) {
     using S = Shared<L, N>;
     __shared__ S s;
     constexpr int NB = kNeighbours<T>, R = N / NB;   // runs of neighbours of a lane
     constexpr int kSlots = (M + L - 1) / L;          // of a lane's chosen
     const int t = threadIdx.x, lane = t & (L - 1);
     if (t == 0) s.left = 0;
-    for (int i = t; i <= a.experts; i += kThreads) s.count[i] = 0;
+    for (int i = t; i <= args.experts; i += kThreads) s.count[i] = 0;
     __syncthreads();
     float bias[N], widest = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int e = expert_of<T, L>(lane, i);
-        bias[i] = e >= a.experts ? -kInf : a.bias ? a.bias[e] : 0.0f;
+        bias[i] = e >= args.experts ? -kInf : args.bias ? args.bias[e] : 0.0f;
         if (bias[i] > -kInf) widest = __builtin_fmaxf(widest, __builtin_fabsf(bias[i]));
     }
     widest = lanes_max<L>(widest);
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
     const int32_t none = none_of(lane);
     const float rounded = (1.0f + 4.0f * widest) * 0x1p-23f;
     // groups that are runs of P lanes, or not
-    const int size = a.experts / a.groups, P = size / NB;
+    const int size = args.experts / args.groups, P = size / NB;
     const bool runs = size % NB == 0 && (P & (P - 1)) == 0 && P <= L && P <= 16;
     const int shift = 31 - __builtin_clz(P | 1);
     // e / size for e and size below 2^10: e * (2^20 / size, rounded up) is off by less than 2^20
@@ -385,7 +387,9 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
     const auto group_of = [&](int e) { return static_cast<int>(e * by_size >> 20); };
     typename S::Token& mine = s.token[t / L];
     const uint32_t step = gridDim.x * (kThreads / L);
-    for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < a.tokens; token += step) {
+    for (uint64_t token = blockIdx.x * (kThreads / L) + t / L; token < args.tokens; token += step) {
+        Biased a = args;   // (see above)
+        asm volatile("" : "+s"(a.k), "+s"(a.groups), "+s"(a.kept), "+s"(a.soft), "+s"(a.normalize));
         const T* const row = static_cast<const T*>(a.logits) + token * a.stride;
         const bool keep = !a.keep || a.keep[token];
         int here = lane;   // (or what only some calls need of all places, masks and groups, would be kept in registers for all tokens)
@@ -395,15 +399,9 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
         if (a.keep)
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = keep ? x[i] : -kInf;
-        // infinities and NaN: largest as whole numbers, with and without a sign
-        int32_t above = bits_of(x[0]);
-        uint32_t below = above;
+        float least = x[0];   // (NaN if one is)
 #pragma unroll
-        for (int i = 1; i < N; ++i) {
-            above = max_of(above, bits_of(x[i]));
-            below = below > static_cast<uint32_t>(bits_of(x[i])) ? below : bits_of(x[i]);
-        }
-        const bool special = above >= 0x7f800000 || below >= 0xff800000u;
+        for (int i = 1; i < N; ++i) least = __builtin_elementwise_minimum(least, x[i]);
         bool bad = false;
         float most = 0.0f, sum = 0.0f, off = kSigmoidOff;
         int32_t v[N];   // sums with the bias
@@ -432,7 +430,7 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = bits_of(p[i] + bias[i]);
         }
-        if (special) {
+        if (!(least > -kInf) || (a.soft && most == kInf)) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if (!(x[i] > -kInf)) v[i] = none;
@@ -554,7 +552,7 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
                 const int least = lanes_least<L>(won ? lane : L);   // (asked of all lanes)
                 won = won && lane == least;
             }
-            if (won) *reinterpret_cast<int2*>(mine.won[j]) = int2{first, lane};
+            *reinterpret_cast<int2*>((won ? mine.won : s.lost)[j]) = int2{first, lane};   // (see above)
             return won;
         };
         if constexpr (M == 8) {   // (what the j-th leaves behind of a lane's keys gets shorter)
@@ -611,8 +609,8 @@ __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(
         }
     }
     __syncthreads();
-    for (int i = t; i <= a.experts; i += kThreads) a.counts[static_cast<uint64_t>(blockIdx.x) * (a.experts + 1) + i] = s.count[i];
-    if (t == 0) a.left[blockIdx.x] = s.left;
+    for (int i = t; i <= args.experts; i += kThreads) args.counts[static_cast<uint64_t>(blockIdx.x) * (args.experts + 1) + i] = s.count[i];
+    if (t == 0) args.left[blockIdx.x] = s.left;
 }
 
 // Adds up what the workgroups left: eight columns to a workgroup, so that it has many loads under way at once.
