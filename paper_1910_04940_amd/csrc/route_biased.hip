@@ -155,8 +155,8 @@ __device__ inline Two64 joined(Two64 a, Two64 b) {
 
 // A wave to a token, N experts to a lane, expert 64 i + lane the i-th: for the tokens that a workgroup of route_biased_choose left in its list, for calls of a
 // few tokens and for k above kMostFast.
-// Bound by one token's chain of 64-bit instructions: 2100 tokens of 256 experts, eight groups, 15 us.  Six waves on a SIMD hold all 640 workgroups at once; with the
-// registers for five, which hold 512, it was 21, with a workgroup of four waves for each list 25.
+// Bound by one token's chain of 64-bit instructions: the tokens that 262144 x 256 leave, 0.8 % of them, 15 us.  Six waves on a SIMD hold all 640 workgroups at
+// once; with the registers for five, which hold 512, it was 21, with a workgroup of four waves for each list 25.
 template <typename T, int N>
 __global__ __launch_bounds__(kExactThreads, N <= 4 ? 6 : 2) void route_biased_exact(const Biased a) {
     __shared__ int32_t count[64 * N + 1];
@@ -349,11 +349,12 @@ struct Shared {   // of a workgroup
 
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
 // route_biased_exact.
-// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 95 us; all tokens in 64 bits took 630.  Five waves on a SIMD are 3 % faster than
-// four, a lane's chosen in registers rather than read from LDS for each of their uses 2.5 %.  The call's numbers are asked of for each token: kept as masks of lanes
-// they fill the scalar registers and move to vector registers and back, which with a branch around each write of a winner, whose two
-// sides both move the lane's keys, took 104 us.  Without groups 89 us (before that).  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their
-// sums go through LDS (20011 x 60 in six groups 9.9 us, the latency of one pass).
+// Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 94 us, 598 a wave for four tokens (32 of them powers and reciprocals at a quarter of
+// the rate); all tokens in 64 bits took 630.  Without groups 82 us.  What brought it there: five waves on a SIMD
+// rather than four, 3 %; a lane's chosen in registers, not read from LDS for each of their uses, 2.5 %; the call's numbers asked of for each token
+// and winners written without a branch, 9 %: kept as masks of lanes the numbers fill the scalar registers and move to vector registers and back, and both sides of
+// the branch moved the lane's keys.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their sums go through LDS (20011 x 60 in six groups
+// 9.8 us, the latency of one pass).
 template <typename T, int L, int N, int M, int V>
 __global__ __launch_bounds__(kThreads, L >= 8 ? 5 : 4) void route_biased_choose(const Biased args) {
     using S = Shared<L, N>;

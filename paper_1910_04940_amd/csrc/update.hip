@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void update_squares(const Norm a) {
     s = add_up(s, part);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
-constexpr int kNormThreads = 1024;   // two sums to each at the most: 3.0 us of 2048, 4.4 with 256 threads
+constexpr int kNormThreads = 1024;   // two sums to each at the most: 2.7 to 3.7 us of 2048, 4.1 with 256 threads
 __global__ __launch_bounds__(kNormThreads) void update_norm(const double* sums, uint32_t n, const Clip clip) {
     __shared__ double part[kNormThreads / 64];
     double s = 0.0;
