@@ -597,7 +597,8 @@ blink_status_t blink_orthogonal_step(const float* weights, float* weights_out, c
 
 /* The tensors that an optimiser changes, once for all steps: the list is read, and kept with the addresses in it, in device memory of the
  * current device (allocated and written synchronously, not while a stream is captured).  The calls below take it on that device (EMISMATCH on
- * another); it must outlive them, and graphs that hold them. */
+ * another); it must outlive them, and graphs that hold them.  What a step writes may overlap nothing else in the list (EINVAL): weights that
+ * two names stand for are listed once. */
 typedef struct {
     const void* grad;        /* [elements], of grad_type */
     void* weights;           /* [elements], of weight_type; null: the gradient counts in the norm, and the tensor is left to others */

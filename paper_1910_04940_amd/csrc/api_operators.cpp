@@ -1,6 +1,8 @@
 // extern "C" boundary of the operators around the collectives: argument checks.
+#include <algorithm>
 #include <cmath>
 #include <new>
+#include <vector>
 
 #include "operators_api.hpp"
 
@@ -29,6 +31,38 @@ bool tensor_ok(const blink_update_tensor_t& t) {
     return blink::aligned(t.weights, blink::size_of(t.weight_type)) && blink::aligned(t.master, 4) && buffer_ok(t.moment1, t.elements, eight ? 1 : 4) &&
            buffer_ok(t.moment2, t.elements, eight ? 1 : 4) && (eight ? buffer_ok(t.scale1, t.elements, 4) && buffer_ok(t.scale2, t.elements, 4) : !t.scale1 && !t.scale2) &&
            std::isfinite(t.rate) && std::isfinite(t.decay);
+}
+// Whether what a step writes is written by one tensor of the list, and read by no other: their workgroups run at once.
+bool tensors_apart(const blink_update_tensor_t* tensors, int n) {
+    struct Range {
+        uintptr_t from, to;
+        bool written;
+    };
+    std::vector<Range> all;
+    const auto add = [&](const void* p, size_t bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes) all.push_back({at, at + bytes, written});
+    };
+    for (int i = 0; i < n; ++i) {
+        const blink_update_tensor_t& t = tensors[i];
+        const size_t moment = t.moment_type == BLINK_FP8 ? 1 : 4, scales = (t.elements + 255) / 256 * 4;
+        add(t.grad, t.elements * blink::size_of(t.grad_type), false);
+        if (!t.weights) continue;
+        add(t.weights, t.elements * blink::size_of(t.weight_type), true);
+        add(t.master, t.elements * 4, true);
+        add(t.moment1, t.elements * moment, true);
+        add(t.moment2, t.elements * moment, true);
+        add(t.scale1, scales, true);
+        add(t.scale2, scales, true);
+    }
+    std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t read = 0, written = 0;   // where those so far end
+    for (const Range& r : all) {
+        if (r.from < written || (r.written && r.from < read)) return false;
+        uintptr_t& end = r.written ? written : read;
+        end = std::max(end, r.to);
+    }
+    return true;
 }
 
 }  // namespace
@@ -171,6 +205,7 @@ blink_status_t blink_make_update(const blink_update_tensor_t* tensors, int n, bl
     for (int i = 0; i < n; ++i)
         if (!tensor_ok(tensors[i])) return BLINK_EINVAL;
     try {
+        if (!tensors_apart(tensors, n)) return BLINK_EINVAL;
         return blink::make_update(tensors, n, out);
     } catch (...) {   // (nothing else throws)
         return BLINK_ENOMEM;

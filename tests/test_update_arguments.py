@@ -10,8 +10,8 @@ from paper_1910_04940_amd import binding
 torch = pytest.importorskip("torch")
 
 P = 1 << 20
-GOOD = dict(grad=P, weights=P, master=0, moment1=P, moment2=P, scale1=0, scale2=0, elements=1000, weight_type=1, grad_type=1, moment_type=1, rate=1.0, decay=0.0)
-EIGHT = dict(moment_type=5, scale1=P, scale2=P)
+GOOD = dict(grad=P, weights=2 * P, master=0, moment1=3 * P, moment2=4 * P, scale1=0, scale2=0, elements=1000, weight_type=1, grad_type=1, moment_type=1, rate=1.0, decay=0.0)
+EIGHT = dict(moment_type=5, scale1=5 * P, scale2=6 * P)
 
 
 def make(n=1, table=True, **change):
@@ -26,13 +26,48 @@ def make(n=1, table=True, **change):
 
 @pytest.mark.parametrize("change", [
     dict(n=0), dict(n=-1), dict(n=(1 << 20) + 1), dict(table=False), dict(grad=0), dict(grad=P + 2), dict(grad_type=0), dict(grad_type=4), dict(grad_type=5),
-    dict(weight_type=0), dict(weight_type=5), dict(weights=P + 2), dict(weights=P + 1, weight_type=2), dict(moment1=0), dict(moment2=0), dict(moment1=P + 2),
-    dict(moment_type=2), dict(moment_type=0), dict(master=P), dict(master=P + 2, weight_type=2), dict(scale1=P), dict(scale2=P), dict(moment_type=5),
-    {**EIGHT, "scale1": 0}, {**EIGHT, "scale2": P + 2}, dict(weights=0), dict(weights=0, moment1=0), dict(weights=0, moment1=0, moment2=0, master=P),
-    dict(weights=0, moment1=0, moment2=0, scale1=P), dict(elements=(1 << 40) + 1), dict(rate=float("nan")), dict(decay=float("inf")), dict(n=2, elements=1 << 40, rate=float("inf"))],
+    dict(weight_type=0), dict(weight_type=5), dict(weights=2 * P + 2), dict(weights=2 * P + 1, weight_type=2), dict(moment1=0), dict(moment2=0), dict(moment1=3 * P + 2),
+    dict(moment_type=2), dict(moment_type=0), dict(master=7 * P), dict(master=7 * P + 2, weight_type=2), dict(scale1=5 * P), dict(scale2=5 * P), dict(moment_type=5),
+    {**EIGHT, "scale1": 0}, {**EIGHT, "scale2": 6 * P + 2}, dict(weights=0), dict(weights=0, moment1=0), dict(weights=0, moment1=0, moment2=0, master=7 * P),
+    dict(weights=0, moment1=0, moment2=0, scale1=5 * P), dict(elements=(1 << 40) + 1), dict(rate=float("nan")), dict(decay=float("inf")), dict(n=2, elements=1 << 40, rate=float("inf"))],
     ids=str)
 def test_lists_that_are_refused(change):
     assert make(**change) == bl.BLINK_EINVAL
+
+
+def _two(**change):
+    """Two tensors of 1000 elements, 8000 bytes from one list to the next, of which `change` moves some: name -> (of which tensor, address)."""
+    row = np.zeros(2, binding.UPDATE_TENSOR_DTYPE)
+    for i in range(2):
+        for name, value in {**GOOD, "grad": P, "weights": P + 8000, "moment1": P + 16000, "moment2": P + 24000}.items():
+            row[name][i] = value + 4000 * i if value >= P else value
+    for name, (i, value) in change.items():
+        row[name][i] = value
+    return row
+
+
+@pytest.mark.parametrize("change", [
+    dict(weights=(1, P + 8000)), dict(weights=(1, P + 8004)), dict(weights=(0, P + 12000)), dict(moment1=(1, P + 16000)), dict(moment2=(1, P + 24000 + 3996)),
+    dict(moment1=(0, P + 24000)), dict(grad=(1, P + 8000)), dict(grad=(0, P + 8000 - 4)), dict(grad=(1, P + 28000 + 3996)), dict(weights=(0, P))], ids=str)
+def test_lists_that_write_a_place_twice(change):
+    """The same weights under two names, and what overlaps by an element: two workgroups would step it at once."""
+    row, out = _two(**change), C.c_void_p(1)
+    assert binding.lib().blink_make_update(row.ctypes.data, 2, C.byref(out)) == bl.BLINK_EINVAL and out.value is None
+
+
+@pytest.mark.gpu
+def test_lists_that_touch():
+    """Neighbours in one buffer, and one gradient for two tensors, are no overlap."""
+    buffer = torch.zeros(5, 2, 1000, device="cuda")
+    grad, weights, moment1, moment2, _ = (list(x) for x in buffer)
+    shared = [grad[0], grad[0]]
+    for grads in (grad, shared):
+        bl.blink_make_update(grads, weights, moment1, moment2)
+    for bad in (dict(weights=[weights[0]] * 2), dict(moments1=[moment1[1]] * 2), dict(moments2=[moment1[0], moment2[1]]), dict(grads=[grad[0], weights[0]]),
+                dict(weights=[buffer.view(-1)[2001:3001], buffer.view(-1)[3000:4000]])):
+        with pytest.raises(bl.BlinkError) as e:
+            bl.blink_make_update(**{**dict(grads=grad, weights=weights, moments1=moment1, moments2=moment2), **bad})
+        assert e.value.status == bl.BLINK_EINVAL
 
 
 def test_no_list():
