@@ -351,7 +351,7 @@ struct Shared {   // of a workgroup
 // route_biased_exact.
 // Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 94 us, 598 a wave for four tokens (32 of them powers and reciprocals at a quarter of
 // the rate); all tokens in 64 bits took 630.  Without groups 82 us.  What brought it there: five waves on a SIMD
-// rather than four, 3 %; a lane's chosen in registers, not read from LDS for each of their uses, 2.5 %; the call's numbers asked of for each token
+// (four 103, six, which spill, 110); a lane's chosen in registers, not read from LDS for each of their uses, 2.5 %; the call's numbers asked of for each token
 // and winners written without a branch, 9 %: kept as masks of lanes the numbers fill the scalar registers and move to vector registers and back, and both sides of
 // the branch moved the lane's keys.  Where groups are no runs of neighbours of 1, 2, 4 .. lanes their sums go through LDS (20011 x 60 in six groups
 // 9.8 us, the latency of one pass).
