@@ -439,3 +439,33 @@ def test_both_ways_from_python(monkeypatch):
     monkeypatch.setattr(operators, "_operators", {})
     for a, b in zip(native, all_of()):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("e,k", [(5, 2), (8, 8), (64, 2), (64, 6), (256, 8), (1000, 20)])
+def test_whole_softmax_with_a_leading_expert(e, k, dtype):
+    """dx_i = p_i (d_i - sum_j p_j d_j) where one expert has nearly all: its d_i - mean is about (1 - p_i) d_i."""
+    t = 60
+    logits = _logits(t, e, F32, e, 0.5)
+    lead = torch.arange(t, device="cuda") % e
+    # 0 to 29.5 above the others; a chosen expert next to it, but for the last rows
+    logits[torch.arange(t, device="cuda"), lead] = logits.amax(1) + 0.5 * torch.arange(t, device="cuda")
+    logits = logits.to(dtype)
+    g = _randn(t, k, seed=e)
+    g[::7] = 1.0                              # nothing to gain by moving between the chosen
+    run = Run(logits, k, None, None, 1, 1, "softmax", False, g)
+    x = logits.cpu().double()
+    p = torch.softmax(x, 1)
+    d = torch.zeros(t, e, dtype=torch.float64).scatter_(1, run.chosen.cpu().long(), g.cpu().double())
+    moved = p[:, :, None] * p[:, None, :] * (d[:, :, None] - d[:, None, :])
+    want = SCALE * moved.sum(2)
+    # a power is off by half a step of the difference of logits and 1.25 of its product with log2 e, and two of its own; the sum of the powers by their mean;
+    # differences and sums are in 64 bits; five roundings to 32 follow, and the result's own
+    far = (x.amax(1, keepdim=True) - x).clamp(max=110)
+    off = (2.25 * far + 4) * 2.0 ** -24
+    both = off[:, :, None] + off[:, None, :] + 2 * (p * off).sum(1)[:, None, None] + 6 * 2.0 ** -24
+    allowed = SCALE * (moved.abs() * both).sum(2) + 1.01 * HALF[dtype] * want.abs() + TINY[dtype]
+    # sums of e powers and k products in 64 bits; p below the normal numbers of 32 bits may be 0
+    allowed += SCALE * d.abs().amax(1, keepdim=True) * ((e + k + 4) * 2.0 ** -53 * p + torch.where(p < 2.0 ** -126, 2.0 ** -125, 0.0))
+    over = (run.grad.cpu().double() - want).abs() / allowed
+    assert (over <= 1).all(), (float(over.max()), int(over.amax(1).argmax()))
