@@ -105,6 +105,7 @@ class BiasTrainer(Trainer):
         self.scales = [[torch.zeros(blocks, device="cuda") for _ in range(2)] for _ in range(ranks)]
         self.norm = [torch.empty(2, device="cuda") for _ in range(ranks)]      # the gradient's norm, and what it is to be multiplied by
         self.count = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(ranks)]
+        self.moved = [torch.empty_like(self.router[0]) for _ in range(2)]      # the router's matrix and its momentum after a step
         # the router's matrix has no weights in the list: its gradient counts in the norm, its update is the orthogonalised one
         self.update = [bl.blink_make_update([self.grad[r][:split], self.grad[r][split:]], [self.table[r].view(-1), None], [self.moments[r][0], None],
                                             [self.moments[r][1], None], scales1=[self.scales[r][0], None], scales2=[self.scales[r][1], None])
@@ -142,8 +143,11 @@ class BiasTrainer(Trainer):
         for r in range(self.ranks):
             bl.blink_gradient_norm(self.update[r], self.norm[r], self.work, self.max_norm, 1.0, self.count[r], stream)
             bl.blink_adamw_step(self.update[r], self.count[r], rate, 0.9, 0.99, 1e-8, self.norm[r][1:], None, 1234, stream)
+            # AdamW leaves the step out where the factor is NaN (a gradient was no number); the other update is taken or left here, without asking the host
             router = (self.grad[r][split:] * self.norm[r][1]).view(self.dim, e)
-            bl.blink_orthogonal_step(self.router[r], self.momentum[r], router, self.router[r], self.momentum[r], self.work, rate, 0.9, True, stream=stream)
+            bl.blink_orthogonal_step(self.router[r], self.momentum[r], router, *self.moved, self.work, rate, 0.9, True, stream=stream)
+            for old, new in zip((self.router[r], self.momentum[r]), self.moved):
+                old.copy_(torch.where(torch.isnan(self.norm[r][1]), old, new))
         return torch.stack((task, self.counts[0][:e].max() * e / self.counts[0][:e].sum()))
 
 

@@ -614,7 +614,8 @@ void blink_update_free(blink_update_t* u);
 
 /* norm[0] = |factor| * the root of the sum of the squares of all gradients; norm[1] = what a step is to multiply them by: factor, times
  * max_norm / norm[0] where that is less than 1 (max_norm > 0; infinity: never), or NaN where a gradient is infinite or NaN.  factor: 1 / ranks
- * makes the mean of a sum over ranks.  step: null, or counted up by one unless norm[1] is NaN. */
+ * makes the mean of a sum over ranks.  step: null, or counted up by one unless norm[1] is NaN.  blink_adamw_step takes a NaN as "not this time"; what else
+ * steps by it (blink_orthogonal_step) is for the caller to take or leave. */
 size_t blink_gradient_norm_workspace(const blink_update_t* u);
 blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, double factor, float* norm, int32_t* step,
                                    void* workspace, size_t workspace_bytes, void* stream);

@@ -56,3 +56,27 @@ def test_one_step_against_autograd():
         g = trainer.grad[r][:split].view(60, 24).double() * float(trainer.norm[r][1])
         want = before - 0.01 * g / (g.abs() + 1e-8)
         assert (trainer.table[r].double() - want).abs().max() <= 0.01 * 16 * 2.0 ** -24 + 2.0 ** -23 * float(before.abs().max())
+
+
+def test_a_step_that_is_left_out(monkeypatch):
+    """One rank's gradient holds an infinity: no parameter, momentum, moment or count of any rank changes; the step after it is an ordinary one."""
+    import paper_1910_04940_amd as bl
+    from data_parallel_step import BiasTrainer
+    trainer = BiasTrainer(ranks=3, tokens=200, vocab=60, dim=24, experts=8)
+    trainer.step()
+    state = lambda: [t.clone() for part in (trainer.table, trainer.router, trainer.momentum, trainer.count, *trainer.moments, *trainer.scales) for t in part]   # noqa: E731
+    before, real = state(), bl.blink_allreduce
+
+    def spoiled(bufs, n, dtype, *rest):
+        if dtype == bl.BLINK_FP32:
+            bufs[1][5] = float("inf")
+        real(bufs, n, dtype, *rest)
+    monkeypatch.setattr(bl, "blink_allreduce", spoiled)
+    trainer.step()
+    assert all(torch.isnan(n[1]) for n in trainer.norm)
+    for a, b in zip(before, state()):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    monkeypatch.setattr(bl, "blink_allreduce", real)
+    trainer.step()
+    assert int(trainer.count[0]) == 2 and all(torch.isfinite(t).all() for t in trainer.table + trainer.router + trainer.momentum)
+    assert not any(torch.equal(a, b) for a, b in zip(before[:6], state()[:6]))
