@@ -613,9 +613,10 @@ blink_status_t blink_make_update(const blink_update_tensor_t* tensors /* host */
 void blink_update_free(blink_update_t* u);
 
 /* norm[0] = |factor| * the root of the sum of the squares of all gradients; norm[1] = what a step is to multiply them by: factor, times
- * max_norm / norm[0] where that is less than 1 (max_norm > 0; infinity: never), or NaN where a gradient is infinite or NaN.  factor: 1 / ranks
- * makes the mean of a sum over ranks.  step: null, or counted up by one unless norm[1] is NaN.  blink_adamw_step takes a NaN as "not this time"; what else
- * steps by it (blink_orthogonal_step) is for the caller to take or leave. */
+ * max_norm / norm[0] where that is less than 1 (max_norm > 0; infinity: never), or NaN where a gradient is infinite or NaN, or where a step in FP32
+ * could not use it: norm[1] past FP32's largest, or a length of the scaled gradients above 2^63, whose square is near it.  factor: 1 / ranks makes the
+ * mean of a sum over ranks.  step: null, or counted up by one unless norm[1] is NaN.  blink_adamw_step takes a NaN as "not this time"; what else steps
+ * by it (blink_orthogonal_step) is for the caller to take or leave. */
 size_t blink_gradient_norm_workspace(const blink_update_t* u);
 blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, double factor, float* norm, int32_t* step,
                                    void* workspace, size_t workspace_bytes, void* stream);
@@ -625,7 +626,8 @@ blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, dou
  * t = step[0] (read on the device, so that a graph's replays step on); nothing is written where it is below 1 or scale[0] is NaN.  eps > 0.
  * FP8 moments: a scale is the largest of its 256 / 448 (moments below 2^-100 are 0), and numbers are rounded up or down by random bits of seed, t, the
  * tensor's place in the list and the element's in it, up with the probability of what down would drop; a root that is not 0 is at least 2^-9
- * times its scale.  A NaN or an infinity makes its 256 elements' moments NaN.  seed is without meaning for FP32. */
+ * times its scale.  A NaN or an infinity makes its 256 elements' moments NaN.  Scaled gradients of 2^64 and more have an infinite square
+ * (after blink_gradient_norm there are none).  seed is without meaning for FP32. */
 blink_status_t blink_adamw_step(const blink_update_t* u, const int32_t* step, double lr, double beta1, double beta2, double eps,
                                 const float* scale, const float* rate, uint32_t seed, void* stream);
 

@@ -105,15 +105,18 @@ __device__ inline double add_up(double s, double (&part)[WAVES]) {   // for thre
 }
 
 // What a sum of squares makes.
+constexpr double kMostLength = 0x1p63;   // of scaled gradients: the square of one, and b2 v + (1 - b2) g^2 of two, stay below 2^127
 struct Clip {
     double most, factor;
     float* norm;
     int32_t* step;
     __device__ void finish(double s) const {
-        const bool fine = s < __builtin_inf();   // (not with an infinite gradient, nor with a NaN)
         const double length = sqrt(s) * fabs(factor);
+        const float scale = static_cast<float>(length > most ? factor * (most / length) : factor);
+        // not with an infinite gradient, nor a NaN, nor where the step, in 32 bits, could not scale the gradients or square what that makes of them
+        const bool fine = length < __builtin_inf() && fmin(length, most) <= kMostLength && fabsf(scale) < __builtin_inff();
         norm[0] = static_cast<float>(length);
-        norm[1] = fine ? static_cast<float>(length > most ? factor * (most / length) : factor) : __builtin_nanf("");
+        norm[1] = fine ? scale : __builtin_nanf("");
         if (step && fine) *step += 1;
     }
 };

@@ -389,3 +389,53 @@ def test_a_tensor_past_32_bits():
     for x, y in zip((w, m, v), tail[1:]):
         assert torch.equal(x[-last:], y)
     assert bool((w[:1 << 20] == w[0]).all()) and float(w[0]) != 0
+
+
+@pytest.mark.parametrize("weights,grads,master,eight", [(F32, F32, False, False), (F32, F32, False, True), (B16, F32, True, True), (B16, B16, False, False),
+                                                        (F32, B16, False, True)])
+def test_gradients_whose_squares_32_bits_hold(weights, grads, master, eight):
+    """A scaled length below 2^63: moments and weights as in 64 bits, and an ordinary step after it."""
+    T = Tensors([5, 1000, 4096], weights, grads, master, eight, seed=6)
+    for i, at, value in ((0, 2, 5e18), (1, 300, -3e18), (1, 301, 2e18), (1, 999, 1e15), (2, 4000, 4e18)):
+        T.lists["grads"][i][at] = T.before["grads"][i][at] = value
+    norm, step = torch.empty(2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bl.blink_gradient_norm(T.update, norm, _work(T.update), step=step, stream=_stream())
+    assert float(norm[1]) == 1 and int(step) == 1
+    for t, value in ((1, None), (2, 0.5)):
+        if value is not None:
+            T.before = {k: [v.clone() for v in views] for k, views in T.lists.items()}
+            for v in T.lists["grads"] + T.before["grads"]:
+                v.fill_(value)
+        bl.blink_adamw_step(T.update, step.fill_(t), LR, B1, B2, EPS, norm[1:], None, 5, _stream())
+        _check(T, t, seed=5)
+        assert all(torch.isfinite(v.float()).all() for views in T.lists.values() for v in views)
+
+
+# (gradient, max_norm, factor) and whether a step can be made of it
+SCALED = [(1e20, math.inf, 1.0, False), (3e38, math.inf, 1.0, False), (-1e20, math.inf, 1.0, False), (3e38, math.inf, 2.0, False), (3e38, 1e19, 1.0, False),
+          (3e38, 1e18, 2.0, True), (3e38, 1.0, -2.0, True), (9e18, math.inf, 1.0, True), (9e18, math.inf, -2.0, False), (1e-3, math.inf, 1e39, False),
+          (1e-3, 1.0, 1e39, True), (1e-30, math.inf, 1e39, False), (0.0, 1.0, 1e39, False), (1e-3, math.inf, 1e20, True)]
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("value,most,factor,fine", SCALED)
+def test_a_step_whose_squares_pass_32_bits_is_left_out(value, most, factor, fine, eight):
+    """Scaled gradients that 32 bits cannot hold or square are no step, like a gradient that is no number; clipped ones are."""
+    T = Tensors([3000], eight=eight)
+    T.lists["grads"][0].zero_()
+    T.lists["grads"][0][2999] = value
+    norm, step = torch.empty(2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    bl.blink_gradient_norm(T.update, norm, _work(T.update), most, factor, step, _stream())
+    value = float(np.float32(value))
+    if abs(factor * value) < 3.4e38:
+        assert abs(float(norm[0]) - abs(factor * value)) <= 1.01 * 2.0 ** -24 * abs(factor * value)
+    assert int(step) == fine and bool(torch.isnan(norm[1])) != fine
+    bl.blink_adamw_step(T.update, step, LR, B1, B2, EPS, norm[1:], stream=_stream())
+    if fine:
+        want = factor * min(1.0, most / abs(factor * value))
+        assert abs(float(norm[1]) - want) <= 1.01 * 2.0 ** -24 * abs(want) + 2.0 ** -150      # (half a step of numbers below 2^-126: -2 / 6e38 is one)
+        assert all(torch.isfinite(v.float()).all() for views in T.lists.values() for v in views)
+        return
+    for name, views in T.lists.items():
+        if name != "grads":
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(views, T.before[name]))
