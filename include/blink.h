@@ -608,7 +608,7 @@ typedef struct {
     size_t elements;
     blink_dtype_t weight_type, grad_type, moment_type;
     double rate, decay;      /* lr is multiplied by rate; decay: of the weights, per unit of lr * rate */
-} blink_update_tensor_t;     /* elements lie one after the other and may start anywhere, moments all 0 before the first step */
+} blink_update_tensor_t;     /* elements lie one after the other and may start anywhere, moments all 0 before the first step, scales whatever they are */
 blink_status_t blink_make_update(const blink_update_tensor_t* tensors /* host */, int n_tensors, blink_update_t** out);
 void blink_update_free(blink_update_t* u);
 

@@ -239,7 +239,9 @@ __device__ inline uint32_t encode(const float (&y)[4], const uint32_t (&up)[4], 
     return codes;
 }
 
+// Codes that are all 0 are 0 whatever the scale: before the first step nobody has written one.
 __device__ inline void decode(uint32_t codes, float scale, float (&y)[4]) {
+    scale = codes ? scale : 0.0f;
     const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), high = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
     y[0] = low[0] * scale;
     y[1] = low[1] * scale;

@@ -439,3 +439,24 @@ def test_a_step_whose_squares_pass_32_bits_is_left_out(value, most, factor, fine
     for name, views in T.lists.items():
         if name != "grads":
             assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(views, T.before[name]))
+
+
+@pytest.mark.parametrize("sizes", [[1, 300, 4097], [30_000_001, 256]])
+def test_first_step_whatever_the_scales_hold(sizes):
+    """Moments that are all 0 are 0 with any scales, those of memory that nobody has written among them."""
+    both = []
+    for fill in (0, 255):
+        T = Tensors(sizes, B16, F32, True, True)
+        for name in ("moments1", "moments2"):
+            for v in T.lists[name]:
+                v.zero_()
+        for name in ("scales1", "scales2"):
+            for v in T.lists[name]:
+                v.view(torch.uint8).fill_(fill)
+        T.lists["scales1"][0][:1] = math.inf if fill else 0.0
+        bl.blink_adamw_step(T.update, torch.ones(1, dtype=torch.int32, device="cuda"), LR, B1, B2, EPS, seed=5, stream=_stream())
+        both.append(T)
+    for name, views in both[0].lists.items():
+        for a, b in zip(views, both[1].lists[name]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), name
+    assert all(torch.isfinite(v).all() for v in both[1].lists["masters"] + both[1].lists["scales1"] + both[1].lists["scales2"])
