@@ -623,7 +623,8 @@ blink_status_t blink_gradient_norm(const blink_update_t* u, double max_norm, dou
 /* A step of AdamW on every tensor that has weights, in place, with g = scale[0] * gradient (null: 1) and r = lr * rate of the tensor * rate[0] (null: 1):
  *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - r decay) - r (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * t = step[0] (read on the device, so that a graph's replays step on); nothing is written where it is below 1 or scale[0] is NaN.  eps > 0.
+ * t = step[0] (read on the device, so that a graph's replays step on); nothing is written where it is below 1 or scale[0] is NaN.
+ * eps > 0.  FP32 loses digits of v below 2^-126 and all of it below 2^-150: for gradients that small, 1e-21 and less, an eps below them does not bound the step.
  * FP8 moments: a scale is the largest of its 256 / 448 (moments below 2^-100 are 0), and numbers are rounded up or down by random bits of seed, t, the
  * tensor's place in the list and the element's in it, up with the probability of what down would drop; a root that is not 0 is at least 2^-9
  * times its scale.  A NaN or an infinity makes its 256 elements' moments NaN.  Scaled gradients of 2^64 and more have an infinite square

@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <new>
 #include <vector>
 
@@ -560,10 +561,12 @@ blink_status_t gradient_norm(const blink_update& u, double most, double factor, 
 blink_status_t adamw_step(const blink_update& u, const int32_t* step, double lr, double beta1, double beta2, double eps, const float* scale, const float* rate,
                           uint32_t seed, hipStream_t stream) {
     BLINK_TRY(on_its_device(u));
+    // an eps that 32 bits round to 0 would divide 0 by 0 wherever nothing has moved yet
+    const float at_least = std::max(static_cast<float>(eps), std::numeric_limits<float>::denorm_min());
     for (const Kind& k : u.kinds) {
         if (!k.stepped || k.n == 0) continue;
         const Step a{u.tensors, u.pieces + k.first, k.n, step, scale, rate, lr, std::log(beta1), std::log(beta2), static_cast<float>(beta1),
-                     static_cast<float>(beta2), static_cast<float>(1 - beta1), static_cast<float>(1 - beta2), static_cast<float>(eps), seed};
+                     static_cast<float>(beta2), static_cast<float>(1 - beta1), static_cast<float>(1 - beta2), at_least, seed};
         BLINK_TRY(with_float(k.weights, [&](auto w) {
             return with_float(k.grad, [&](auto g) {
                 using W = decltype(w);

@@ -460,3 +460,15 @@ def test_first_step_whatever_the_scales_hold(sizes):
         for a, b in zip(views, both[1].lists[name]):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), name
     assert all(torch.isfinite(v).all() for v in both[1].lists["masters"] + both[1].lists["scales1"] + both[1].lists["scales2"])
+
+
+@pytest.mark.parametrize("eps", [1e-50, 5e-324])
+def test_eps_below_32_bits(eps):
+    """It is more than 0: where nothing moves nothing is divided by 0."""
+    g = torch.tensor([0.0, 1.0, -1e-3], device="cuda")
+    w, m, v = (torch.zeros(3, device="cuda") for _ in range(3))
+    w.fill_(2.0)
+    update = bl.blink_make_update([g], [w], [m], [v])
+    bl.blink_adamw_step(update, torch.ones(1, dtype=torch.int32, device="cuda"), LR, B1, B2, eps, stream=_stream())
+    assert (w.cpu() - torch.tensor([2.0, 2.0 - LR, 2.0 + LR])).abs().max() <= 10 * 2.0 ** -24 * LR + 2 * 2.0 ** -23
+    assert w[0] == 2
