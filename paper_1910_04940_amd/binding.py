@@ -226,6 +226,14 @@ def _ptr(a: np.ndarray, ctype):
     return a.ctypes.data_as(C.POINTER(ctype))
 
 
+def _handle(owner, kind):
+    """The handle in an object of that class: in another's place it would be read as what it is not."""
+    handle = owner._h
+    if not isinstance(owner, kind):
+        raise TypeError(f"{kind.__name__} wanted: got {type(owner).__name__}")
+    return handle
+
+
 class Trees:
     """Owns a blink_trees_t handle."""
 
@@ -295,7 +303,7 @@ class Schedule:
 
     def __init__(self, handle: int, k: int, n: int, op: int):
         self._h = C.c_void_p(handle)
-        self._address = handle
+        self._address = handle      # (a name of its own for every class whose handle _blinkcall takes)
         self.k, self.n, self.op = k, n, op
 
     def __del__(self):
@@ -402,7 +410,7 @@ class Schedule:
 def blink_make_schedule(trees: Trees, op: int, n_elems: int, chunk_elems: int,
                         fusion: int = BLINK_FUSE_TREE) -> Schedule:
     out = C.c_void_p()
-    _check(lib().blink_make_schedule(trees._h, op, n_elems, chunk_elems, fusion, C.byref(out)),
+    _check(lib().blink_make_schedule(_handle(trees, Trees), op, n_elems, chunk_elems, fusion, C.byref(out)),
            "blink_make_schedule")
     return Schedule(out.value, trees.k, n_elems, op)
 
@@ -414,10 +422,11 @@ def blink_make_schedule_servers(local: Sequence[Optional[Trees]], ranks: Sequenc
     global ids of its local ranks, ascending."""
     if len(local) != len(ranks):
         raise ValueError("one rank list per server")
+    given = [None if t is None else _handle(t, Trees) for t in local]
     for t, r in zip(local, ranks):
         if len(r) != (t.k if t is not None else 1):
             raise ValueError("a server's rank list must have one id per local rank")
-    handles = (C.c_void_p * len(local))(*[t._h if t is not None else None for t in local])
+    handles = (C.c_void_p * len(local))(*given)
     flat = np.ascontiguousarray([g for r in ranks for g in r], dtype=np.int32)
     out = C.c_void_p()
     _check(lib().blink_make_schedule_servers(len(local), handles, _ptr(flat, C.c_int32), n_elems,
@@ -452,7 +461,7 @@ def blink_allreduce(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule
     """bufs: k device pointers (ints) or objects with .data_ptr(); stream: hipStream_t as int."""
     status = _call(_at["blink_allreduce"], bufs, n_elems, dtype, schedule, stream)
     if status is None:
-        status = (_lib or lib()).blink_allreduce(_pointers(bufs), len(bufs), n_elems, dtype, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_allreduce(_pointers(bufs), len(bufs), n_elems, dtype, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_allreduce")
 
@@ -461,7 +470,7 @@ def blink_allreduce_noalloc(bufs: Sequence, n_elems: int, dtype: int, schedule: 
     """blink_allreduce on the library's static device block: the call allocates nothing."""
     status = _call(_at["blink_allreduce_noalloc"], bufs, n_elems, dtype, schedule, stream)
     if status is None:
-        status = (_lib or lib()).blink_allreduce_noalloc(_pointers(bufs), len(bufs), n_elems, dtype, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_allreduce_noalloc(_pointers(bufs), len(bufs), n_elems, dtype, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_allreduce_noalloc")
 
@@ -469,7 +478,7 @@ def blink_allreduce_noalloc(bufs: Sequence, n_elems: int, dtype: int, schedule: 
 def blink_broadcast(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule, stream: int = 0) -> None:
     status = _call(_at["blink_broadcast"], bufs, n_elems, dtype, schedule, stream)
     if status is None:
-        status = (_lib or lib()).blink_broadcast(_pointers(bufs), len(bufs), n_elems, dtype, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_broadcast(_pointers(bufs), len(bufs), n_elems, dtype, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_broadcast")
 
@@ -477,7 +486,7 @@ def blink_broadcast(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule
 def blink_allgather(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule, stream: int = 0) -> None:
     status = _call(_at["blink_allgather"], bufs, n_elems, dtype, schedule, stream)
     if status is None:
-        status = (_lib or lib()).blink_allgather(_pointers(bufs), len(bufs), n_elems, dtype, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_allgather(_pointers(bufs), len(bufs), n_elems, dtype, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_allgather")
 
@@ -485,7 +494,7 @@ def blink_allgather(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule
 def blink_gather(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule, stream: int = 0) -> None:
     status = _call(_at["blink_gather"], bufs, n_elems, dtype, schedule, stream)
     if status is None:
-        status = (_lib or lib()).blink_gather(_pointers(bufs), len(bufs), n_elems, dtype, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_gather(_pointers(bufs), len(bufs), n_elems, dtype, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_gather")
 
@@ -493,7 +502,7 @@ def blink_gather(bufs: Sequence, n_elems: int, dtype: int, schedule: Schedule, s
 def blink_allreduce_op(bufs: Sequence, n_elems: int, dtype: int, redop: int, schedule: Schedule, stream: int = 0) -> None:
     status = _call(_at["blink_allreduce_op"], bufs, n_elems, dtype, schedule, stream, redop)
     if status is None:
-        status = (_lib or lib()).blink_allreduce_op(_pointers(bufs), len(bufs), n_elems, dtype, redop, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_allreduce_op(_pointers(bufs), len(bufs), n_elems, dtype, redop, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_allreduce_op")
 
@@ -501,7 +510,7 @@ def blink_allreduce_op(bufs: Sequence, n_elems: int, dtype: int, redop: int, sch
 def blink_reduce(bufs: Sequence, n_elems: int, dtype: int, redop: int, schedule: Schedule, stream: int = 0) -> None:
     status = _call(_at["blink_reduce"], bufs, n_elems, dtype, schedule, stream, redop)
     if status is None:
-        status = (_lib or lib()).blink_reduce(_pointers(bufs), len(bufs), n_elems, dtype, redop, schedule._h, C.c_void_p(stream))
+        status = (_lib or lib()).blink_reduce(_pointers(bufs), len(bufs), n_elems, dtype, redop, _handle(schedule, Schedule), C.c_void_p(stream))
     if status:
         _check(status, "blink_reduce")
 

@@ -19,7 +19,7 @@
 typedef blink_status_t (*plain_fn)(void* const*, int, size_t, blink_dtype_t, blink_schedule_t*, void*);
 typedef blink_status_t (*redop_fn)(void* const*, int, size_t, blink_dtype_t, blink_redop_t, blink_schedule_t*, void*);
 
-static PyObject *data_ptr_name, *address_name;
+static PyObject *data_ptr_name, *address_name, *update_name;   /* (handles: a name for each kind) */
 
 /* A non-negative int of at most 64 bits; 0 if it is something else. */
 static int word(PyObject* o, unsigned long long* out) {
@@ -193,9 +193,9 @@ static int number(PyObject* o, float* out) {
     *out = (float)v;
     return 1;
 }
-static int owned(PyObject* o, void** handle) {   /* what a handle's owner holds */
+static int update_of(PyObject* o, void** handle) {   /* what its owner holds */
     unsigned long long w = 0;
-    const int ok = word_of(PyObject_GetAttr(o, address_name), &w);
+    const int ok = word_of(PyObject_GetAttr(o, update_name), &w);
     *handle = (void*)w;
     return ok;
 }
@@ -355,7 +355,7 @@ static PyObject* gradient_norm(PyObject* self, PyObject* const* args, Py_ssize_t
     Py_ssize_t one = 1, two = 2, size;
     void *update, *norm, *work, *step = NULL;
     double most, factor;
-    USUAL(owned(args[2], &update) && whole(types, args[3], BLINK_FP32, &two, &norm) && space(args[4], &work, &size) && precise(args[5], &most) &&
+    USUAL(update_of(args[2], &update) && whole(types, args[3], BLINK_FP32, &two, &norm) && space(args[4], &work, &size) && precise(args[5], &most) &&
           precise(args[6], &factor) && (args[7] == Py_None || whole(types, args[7], BLINK_INT32, &one, &step)));
     RUN(((__typeof__(&blink_gradient_norm))fn)(update, most, factor, norm, step, work, (size_t)size, (void*)stream));
 }
@@ -367,7 +367,7 @@ static PyObject* adamw_step(PyObject* self, PyObject* const* args, Py_ssize_t na
     unsigned long long seed;
     void *update, *step, *scale = NULL, *rate = NULL;
     double lr, beta1, beta2, eps;
-    USUAL(owned(args[2], &update) && whole(types, args[3], BLINK_INT32, &one, &step) && precise(args[4], &lr) && precise(args[5], &beta1) &&
+    USUAL(update_of(args[2], &update) && whole(types, args[3], BLINK_INT32, &one, &step) && precise(args[4], &lr) && precise(args[5], &beta1) &&
           precise(args[6], &beta2) && precise(args[7], &eps) && (args[8] == Py_None || whole(types, args[8], BLINK_FP32, &one, &scale)) &&
           (args[9] == Py_None || whole(types, args[9], BLINK_FP32, &one, &rate)) && word(args[10], &seed) && seed <= 0xffffffffu);
     RUN(((__typeof__(&blink_adamw_step))fn)(update, step, lr, beta1, beta2, eps, scale, rate, (uint32_t)seed, (void*)stream));
@@ -392,6 +392,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_blinkcall", NULL, 0
 PyMODINIT_FUNC PyInit__blinkcall(void) {
     data_ptr_name = PyUnicode_InternFromString("data_ptr");
     address_name = PyUnicode_InternFromString("_address");
+    update_name = PyUnicode_InternFromString("_update");
     dtype_name = PyUnicode_InternFromString("dtype");
     cuda_name = PyUnicode_InternFromString("is_cuda");
     shape_name = PyUnicode_InternFromString("shape");
@@ -399,6 +400,6 @@ PyMODINIT_FUNC PyInit__blinkcall(void) {
     contiguous_name = PyUnicode_InternFromString("is_contiguous");
     numel_name = PyUnicode_InternFromString("numel");
     nbytes_name = PyUnicode_InternFromString("nbytes");
-    if (!data_ptr_name || !address_name || !dtype_name || !cuda_name || !shape_name || !stride_name || !contiguous_name || !numel_name || !nbytes_name) return NULL;
+    if (!data_ptr_name || !address_name || !update_name || !dtype_name || !cuda_name || !shape_name || !stride_name || !contiguous_name || !numel_name || !nbytes_name) return NULL;
     return PyModule_Create(&module);
 }

@@ -12,7 +12,7 @@ from typing import Optional, Sequence, Tuple
 import numpy as np
 
 from . import binding
-from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_FP8, BLINK_INT32, BLINK_INT64, BLINK_SIGMOID, BLINK_SOFTMAX, _check
+from .binding import BLINK_BF16, BLINK_FP16, BLINK_FP32, BLINK_FP8, BLINK_INT32, BLINK_INT64, BLINK_SIGMOID, BLINK_SOFTMAX, _check, _handle
 
 # Five steps (a, b, c) that move every singular value above 0.003 to between 0.68 and 1.21.
 BLINK_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
@@ -297,13 +297,13 @@ class Update:
 
     def __init__(self, handle: int, tensors):
         self._h = C.c_void_p(handle)
-        self._address = handle
+        self._update = handle
         self.tensors = tensors
 
     def __del__(self):
         if getattr(self, "_h", None) and binding is not None and binding._lib is not None:
             binding._lib.blink_update_free(self._h)
-            self._h = self._address = None
+            self._h = self._update = None
 
 
 def blink_make_update(grads: Sequence, weights: Optional[Sequence] = None, moments1: Optional[Sequence] = None, moments2: Optional[Sequence] = None,
@@ -359,7 +359,7 @@ def blink_make_update(grads: Sequence, weights: Optional[Sequence] = None, momen
 
 
 def blink_gradient_norm_workspace(update: Update) -> int:
-    return binding.lib().blink_gradient_norm_workspace(update._h)
+    return binding.lib().blink_gradient_norm_workspace(_handle(update, Update))
 
 
 def blink_gradient_norm(update: Update, norm, workspace, max_norm: float = math.inf, factor: float = 1.0, step=None, stream: int = 0) -> None:
@@ -371,7 +371,7 @@ def blink_gradient_norm(update: Update, norm, workspace, max_norm: float = math.
         _check(status, "blink_gradient_norm")
     space, size = _space(workspace)
     status = (binding._lib or binding.lib()).blink_gradient_norm(
-        update._h, max_norm, factor, _whole(norm, "norm", _FP32, (2,)), None if step is None else _whole(step, "step", _INT32, (1,)), space, size, stream)
+        _handle(update, Update), max_norm, factor, _whole(norm, "norm", _FP32, (2,)), None if step is None else _whole(step, "step", _INT32, (1,)), space, size, stream)
     if status:
         _check(status, "blink_gradient_norm")
 
@@ -387,7 +387,7 @@ def blink_adamw_step(update: Update, step, lr: float, beta1: float = 0.9, beta2:
     if not 0 <= seed < 1 << 32:
         raise ValueError("seed has 32 bits")
     status = (binding._lib or binding.lib()).blink_adamw_step(
-        update._h, _whole(step, "step", _INT32, (1,)), lr, beta1, beta2, eps, None if scale is None else _whole(scale, "scale", _FP32, (1,)),
+        _handle(update, Update), _whole(step, "step", _INT32, (1,)), lr, beta1, beta2, eps, None if scale is None else _whole(scale, "scale", _FP32, (1,)),
         None if rate is None else _whole(rate, "rate", _FP32, (1,)), seed, stream)
     if status:
         _check(status, "blink_adamw_step")
