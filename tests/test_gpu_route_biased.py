@@ -469,3 +469,14 @@ def test_whole_softmax_with_a_leading_expert(e, k, dtype):
     allowed += SCALE * d.abs().amax(1, keepdim=True) * ((e + k + 4) * 2.0 ** -53 * p + torch.where(p < 2.0 ** -126, 2.0 ** -125, 0.0))
     over = (run.grad.cpu().double() - want).abs() / allowed
     assert (over <= 1).all(), (float(over.max()), int(over.amax(1).argmax()))
+
+
+@pytest.mark.parametrize("kept", [1, 2, 3])
+def test_groups_that_lie_in_one_lane(kept):
+    """Eight experts to a group and k = 8: one lane, which holds two groups, may have all that are chosen, and what comes after them."""
+    for e, dtype in ((64, B16), (64, H16), (128, B16), (128, F32), (256, H16)):
+        logits, bias = _logits(3000, e, dtype, e + kept), _bias(e, kept, 0.01)
+        logits[1::2] = logits[1::2].mul(8).round().div(8)
+        for scores in ("sigmoid", "softmax"):
+            arguments = (logits, 8, bias, None, e // 8, kept, scores, True, _randn(3000, 8))
+            _check(Run(*arguments), _want(*arguments), dtype)
