@@ -472,3 +472,29 @@ def test_eps_below_32_bits(eps):
     bl.blink_adamw_step(update, torch.ones(1, dtype=torch.int32, device="cuda"), LR, B1, B2, eps, stream=_stream())
     assert (w.cpu() - torch.tensor([2.0, 2.0 - LR, 2.0 + LR])).abs().max() <= 10 * 2.0 ** -24 * LR + 2 * 2.0 ** -23
     assert w[0] == 2
+
+
+@pytest.mark.parametrize("ratio", [0.5, 1e-2, 1e-4, 1e-6])
+def test_roots_next_to_a_larger_one(ratio):
+    """Gradients that vary, far below the largest of their block: what rounding adds to v, and the least root."""
+    n, steps, b2 = 1 << 16, 600, 0.99
+    T = Tensors([n], eight=True)
+    for name in ("moments1", "moments2", "scales1", "scales2"):
+        T.lists[name][0].zero_()
+    g = torch.Generator("cuda").manual_seed(11)
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for t in range(1, steps + 1):
+        T.lists["grads"][0].copy_(ratio * torch.randn(n, generator=g, device="cuda"))
+        T.lists["grads"][0][::256] = 1.0
+        bl.blink_adamw_step(T.update, step.fill_(t), LR, B1, b2, EPS, seed=3, stream=_stream())
+    some = torch.ones(n, dtype=torch.bool, device="cuda")
+    some[::256] = False
+    if ratio == 1e-6:      # a root that would be a fifth of the least code: sqrt(b2) of that code, rounded down to nothing or up, is the least code again
+        assert (T.lists["moments2"][0].float()[some] == 2.0 ** -9).all()
+        return
+    r = (_blocks(T.lists["moments2"][0].float()) * T.lists["scales2"][0][:, None]).view(-1)[some].double()
+    # Rounding r + d to one of two codes that are u apart adds at most |d| u to the mean of r^2.  Here d = (1 - b2)(g^2 - v) / 2r and u is r / 8 at most (r is
+    # above 2^-6 of a scale's unit): E|z^2 - 1| = 0.968 makes (1 - b2) v 0.968 / 16 a step, against (1 - b2) of the excess that is lost: 0.0605, and 1 / (1 - 0.0605)
+    # of it, for the excess itself counts in v.  v of one element varies by sqrt(2 (1 - b2) / (1 + b2)) = 0.1, their mean over 65280 by 0.0004.
+    got = float(r.square().mean()) / (ratio * ratio * (1 - b2 ** steps))
+    assert -0.003 < got - 1 < 0.0605 / (1 - 0.0605) + 0.003
