@@ -559,7 +559,12 @@ blink_status_t blink_route_gradient(const void* logits, blink_dtype_t dtype, siz
  *   chosen    [n_tokens][k], the largest a first; -1 where none is left, and for tokens left out
  *   weights   [n_tokens][k]: scale * p of the chosen (the bias is not in it), p divided by its sum over them if normalize; 0 next to a -1
  *   counts    [n_experts + 1]: tokens that chose each expert; last the tokens with a chosen one.  They add up over ranks: blink_allreduce on INT32.
- * A token that is kept with a NaN among its logits, or with softmax +inf, has no chosen experts and weights that are NaN. */
+ * A token that is kept with a NaN among its logits, or with softmax +inf, has no chosen experts and weights that are NaN.
+ * Weights are computed in FP32 from the logits of the chosen: off by about 2.5 d 2^-24 of themselves and a few roundings, d being how far a logit is below the
+ * largest of the chosen (normalized), else of the token (softmax) or below 0 (sigmoid).
+ * Tokens whose choice 32 bits leave open are chosen again in 64, by a slower kernel: about a hundredth of them, but all where scores tie at the end of the
+ * choice (logits of a router that starts from zeros, or all far above 0 under a sigmoid) or large biases leave nothing of their differences, with k > 16, and
+ * with k = 8 where one group of eight experts is kept.  Such calls take several times as long. */
 size_t blink_route_biased_workspace(size_t n_tokens, int n_experts);
 blink_status_t blink_route_biased(const void* logits, blink_dtype_t dtype, size_t n_tokens, int n_experts, size_t stride,
                                   const uint8_t* keep, const float* bias, int k, int groups, int kept_groups,
@@ -597,7 +602,8 @@ blink_status_t blink_orthogonal_step(const float* weights, float* weights_out, c
 
 /* The tensors that an optimiser changes, once for all steps: the list is read, and kept with the addresses in it, in device memory of the
  * current device (allocated and written synchronously, not while a stream is captured).  The calls below take it on that device (EMISMATCH on
- * another); it must outlive them, and graphs that hold them.  What a step writes may overlap nothing else in the list (EINVAL): weights that
+ * another); it must outlive them, and graphs that hold them, and is made again when a tensor moves (gradients that are freed and allocated between steps
+ * do: they are better kept, and zeroed).  What a step writes may overlap nothing else in the list (EINVAL): weights that
  * two names stand for are listed once. */
 typedef struct {
     const void* grad;        /* [elements], of grad_type */

@@ -137,8 +137,7 @@ __device__ inline void choose_none(const Biased& a, uint64_t token, int lane) {
 }
 
 // ---- the choice in 64 bits ----------------------------------------------------------------------------------------------------
-// A wave for each of the few tokens that two workgroups leave: so all of the kernel's workgroups are there at once (262144 x 256, 0.8 % of the tokens: 19 us,
-// 28 with a workgroup of four or eight waves to a list).
+// A wave for each of the few tokens that two workgroups leave: so all of the kernel's workgroups are there at once (see below for what that measured).
 constexpr int kExactThreads = 512;
 constexpr uint32_t kLists = 2;
 constexpr int kMostExact = 8;        // tokens of a call that are all chosen this way
@@ -349,7 +348,10 @@ struct Shared {   // of a workgroup
 };
 
 // M: how many of its N keys a lane has to know in order, as many as k at the least or all.  Tokens whose choice in 32 bits is not sure are left to
-// route_biased_exact.
+// route_biased_exact.  They are few unless a call is such that all are: logits (or their scores, far above 0) that tie at the end of the choice, as from a router
+// of zeros, or a bias so large that nothing is left of the scores' differences: 262144 x 256 then takes 740 to 760 us, 105 otherwise.  So do, with k = 8 and
+// sixteen keys to each of four or more lanes, tokens whose eight all come from one lane, which does not know its ninth: groups of eight, of which one
+// (or two that share a lane) stays.  262144 x 64 in eight groups: one kept 440 us (k = 7: 39), two 96, four 40.
 // Bound by vector instructions: 262144 x 256 bfloat16, eight groups, k = 8, 94 us, 598 a wave for four tokens (32 of them powers and reciprocals at a quarter of
 // the rate); all tokens in 64 bits took 630.  Without groups 82 us.  What brought it there: five waves on a SIMD
 // (four 103, six, which spill, 110); a lane's chosen in registers, not read from LDS for each of their uses, 2.5 %; the call's numbers asked of for each token

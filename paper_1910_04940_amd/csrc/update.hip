@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void update_squares(const Norm a) {
     s = add_up(s, part);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
-constexpr int kNormThreads = 1024;   // two sums to each at the most: 2.7 to 3.7 us of 2048, 4.1 with 256 threads
+constexpr int kNormThreads = 1024;   // two sums to each at the most: 330 sums 2.0 us, 2.2 with 256 threads; 2048 behind a list beyond the caches 4.5 to 4.7 either way
 __global__ __launch_bounds__(kNormThreads) void update_norm(const double* sums, uint32_t n, const Clip clip) {
     __shared__ double part[kNormThreads / 64];
     double s = 0.0;
@@ -349,7 +349,7 @@ struct Held {
 // W, G: types of the weights and the gradient; MASTER: weights are the rounding of a copy in 32 bits; EIGHT: moments in 8 bits.  Bound by memory.
 // Lists that read more than the memory-side cache holds go past the caches (PAST): 168 M fp32 elements, 4.7 GB, 860 us otherwise, 830 so, and 752 (6.2 TB/s)
 // with three workgroups on a unit, which follow one another closely through memory (four 790, two 835).  In 8 bits (16-bit weights with a copy,
-// 3.0 GB) there is more to compute, 97 vector instructions an element: as many workgroups as fit, both blocks of a wave loaded
+// 3.0 GB) there is more to compute, 98 vector instructions an element: as many workgroups as fit, both blocks of a wave loaded
 // before either is computed, 506 to 555 us (six TB/s at the best); with LDS for three workgroups 650, one block after the other 600.
 // Smaller lists are served by that cache when they were written a step ago: half a piece to a workgroup, 4.9 M elements 19.9 us, a whole one 21.3, past
 // the caches 27.

@@ -310,8 +310,9 @@ def blink_make_update(grads: Sequence, weights: Optional[Sequence] = None, momen
                       masters: Optional[Sequence] = None, scales1: Optional[Sequence] = None, scales2: Optional[Sequence] = None,
                       rates: Optional[Sequence[float]] = None, decays: Optional[Sequence[float]] = None) -> Update:
     """The tensors that an optimiser changes, a place in every list for each (None: it has none): contiguous, on one device.  Where weights are
-    None the gradient counts in the norm only.  Moments: float32, or float8_e4m3fn with float32 scales, one for every 256 elements;
-    zeros before the first step (scales need not be).  Nothing but gradients may overlap: weights that two names stand for are listed once."""
+    None the gradient counts in the norm only.  Moments: float32, or float8_e4m3fn with float32 scales, one for every 256 elements; zeros before
+    the first step (scales need not be).  Nothing but gradients may overlap: weights that two names stand for are listed once.  Addresses are
+    kept: a tensor that moves (a gradient that is freed after each step) needs a new list."""
     lists = {"grad": grads, "weights": weights, "master": masters, "moment1": moments1, "moment2": moments2, "scale1": scales1, "scale2": scales2}
     n = len(grads)
     if n == 0:
